@@ -25,7 +25,8 @@
  *    graph may be replayed until pnn_destroy, also after later calls with more rows.
  *  - Errors are returned as a pnn_status; the message of the last failure is available
  *    from pnn_last_error (per handle; a NULL handle gives the message of the last failed
- *    pnn_init on the calling thread).  No exception or abort crosses the interface.
+ *    pnn_init, or other call without a handle, on the calling thread).  No exception or abort
+ *    crosses the interface.
  *  - One handle must not be used from two host threads at once.
  *  - Input rows x_dev are read with 16-byte vector loads: x_dev must be 16-byte aligned
  *    (PNN_EINVAL otherwise); sizes[0] is a multiple of 8, so every row then is too.
@@ -190,8 +191,9 @@ pnn_status pnn_get_params(pnn_net* net, int32_t which, float* host_out);
  * resume: training continued from restored parameters is bitwise identical. */
 pnn_status pnn_set_params(pnn_net* net, int32_t which, const float* host_in);
 
-/* Message of the last failure on this handle ("" if none); NULL net: last pnn_init failure
- * of the calling thread.  The string lives until the next call on the same handle. */
+/* Message of the last failure on this handle ("" if none); NULL net: last failure of pnn_init, or
+ * of another call without a handle, on the calling thread.  The string lives until the next call on
+ * the same handle. */
 const char* pnn_last_error(const pnn_net* net);
 
 /* Device time of the library's kernels, for throughput accounting.  pnn_profile(net, 1)
@@ -243,6 +245,76 @@ const char* pnn_plan(const pnn_net* net);
 
 /* Releases the handle and everything it owns (NULL is ignored). */
 void pnn_destroy(pnn_net* net);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rows that name their network.  The calls above give every network a contiguous slice of the
+ * rows, or all of them; here each row names the networks that it goes through, for any number of
+ * rows per network.  These calls take no handle: every matrix, the plan and the workspaces are the
+ * caller's device memory, nothing is kept between calls, and two calls may run at the same time if
+ * they write to different memory.  All of them may be recorded into a graph.  Work runs on
+ * hip_stream and on its device (the null stream: on the current device).  A row's values are
+ * contiguous; `_ld` is the distance between rows and `_net` between networks, in values.  Rows need
+ * be aligned to their type only (16-byte alignment and widths that are multiples of 8 are faster).
+ * `type` is PNN_FP32 (fp32) or PNN_BF16_MIXED (bfloat16).  Products are summed in fp32; fp32
+ * operands enter the matrix units in three bf16 parts (six products, as exact as fp32 products),
+ * so they have to be finite and below 3.38e38: an infinite operand gives NaN in what it reaches,
+ * as a NaN does.  Results must not overlap operands. */
+
+/* Row r's per_row ids are ids_dev[r per_row + j]: pair p = r per_row + j goes through network
+ * ids_dev[p] in [0, networks); any other id drops the pair.  The same network may stand twice. */
+typedef struct {
+    const void* plan_dev; /* written by pnn_group_rows */
+    int64_t n;            /* rows, n per_row <= 2^30 */
+    int32_t per_row;      /* >= 1 */
+    int32_t networks;     /* 1..1024 */
+} pnn_groups;
+
+/* Size of the plan of a grouping. */
+pnn_status pnn_group_bytes(int64_t n, int32_t per_row, int32_t networks, int64_t* bytes);
+
+/* Groups the pairs by network: a stable counting sort.  plan_dev (plan_bytes of memory, 16-byte
+ * aligned) then holds, as int32: offsets[networks + 1], from the next multiple of four words on the
+ * pair numbers: positions offsets[e] .. offsets[e + 1) are network e's pairs in ascending order, and
+ * those from offsets[networks] on the dropped ones; then the library's own tables. */
+pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, int32_t networks, void* plan_dev,
+                          int64_t plan_bytes, void* hip_stream);
+
+/* One layer of every network: weights w_dev[e w_net + o w_ld + i], biases b_dev[e b_net + o] (fp32,
+ * NULL for none).  A weight gradient reads the sizes and the type alone. */
+typedef struct {
+    int32_t inputs, outputs; /* 1..2^20 each */
+    int32_t type;            /* of the weights, and of x, dy and a */
+    const void* w_dev;
+    int64_t w_net, w_ld;
+    const float* b_dev;
+    int64_t b_net;
+} pnn_group_layer;
+
+/* y[p] = phi(W_e x[p / per_row] + b_e) for every pair p of network e (eq. (2)-(3)); 0 for a dropped
+ * pair.  act is an elementwise pnn_act or -1 for none.  x_dev [n][inputs], y_dev [n per_row][outputs]
+ * of y_type. */
+pnn_status pnn_grouped_forward(const pnn_groups* groups, const pnn_group_layer* layer, const void* x_dev, int64_t x_ld,
+                               int32_t act, void* y_dev, int64_t y_ld, int32_t y_type, void* hip_stream);
+
+/* Workspace of the two gradients below (0 where none is needed; either pointer may be NULL). */
+pnn_status pnn_grouped_workspace(const pnn_groups* groups, const pnn_group_layer* layer, int64_t* input_bytes,
+                                 int64_t* weights_bytes);
+
+/* Hidden errors (eq. (11)): dx[r] = (sum_j W_e^T dy[r per_row + j]) (.) phi'(a[r]), the sum over the
+ * row's pairs that are not dropped, j ascending; a row without one gets 0.  dy_dev [n per_row][outputs],
+ * dx_dev [n][inputs] of dx_type.  act -1: no phi'; else a_dev [n][inputs] holds the stored activations
+ * that the slope is read from (the rectifiers' derivative is 1 unless the sign bit is set). */
+pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_layer* layer, const void* dy_dev, int64_t dy_ld,
+                                      const void* a_dev, int64_t a_ld, int32_t act, void* dx_dev, int64_t dx_ld,
+                                      int32_t dx_type, void* ws_dev, int64_t ws_bytes, void* hip_stream);
+
+/* Gradients of the weights and biases (eq. (12)-(13)): dw_e = sum_p dy[p] x[p / per_row]^T and
+ * db_e = sum_p dy[p] over network e's pairs, in fp32; 0 for a network without pairs.  db_dev may be
+ * NULL.  The sums' order depends on the sizes alone: the same call gives the same bits. */
+pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_group_layer* layer, const void* dy_dev,
+                                        int64_t dy_ld, const void* x_dev, int64_t x_ld, float* dw_dev, int64_t dw_net,
+                                        int64_t dw_ld, float* db_dev, int64_t db_net, void* ws_dev, int64_t ws_bytes,
+                                        void* hip_stream);
 
 #ifdef __cplusplus
 }

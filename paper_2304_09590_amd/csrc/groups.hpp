@@ -1,0 +1,714 @@
+// groups.hpp -- rows that name their network: grouping them, and the products of one layer of
+// every network with the rows that name it (forward, input gradient, weight gradient).
+//
+// Row r of n has per_row pairs p = r per_row + j, each naming one of K networks (or none: an id
+// outside [0, K), the pair is dropped).  The grouping is a stable counting sort of the pairs by
+// network; network e's pairs are then the positions off[e] .. off[e + 1) of `pairs`, the dropped
+// ones the positions from off[K].  The products read rows and write results through `pairs`, so
+// nothing is ever moved into sorted order: x is read at row pair / per_row, y, dy at row pair.
+//
+//   forward          y[p]  = phi(W_e x[p / per_row] + b_e), e = id[p]
+//   input gradient   dx[r] = sum_j W_e^T dy[r per_row + j] (.) phi'(a[r])
+//   weight gradient  dW_e  = sum_p dy[p] x[p / per_row]^T,  db_e = sum_p dy[p]
+#pragma once
+#include "kernels.hpp"
+
+namespace pnn {
+
+constexpr int GR_MAX_NETS = 1024;   // most networks of a grouping (its counters live in LDS)
+constexpr int GR_THREADS = 512, GR_WAVES = GR_THREADS / 64;
+constexpr int GR_MAX_BLOCKS = 256;  // most workgroups that count (each reads all their counts)
+constexpr int GR_SMALL = 16;        // pairs per tile of the kernels for few rows
+constexpr int GR_LARGE = 128;       // pairs per tile of the matrix-tile kernels
+
+// Layout of a plan (int32 words): off[K + 1] | pairs[P] | tiles of 16 pairs | tiles of 128 pairs |
+// counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
+// pairs, -1 for no tile: the host knows only the most tiles there can be.
+struct GroupPlan {
+    int64_t P;
+    int K;
+    int64_t o_pairs, o_small, o_large, o_hist, words;
+    int64_t n_small, n_large;
+    int blocks;
+    int64_t chunk;  // pairs per counting workgroup
+};
+
+__host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
+    GroupPlan g;
+    g.P = n * per_row;
+    g.K = K;
+    const int64_t extra = g.P < K + 1 ? g.P : K + 1;
+    g.n_small = g.P / GR_SMALL + extra;
+    g.n_large = g.P / GR_LARGE + extra;
+    auto up = [](int64_t v) { return (v + 3) / 4 * 4; };
+    g.o_pairs = up(K + 1);
+    g.o_small = g.o_pairs + up(g.P);
+    g.o_large = g.o_small + up(2 * g.n_small);
+    g.o_hist = g.o_large + up(2 * g.n_large);
+    g.chunk = (g.P + GR_MAX_BLOCKS - 1) / GR_MAX_BLOCKS;
+    if (g.chunk < 4096) g.chunk = 4096;
+    g.blocks = (int)((g.P + g.chunk - 1) / g.chunk);
+    g.words = g.o_hist + (g.blocks > 1 ? up((int64_t)g.blocks * (K + 1)) : 0);
+    return g;
+}
+
+struct GroupArgs {
+    const int32_t* ids;
+    int32_t *off, *pairs, *hist;
+    int2 *small, *large;
+    int64_t P, chunk, n_small, n_large;
+    int K, blocks;
+};
+
+__device__ inline int group_key(const GroupArgs& g, int64_t i) {
+    const int id = g.ids[i];
+    return (unsigned)id < (unsigned)g.K ? id : g.K;
+}
+
+// pairs of network e within this workgroup's chunk, into hist
+__global__ __launch_bounds__(GR_THREADS) void group_count_kernel(GroupArgs g) {
+    __shared__ int cnt[GR_MAX_NETS + 1];
+    for (int e = threadIdx.x; e <= g.K; e += GR_THREADS) cnt[e] = 0;
+    __syncthreads();
+    const int64_t lo = blockIdx.x * g.chunk, hi = lo + g.chunk < g.P ? lo + g.chunk : g.P;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += GR_THREADS) atomicAdd(&cnt[group_key(g, i)], 1);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= g.K; e += GR_THREADS) g.hist[(int64_t)blockIdx.x * (g.K + 1) + e] = cnt[e];
+}
+
+// exclusive scan of v[0..n) into out[0..n], by one wave; v is mapped through f first
+template <typename F>
+__device__ inline void wave_scan(int* out, int n, int lane, F f) {
+    int carry = 0;
+    for (int b = 0; b < n; b += 64) {
+        const int v = b + lane < n ? f(b + lane) : 0;
+        int s = v;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(s, d);
+            if (lane >= d) s += u;
+        }
+        if (b + lane < n) out[b + lane] = carry + s - v;
+        carry += __shfl(s, 63);
+    }
+    if (lane == 0) out[n] = carry;
+}
+
+// Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds
+// what the chunks and waves before it hold, and places its pairs; lanes with equal keys find their
+// order with one ballot per key bit.  Integer sums only: the same bits every run.  With one
+// workgroup its own counts are all there is (no earlier launch).  All workgroups share the tiles.
+__global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
+    extern __shared__ int gsm[];
+    const int K1 = g.K + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int* cur = gsm;                  // [GR_WAVES][K1]
+    int* tot = cur + GR_WAVES * K1;  // [K1]
+    int* off = tot + K1;             // [K1 + 1]
+    int* fs = off + K1 + 1;          // [K1 + 1] first small tile of each network
+    int* fl = fs + K1 + 1;           // [K1 + 1] first large tile
+    for (int e = tid; e < GR_WAVES * K1; e += GR_THREADS) cur[e] = 0;
+    __syncthreads();
+    const int64_t lo = blockIdx.x * g.chunk, hi = lo + g.chunk < g.P ? lo + g.chunk : g.P;
+    const int64_t part = (g.chunk + GR_WAVES * 64 - 1) / (GR_WAVES * 64) * 64;
+    const int64_t w0 = lo + wave * part, w1 = w0 + part < hi ? w0 + part : hi;
+    for (int64_t i = w0 + lane; i < w1; i += 64) atomicAdd(&cur[wave * K1 + group_key(g, i)], 1);
+    __syncthreads();
+    for (int e = tid; e < K1; e += GR_THREADS) {
+        int before = 0, all = 0;
+        if (g.blocks > 1)
+            for (int b = 0; b < g.blocks; ++b) {
+                const int h = g.hist[(int64_t)b * K1 + e];
+                all += h;
+                if (b < (int)blockIdx.x) before += h;
+            }
+        for (int w = 0; w < GR_WAVES; ++w) {
+            const int c = cur[w * K1 + e];
+            cur[w * K1 + e] = before;
+            before += c;
+        }
+        tot[e] = g.blocks > 1 ? all : before;
+    }
+    __syncthreads();
+    if (wave == 0) wave_scan(off, K1, lane, [&](int e) { return tot[e]; });
+    if (wave == 1) wave_scan(fs, K1, lane, [&](int e) { return (tot[e] + GR_SMALL - 1) / GR_SMALL; });
+    if (wave == 2) wave_scan(fl, K1, lane, [&](int e) { return (tot[e] + GR_LARGE - 1) / GR_LARGE; });
+    __syncthreads();
+    const int bits = 32 - __clz(g.K);
+    for (int64_t b = w0; b < w1; b += 64) {
+        const int64_t i = b + lane;
+        const bool live = i < w1;
+        const int key = live ? group_key(g, i) : 0;
+        uint64_t same = __ballot(live);
+        for (int t = 0; t < bits; ++t) {
+            const uint64_t one = __ballot((key >> t) & 1);
+            same &= ((key >> t) & 1) ? one : ~one;
+        }
+        if (live) {
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int first = __ffsll((unsigned long long)same) - 1;
+            int base = 0;
+            if (rank == 0) base = atomicAdd(&cur[wave * K1 + key], __popcll(same));
+            base = __shfl(base, first);
+            g.pairs[off[key] + base + rank] = (int)i;
+        }
+    }
+    if (blockIdx.x == 0)
+        for (int e = tid; e < K1; e += GR_THREADS) g.off[e] = off[e];
+    const int64_t step = (int64_t)gridDim.x * GR_THREADS;
+    for (int64_t t = blockIdx.x * (int64_t)GR_THREADS + tid; t < g.n_small + g.n_large; t += step) {
+        const bool s = t < g.n_small;
+        const int* f = s ? fs : fl;
+        const int64_t u = s ? t : t - g.n_small;
+        int2 v = make_int2(-1, 0);
+        if (u < f[K1]) {
+            int a = 0, b = K1;  // the last network whose first tile is at most u
+            while (b - a > 1) {
+                const int m = (a + b) >> 1;
+                if (f[m] <= u) a = m;
+                else b = m;
+            }
+            v = make_int2(a, off[a] + (int)(u - f[a]) * (s ? GR_SMALL : GR_LARGE));
+        }
+        (s ? g.small : g.large)[u] = v;
+    }
+}
+
+__host__ inline size_t group_lds(int K) { return sizeof(int) * ((size_t)GR_WAVES * (K + 1) + 4 * (K + 2)); }
+
+// ------------------------------------------------------------------------------------
+// products
+
+enum { GR_FWD = 0, GR_DX = 1, GR_DW = 2 };
+
+// m is the result's contiguous extent (outputs of a forward product, inputs of both gradients), n
+// the other one (pairs; outputs of a weight gradient), k the contraction.
+struct GroupGemm {
+    const int32_t *off, *pairs;
+    const int2* tiles;
+    int64_t n_tiles;
+    int K;
+    int M, N, Kx;              // extents; N of the pairs' products is the number of pairs, dropped ones among them,
+                               // and k of a weight gradient the group's pairs
+    const void* p;             // rows of pairs: x (forward), dy (gradients); row (pair / pdiv)
+    int64_t ldp;
+    int pdiv;
+    const void* w;             // weights; x of a weight gradient, row (pair / wdiv)
+    int64_t wnet, ldw;
+    int wdiv;
+    const float* b;            // bias (nullable)
+    int64_t bnet;
+    int act;                   // activation (forward), or the one whose slope at a scales the result; -1 none
+    const void* a;             // stored activations of the slope, row (pair)
+    int64_t lda;
+    void* y;                   // result; fp32 gradients of a weight gradient
+    int64_t ldy, ynet;
+    int vec;                   // the result's rows may be stored four values at a time
+    float* db;                 // (weight gradient) bias gradient, nullable
+    int64_t dbnet;
+    int splits;                // (weight gradient) parts of a group, summed by group_join_kernel
+    float upd;                 // (weight gradient) != 0: y -= upd / pairs * sum instead of y = sum
+    bf16_t* shadow;            // (with upd) bf16 copy of y, same strides
+};
+
+// The activations of act_fn; a NaN stays one (the rectifiers' comparison is z < 0).
+__device__ inline float group_act(int act, float z) {
+    switch (act) {
+    case ACT_SIGMOID: return 1.0f / (1.0f + expf(-z));
+    case ACT_TANH: return tanhf(z);
+    case ACT_RELU: return z < 0.0f ? -0.0f : z + 0.0f;
+    case ACT_LEAKY: return z < 0.0f ? 0.01f * z : z + 0.0f;
+    default: return z;
+    }
+}
+
+// Eight neighbouring values as loaded.  Rows may start at any multiple of the value's size: the
+// global loads of gfx950 take any alignment, so odd widths and strides cost lines, not instructions.
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef u4v u4v_a2 __attribute__((aligned(2)));
+typedef f4 f4_a4 __attribute__((aligned(4)));
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16_t> { u4v v; };
+template <> struct Raw8<float> { f4 v[2]; };
+
+// the first nv of eight values at p (the others 0); nv <= 0 reads nothing
+__device__ inline void load8(Raw8<bf16_t>& r, const bf16_t* p, int nv) {
+    if (nv >= 8) {
+        r.v = *(const u4v_a2*)p;
+    } else {
+        uint32_t q[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < nv) q[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+        r.v = u4v{q[0], q[1], q[2], q[3]};
+    }
+}
+__device__ inline void load8(Raw8<float>& r, const float* p, int nv) {
+    if (nv >= 8) {
+        r.v[0] = *(const f4_a4*)p;
+        r.v[1] = *(const f4_a4*)(p + 4);
+    } else {
+        float q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < nv) q[j] = p[j];
+        r.v[0] = f4{q[0], q[1], q[2], q[3]};
+        r.v[1] = f4{q[4], q[5], q[6], q[7]};
+    }
+}
+
+template <typename TO>
+__device__ inline void store_row4(TO* p, const float (&v)[4], int nv, bool vec) {
+    if (vec && nv >= 4) {
+        store4<TO>(p, make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < nv) p[r] = from_f<TO>(v[r]);
+    }
+}
+
+// workgroup number -> place in an order in which each XCD (its numbers are those equal mod 8) gets
+// one contiguous stretch, so that neighbours in it share an L2
+__device__ inline int64_t group_xcd(int64_t id, int64_t total) {
+    const int64_t q = total >> 3, r = total & 7, x = id & 7;
+    return x * q + (x < r ? x : r) + (id >> 3);
+}
+
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s4v lds_s4v;
+
+// An operand tile in LDS, 128 wide and BK deep, in bf16 (fp32 operands as three such planes).
+//  KC (memory runs along k): rows of BK values in 16-byte chunks; a row's chunks are permuted by
+//     XOR so that 8 and 16 neighbouring rows' reads of one chunk fall on different banks.
+//  NC (memory runs across k): rows of 128 values, one per k, in 32-byte blocks, permuted by XOR so
+//     that the rows which one transposing read touches fall on different banks.
+template <bool KC, int BK>
+struct GTile {
+    static constexpr int ELEMS = 128 * BK, CPR = KC ? BK / 8 : 16;
+    static __device__ inline int row(int s) { return s / CPR; }
+    static __device__ inline int chunk(int s) { return s % CPR; }
+    static __device__ inline int key(int r) {
+        if (KC) return CPR == 8 ? (r & 7) ^ ((r >> 3) & 1) : ((r >> 1) & 3) ^ ((r >> 3) & 1);
+        return (r & 3) | ((r >> 1) & 4);
+    }
+    static __device__ inline int offset(int r, int c) {
+        if (KC) return r * BK + (c ^ key(r)) * 8;
+        return r * 128 + (((c >> 1) ^ key(r)) << 4) + (c & 1) * 8;
+    }
+    // operand fragment of the 16 x 16 x 32 instruction: index t0 + (lane & 15), k kb + 8 (lane >> 4) ..
+    static __device__ inline bf8v frag(const bf16_t* lds, int t0, int kb, int lane) {
+        const int l15 = lane & 15, kg = lane >> 4;
+        if (KC) return *(const bf8v*)(lds + offset(t0 + l15, kb / 8 + kg));
+        const int r = kb + 8 * kg + (l15 >> 2);
+        const bf16_t* q = lds + r * 128 + (((t0 >> 4) ^ key(r)) << 4) + (l15 & 3) * 4;
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)q);
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(q + 4 * 128));
+        const s4v both[2] = {lo, hi};
+        return __builtin_bit_cast(bf8v, both);
+    }
+};
+
+__device__ inline void gt_store(bf16_t* lds, int plane, const Raw8<bf16_t>& r) { *(u4v*)lds = r.v; }
+__device__ inline void gt_store(bf16_t* lds, int plane, const Raw8<float>& r) {
+    uint32_t h[4], m[4], l[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) split3_pk(r.v[d >> 1][2 * (d & 1)], r.v[d >> 1][2 * (d & 1) + 1], h[d], m[d], l[d]);
+    *(u4v*)lds = u4v{h[0], h[1], h[2], h[3]};
+    *(u4v*)(lds + plane) = u4v{m[0], m[1], m[2], m[3]};
+    *(u4v*)(lds + 2 * plane) = u4v{l[0], l[1], l[2], l[3]};
+}
+
+// 128 x 128 tiles of one network's product, four waves of 64 x 64.
+template <int DIR, typename T, typename TO>
+__global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int BK = F32 ? 32 : 64, PL = F32 ? 3 : 1;
+    typedef GTile<DIR == GR_FWD, BK> TA;
+    typedef GTile<DIR != GR_DW, BK> TB;
+    constexpr int U = TA::ELEMS / 8 / 256;
+    __shared__ __align__(16) bf16_t lds[2 * PL * TA::ELEMS];
+    bf16_t *la = lds, *lb = lds + PL * TA::ELEMS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, kg = lane >> 4;
+    const int mt = (g.M + 127) / 128;
+    const int64_t id = group_xcd(blockIdx.x, gridDim.x);
+    int e, m0, n0 = 0, nv, split = 0, p0, Kx;
+    if (DIR == GR_DW) {
+        const int nt = (g.N + 127) / 128;
+        m0 = (int)(id % mt) * 128;
+        n0 = (int)(id / mt % nt) * 128;
+        e = (int)(id / mt / nt % g.K);
+        split = (int)(id / mt / nt / g.K);
+        nv = g.N - n0 < 128 ? g.N - n0 : 128;
+        const int first = g.off[e], all = g.off[e + 1] - first;
+        const int part = (all + g.splits * BK - 1) / (g.splits * BK) * BK;
+        p0 = first + (split * part < all ? split * part : all);
+        Kx = first + all - p0 < part ? first + all - p0 : part;
+    } else {
+        // eight tiles of pairs next to each other, then along m: their rows and weights stay in L2
+        const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
+        const int64_t left = g.n_tiles - grp * 8, wide = left < 8 ? left : 8;
+        const int2 t = g.tiles[grp * 8 + in % wide];
+        m0 = (int)(in / wide) * 128;
+        e = t.x;
+        if (e < 0) return;
+        p0 = t.y;
+        const int end = e < g.K ? g.off[e + 1] : g.N;
+        nv = end - p0 < 128 ? end - p0 : 128;
+        Kx = e < g.K ? g.Kx : 0;  // (dropped pairs: nothing to sum)
+    }
+    const int mv = g.M - m0 < 128 ? g.M - m0 : 128;
+    f4 acc[4][4], accb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        accb[i] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f4{0, 0, 0, 0};
+    }
+    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
+
+    // this thread's chunks of a tile
+    const T *pa[U], *pb[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int s = u * 256 + tid;
+        if (DIR == GR_FWD) {
+            const int r = TA::row(s);
+            pa[u] = r < mv ? (const T*)g.w + e * g.wnet + (int64_t)(m0 + r) * g.ldw + TA::chunk(s) * 8 : nullptr;
+        }
+        if (DIR != GR_DW) {
+            const int r = TB::row(s);
+            pb[u] = r < nv && Kx > 0 ? (const T*)g.p + (int64_t)(g.pairs[p0 + r] / g.pdiv) * g.ldp + TB::chunk(s) * 8 : nullptr;
+        }
+    }
+    Raw8<T> ra[U], rb[U];
+    auto load = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = u * 256 + tid;
+            if (DIR == GR_FWD) {
+                load8(ra[u], pa[u] + k0, pa[u] ? Kx - k0 - TA::chunk(s) * 8 : 0);
+            } else if (DIR == GR_DX) {
+                const int r = TA::row(s), c = TA::chunk(s) * 8;
+                load8(ra[u], (const T*)g.w + e * g.wnet + (int64_t)(k0 + r) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
+            }
+            if (DIR != GR_DW) {
+                load8(rb[u], pb[u] + k0, pb[u] ? Kx - k0 - TB::chunk(s) * 8 : 0);
+            } else {
+                const int r = TA::row(s), c = TA::chunk(s) * 8;
+                const int pair = k0 + r < Kx ? g.pairs[p0 + k0 + r] : 0;
+                load8(ra[u], (const T*)g.w + (int64_t)(pair / g.wdiv) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
+                load8(rb[u], (const T*)g.p + (int64_t)pair * g.ldp + n0 + c, k0 + r < Kx ? nv - c : 0);
+            }
+        }
+    };
+    if (Kx > 0) load(0);
+    for (int k0 = 0; k0 < Kx; k0 += BK) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = u * 256 + tid;
+            gt_store(la + TA::offset(TA::row(s), TA::chunk(s)), TA::ELEMS, ra[u]);
+            gt_store(lb + TB::offset(TB::row(s), TB::chunk(s)), TB::ELEMS, rb[u]);
+        }
+        __syncthreads();
+        if (k0 + BK < Kx) load(k0 + BK);
+#pragma unroll
+        for (int kb = 0; kb < BK; kb += 32) {
+            bf8v fa[PL][4];
+#pragma unroll
+            for (int q = 0; q < PL; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fa[q][i] = TA::frag(la + q * TA::ELEMS, wm + 16 * i, kb, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf8v fb[PL];
+#pragma unroll
+                for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, wn + 16 * j, kb, lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    // fp32: the six products of parts above 2^-24 of the whole, the smallest first
+                    if constexpr (F32) {
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][i], fb[1], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[2][i], fb[0], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[2], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][i], fb[0], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[1], acc[i][j], 0, 0, 0);
+                    }
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[0], acc[i][j], 0, 0, 0);
+                }
+                if (bias_rows) {  // sums over k: a product with ones
+                    const bf16_t one = 0x3f80;
+                    const uint32_t two = one | (uint32_t)one << 16;
+                    const u4v ones4 = {two, two, two, two};
+                    const bf8v ones = __builtin_bit_cast(bf8v, ones4);
+#pragma unroll
+                    for (int q = PL - 1; q >= 0; --q) accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fb[q], accb[j], 0, 0, 0);
+                }
+            }
+        }
+    }
+    // a lane holds results m0 + wm + 16 i + 4 kg + r of column n = wn + 16 j + l15
+    if (DIR == GR_DW) {
+        const int pairs = g.off[e + 1] - g.off[e];
+        const float scale = g.upd != 0.0f && pairs > 0 ? g.upd / (float)pairs : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = wn + 16 * j + l15;
+            if (n >= nv) continue;
+            float* y = (float*)g.y + ((int64_t)split * g.K + e) * g.ynet + (int64_t)(n0 + n) * g.ldy;
+            if (g.upd != 0.0f && pairs == 0) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int m = m0 + wm + 16 * i + 4 * kg, left = g.M - m;
+                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                if (g.upd != 0.0f)
+                    for (int r = 0; r < 4; ++r)
+                        if (r < left) {
+                            v[r] = y[m + r] - scale * v[r];
+                            if (g.shadow) g.shadow[e * g.ynet + (int64_t)(n0 + n) * g.ldy + m + r] = f2bf(v[r]);
+                        }
+                store_row4<float>(y + m, v, left, g.vec);
+            }
+            if (bias_rows && kg == 0) {
+                float* db = g.db + ((int64_t)split * g.K + e) * g.dbnet + n0 + n;
+                *db = g.upd != 0.0f ? *db - scale * accb[j][0] : accb[j][0];
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = wn + 16 * j + l15;
+        if (n >= nv) continue;
+        const int64_t pair = g.pairs[p0 + n];
+        TO* y = (TO*)g.y + pair * g.ldy;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + wm + 16 * i + 4 * kg, left = g.M - m;
+            float v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                v[r] = acc[i][j][r];
+                if (r >= left || e == g.K) continue;
+                if (DIR == GR_FWD) {
+                    if (g.b) v[r] += g.b[e * g.bnet + m + r];
+                    v[r] = group_act(g.act, v[r]);
+                } else if (g.a) {
+                    v[r] *= act_deriv(g.act, to_f<T>(((const T*)g.a)[pair * g.lda + m + r]));
+                }
+            }
+            store_row4<TO>(y + m, v, left, g.vec);
+        }
+    }
+}
+
+// the sum of a weight gradient's parts, in their order; with upd the update
+struct GroupJoin {
+    const int32_t* off;
+    const float *part, *dbpart;   // [splits][K][N][M], [splits][K][N]
+    int K, M, N, splits;
+    float* y;
+    int64_t ldy, ynet;
+    float* db;
+    int64_t dbnet;
+    float upd;
+    bf16_t* shadow;
+};
+
+__global__ __launch_bounds__(256) void group_join_kernel(GroupJoin g) {
+    const int64_t per = (int64_t)g.N * g.M, all = (int64_t)g.K * per, nb = g.db ? (int64_t)g.K * g.N : 0;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all + nb; i += gridDim.x * 256ll) {
+        const bool w = i < all;
+        const int64_t q = w ? i : i - all, step = w ? all : nb;
+        const float* p = w ? g.part : g.dbpart;
+        float s = p[q];
+        for (int k = 1; k < g.splits; ++k) s += p[k * step + q];
+        const int e = (int)(w ? q / per : q / g.N);
+        const int64_t in = w ? q - e * per : q - (int64_t)e * g.N;
+        float* out = w ? g.y + e * g.ynet + in / g.M * g.ldy + in % g.M : g.db + e * g.dbnet + in;
+        if (g.upd != 0.0f) {
+            const int pairs = g.off[e + 1] - g.off[e];
+            if (pairs == 0) continue;
+            s = *out - g.upd / (float)pairs * s;
+            if (w && g.shadow) g.shadow[out - g.y] = f2bf(s);
+        }
+        *out = s;
+    }
+}
+
+// dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r])
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part, int64_t n, int per_row, int M, const T* a,
+                                                              int64_t lda, int act, TO* dx, int64_t ldx) {
+    const int64_t all = n * M;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+        const int64_t r = i / M;
+        const int m = (int)(i - r * M);
+        float s = 0.0f;
+        for (int j = 0; j < per_row; ++j) s += part[(r * per_row + j) * M + m];
+        if (a) s *= act_deriv(act, to_f<T>(a[r * lda + m]));
+        dx[r * ldx + m] = from_f<TO>(s);
+    }
+}
+
+// Few pairs a network: 16 pairs and a band of the weights per workgroup, whose four waves split the
+// contraction and add their sums in order through LDS.  The weights go straight from memory into the
+// matrix instructions' operands, whole 128-byte lines at a time (k is permuted the same way in both
+// operands), and are read once: bound by the weights' bytes.
+constexpr int GS_OUT = 32;  // outputs of a workgroup (forward)
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int STEP = F32 ? 32 : 64, W = STEP / 4;  // values of a lane per step
+    __shared__ float part[4][GS_OUT / 16][16][20];
+    const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int mt = (g.M + GS_OUT - 1) / GS_OUT;
+    const int64_t id = blockIdx.x;
+    const int2 t = g.tiles[id / mt];
+    const int e = t.x, m0 = (int)(id % mt) * GS_OUT, p0 = t.y;
+    if (e < 0) return;
+    const int end = e < g.K ? g.off[e + 1] : g.N;
+    const int nv = end - p0 < 16 ? end - p0 : 16;
+    f4 acc[GS_OUT / 16];
+#pragma unroll
+    for (int i = 0; i < GS_OUT / 16; ++i) acc[i] = f4{0, 0, 0, 0};
+    if (e < g.K) {
+        const int share = (g.Kx + 4 * STEP - 1) / (4 * STEP) * STEP;
+        const int k1 = (wave + 1) * share < g.Kx ? (wave + 1) * share : g.Kx;
+        const T* x = l15 < nv ? (const T*)g.p + (int64_t)(g.pairs[p0 + l15] / g.pdiv) * g.ldp : nullptr;
+        const T* w[GS_OUT / 16];
+#pragma unroll
+        for (int i = 0; i < GS_OUT / 16; ++i)
+            w[i] = m0 + 16 * i + l15 < g.M ? (const T*)g.w + e * g.wnet + (int64_t)(m0 + 16 * i + l15) * g.ldw : nullptr;
+        for (int kk = wave * share; kk < k1; kk += STEP) {
+            const int k = kk + kg * W;
+            Raw8<T> rx[W / 8], rw[GS_OUT / 16][W / 8];
+#pragma unroll
+            for (int h = 0; h < W / 8; ++h) {
+                load8(rx[h], x + k + 8 * h, x ? k1 - k - 8 * h : 0);
+#pragma unroll
+                for (int i = 0; i < GS_OUT / 16; ++i) load8(rw[i][h], w[i] + k + 8 * h, w[i] ? k1 - k - 8 * h : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < GS_OUT / 16; ++i)
+#pragma unroll
+                for (int h = 0; h < W / 8; ++h) {
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(rw[i][h].v[c >> 2][c & 3], rx[h].v[c >> 2][c & 3], acc[i], 0, 0, 0);
+                    } else {
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, rw[i][h].v),
+                                                                         __builtin_bit_cast(bf8v, rx[h].v), acc[i], 0, 0, 0);
+                    }
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < GS_OUT / 16; ++i) *(f4*)&part[wave][i][l15][4 * kg] = acc[i];
+    __syncthreads();
+    const int n = tid >> 4, i = (tid >> 3) & 1, o = (tid & 7) * 2;
+    if (n >= nv) return;
+    const int64_t pair = g.pairs[p0 + n];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int m = m0 + 16 * i + o + r;
+        if (m >= g.M) continue;
+        float v = 0.0f;
+        if (e < g.K) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v += part[q][i][n][o + r];
+            if (g.b) v += g.b[e * g.bnet + m];
+            v = group_act(g.act, v);
+        }
+        ((TO*)g.y)[pair * g.ldy + m] = from_f<TO>(v);
+    }
+}
+
+// The input gradient of few pairs: lanes hold C neighbouring columns of eight (bf16) or four (fp32)
+// rows of W; column c of all of them is one operand, so the columns of an instruction are C apart.
+template <typename T, typename TO>
+__global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int C = F32 ? 4 : 8, BAND = 16 * C, STEP = F32 ? 16 : 32;
+    __shared__ float part[4][16][BAND + 4];
+    const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, kg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int mt = (g.M + BAND - 1) / BAND;
+    const int64_t id = blockIdx.x;
+    const int2 t = g.tiles[id / mt];
+    const int e = t.x, m0 = (int)(id % mt) * BAND, p0 = t.y;
+    if (e < 0) return;
+    const int end = e < g.K ? g.off[e + 1] : g.N;
+    const int nv = end - p0 < 16 ? end - p0 : 16;
+    f4 acc[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] = f4{0, 0, 0, 0};
+    if (e < g.K) {
+        const int share = (g.Kx + 4 * STEP - 1) / (4 * STEP) * STEP;
+        const int k1 = (wave + 1) * share < g.Kx ? (wave + 1) * share : g.Kx;
+        const T* d = l15 < nv ? (const T*)g.p + (int64_t)(g.pairs[p0 + l15] / g.pdiv) * g.ldp : nullptr;
+        const int cols = g.M - m0 - C * l15;
+        const T* w = (const T*)g.w + e * g.wnet + m0 + C * l15;
+        for (int kk = wave * share; kk < k1; kk += STEP) {
+            const int k = kk + kg * (STEP / 4);
+            if constexpr (F32) {
+                float dv[4], wv[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dv[j] = d && k + j < k1 ? d[k + j] : 0.0f;
+                    const int c4 = k + j < k1 ? cols : 0;
+                    if (c4 >= 4) {
+                        const f4 q = *(const f4_a4*)(w + (int64_t)(k + j) * g.ldw);
+                        wv[j][0] = q[0]; wv[j][1] = q[1]; wv[j][2] = q[2]; wv[j][3] = q[3];
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) wv[j][c] = c < c4 ? w[(int64_t)(k + j) * g.ldw + c] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(wv[j][c], dv[j], acc[c], 0, 0, 0);
+            } else {
+                Raw8<T> rd, rw[8];
+                load8(rd, d + k, d ? k1 - k : 0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) load8(rw[j], w + (int64_t)(k + j) * g.ldw, k + j < k1 ? cols : 0);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+                    u4v q;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) q[h] = __builtin_amdgcn_perm(rw[2 * h + 1].v[c >> 1], rw[2 * h].v[c >> 1], sel);
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, q), __builtin_bit_cast(bf8v, rd.v),
+                                                                     acc[c], 0, 0, 0);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[wave][l15][C * (4 * kg + r) + c] = acc[c][r];
+    __syncthreads();
+    const int n = tid >> 4;
+    if (n >= nv) return;
+    const int64_t pair = g.pairs[p0 + n];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int q = (tid & 15) + 16 * c, m = m0 + q;
+        if (m >= g.M) continue;
+        float v = 0.0f;
+        if (e < g.K) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) v += part[s][n][q];
+            if (g.a) v *= act_deriv(g.act, to_f<T>(((const T*)g.a)[pair * g.lda + m]));
+        }
+        ((TO*)g.y)[pair * g.ldy + m] = from_f<TO>(v);
+    }
+}
+
+}  // namespace pnn

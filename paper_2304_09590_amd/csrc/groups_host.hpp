@@ -1,0 +1,311 @@
+// groups_host.hpp -- C ABI of the grouping and of the grouped products (declared in pnn.h).
+// Included by pnn.hip, whose helpers it uses.
+
+namespace {
+
+// The device that a stream belongs to is the current one for the time of a call (the null stream
+// takes the current device as it is).
+struct OnDeviceOf {
+    int before = -1;
+    explicit OnDeviceOf(hipStream_t s) {
+        hipDevice_t dev = -1;
+        int cur = -1;
+        if (!s || hipStreamGetDevice(s, &dev) != hipSuccess || hipGetDevice(&cur) != hipSuccess || dev == cur) {
+            if (s) (void)hipGetLastError();
+            return;
+        }
+        if (hipSetDevice(dev) == hipSuccess) before = cur;
+    }
+    ~OnDeviceOf() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+pnn_status launched(const char* what) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(nullptr, PNN_EHIP, "%s failed to launch: %s", what, hipGetErrorString(e));
+    return PNN_OK;
+}
+
+constexpr int64_t GROUP_MAX_PAIRS = int64_t(1) << 30;
+constexpr int32_t GROUP_MAX_WIDTH = 1 << 20;
+
+pnn_status check_groups(int64_t n, int32_t per_row, int32_t networks) {
+    if (n < 0) return fail(nullptr, PNN_ESHAPE, "n = %lld < 0", (long long)n);
+    if (per_row < 1) return fail(nullptr, PNN_EINVAL, "per_row = %d (must be >= 1)", per_row);
+    if (networks < 1 || networks > GR_MAX_NETS)
+        return fail(nullptr, PNN_EINVAL, "networks = %d (must be in 1..%d)", networks, GR_MAX_NETS);
+    if (n > GROUP_MAX_PAIRS / per_row)
+        return fail(nullptr, PNN_ESHAPE, "%lld rows of %d networks are more than 2^30 pairs", (long long)n, per_row);
+    return PNN_OK;
+}
+
+pnn_status check_groups(const pnn_groups* g) {
+    if (!g) return fail(nullptr, PNN_EINVAL, "groups is NULL");
+    TRY(check_groups(g->n, g->per_row, g->networks));
+    if (g->n > 0 && !g->plan_dev) return fail(nullptr, PNN_EINVAL, "plan_dev is NULL");
+    if (((uintptr_t)g->plan_dev & 15) != 0) return fail(nullptr, PNN_EINVAL, "plan_dev is not 16-byte aligned");
+    return PNN_OK;
+}
+
+size_t type_size(int32_t type) { return type == PNN_FP32 ? 4 : 2; }
+
+// a matrix argument: present, its rows at least as far apart as they are wide, aligned to its type
+pnn_status check_rows(const char* name, const void* p, int64_t ld, int64_t width, int32_t type) {
+    if (!p) return fail(nullptr, PNN_EINVAL, "%s is NULL", name);
+    if (type != PNN_FP32 && type != PNN_BF16_MIXED) return fail(nullptr, PNN_EINVAL, "unknown type %d of %s", type, name);
+    if (((uintptr_t)p & (type_size(type) - 1)) != 0) return fail(nullptr, PNN_EINVAL, "%s is not aligned to its type", name);
+    if (ld < width) return fail(nullptr, PNN_EINVAL, "the rows of %s are %lld apart and %lld wide", name, (long long)ld, (long long)width);
+    return PNN_OK;
+}
+
+pnn_status check_layer(const pnn_group_layer* l, bool weights) {
+    if (!l) return fail(nullptr, PNN_EINVAL, "layer is NULL");
+    if (l->inputs < 1 || l->inputs > GROUP_MAX_WIDTH || l->outputs < 1 || l->outputs > GROUP_MAX_WIDTH)
+        return fail(nullptr, PNN_EINVAL, "a layer of %d inputs and %d outputs (each must be in 1..%d)", l->inputs, l->outputs,
+                    GROUP_MAX_WIDTH);
+    if (l->type != PNN_FP32 && l->type != PNN_BF16_MIXED) return fail(nullptr, PNN_EINVAL, "unknown type %d of a layer", l->type);
+    if (!weights) return PNN_OK;
+    TRY(check_rows("w_dev", l->w_dev, l->w_ld, l->inputs, l->type));
+    if (l->w_net < 0 || l->b_net < 0) return fail(nullptr, PNN_EINVAL, "negative stride between networks");
+    if (((uintptr_t)l->b_dev & 3) != 0) return fail(nullptr, PNN_EINVAL, "b_dev is not aligned to its type");
+    return PNN_OK;
+}
+
+pnn_status check_act(int32_t act) {
+    if (act < -1 || act > PNN_LEAKY_RELU)
+        return fail(nullptr, PNN_EINVAL, "activation %d (-1 for none, or an elementwise pnn_act)", act);
+    return PNN_OK;
+}
+
+GroupGemm group_base(const pnn_groups* g, bool few) {
+    const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
+    const int32_t* w = (const int32_t*)g->plan_dev;
+    GroupGemm a;
+    memset(&a, 0, sizeof a);
+    a.off = w;
+    a.pairs = w + p.o_pairs;
+    a.tiles = (const int2*)(w + (few ? p.o_small : p.o_large));
+    a.n_tiles = few ? p.n_small : p.n_large;
+    a.K = g->networks;
+    a.N = (int)p.P;
+    a.pdiv = a.wdiv = 1;
+    a.act = -1;
+    a.splits = 1;
+    return a;
+}
+
+// Tiles of 16 pairs re-read the weights for each of them, tiles of 128 multiply what is not there.
+bool few_pairs(const pnn_groups* g) { return g->n * g->per_row <= 24 * (int64_t)g->networks; }
+
+bool store4_ok(const void* p, int64_t ld, int64_t net, int32_t type) {
+    const int64_t a = 4 * (int64_t)type_size(type);
+    return (uintptr_t)p % a == 0 && ld % 4 == 0 && net % 4 == 0;
+}
+
+// parts of a group's pairs in a weight gradient: with fewer workgroups than two per CU the groups
+// are split until there are as many, as long as a part keeps 512 pairs in the mean
+int group_splits(int64_t P, int32_t K, int32_t inputs, int32_t outputs) {
+    const int64_t tiles = (int64_t)K * ((inputs + 127) / 128) * ((outputs + 127) / 128);
+    int64_t s = (512 + tiles - 1) / tiles;
+    s = std::min(s, P / K / 512);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
+}
+
+pnn_status grid_fits(int64_t blocks) {
+    if (blocks > INT32_MAX) return fail(nullptr, PNN_ESHAPE, "%lld workgroups are more than a launch takes", (long long)blocks);
+    return PNN_OK;
+}
+
+template <int DIR, typename T, typename TO>
+pnn_status run_group_pairs(const GroupGemm& a, bool few, hipStream_t s) {
+    const int band = !few ? 128 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128;
+    const int64_t blocks = (a.M + band - 1) / band * a.n_tiles;
+    TRY(grid_fits(blocks));
+    if (!few) group_tile_kernel<DIR, T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else group_few_dx_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
+    return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
+}
+
+template <int DIR>
+pnn_status run_group_pairs(const GroupGemm& a, int32_t type, int32_t out_type, bool few, hipStream_t s) {
+    if (type == PNN_FP32)
+        return out_type == PNN_FP32 ? run_group_pairs<DIR, float, float>(a, few, s) : run_group_pairs<DIR, float, bf16_t>(a, few, s);
+    return out_type == PNN_FP32 ? run_group_pairs<DIR, bf16_t, float>(a, few, s) : run_group_pairs<DIR, bf16_t, bf16_t>(a, few, s);
+}
+
+// weight gradient (upd = 0), or the update y -= upd / pairs * gradient
+pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t outputs, int32_t type, const void* dy, int64_t dy_ld,
+                             const void* x, int64_t x_ld, int xdiv, float* dw, int64_t dw_net, int64_t dw_ld, float* db,
+                             int64_t db_net, float upd, bf16_t* shadow, void* ws, hipStream_t s) {
+    GroupGemm a = group_base(g, false);
+    const int S = group_splits((int64_t)g->n * g->per_row, g->networks, inputs, outputs);
+    a.M = inputs; a.N = outputs;
+    a.p = dy; a.ldp = dy_ld;
+    a.w = x; a.ldw = x_ld; a.wdiv = xdiv;
+    a.splits = S;
+    float* dbpart = (float*)ws + (int64_t)S * g->networks * inputs * outputs;
+    if (S > 1) {
+        a.y = ws; a.ldy = inputs; a.ynet = (int64_t)inputs * outputs;
+        a.db = db ? dbpart : nullptr; a.dbnet = outputs;
+    } else {
+        a.y = dw; a.ldy = dw_ld; a.ynet = dw_net;
+        a.db = db; a.dbnet = db_net;
+        a.upd = upd; a.shadow = shadow;
+    }
+    a.vec = store4_ok(a.y, a.ldy, a.ynet, PNN_FP32);
+    const int64_t blocks = (int64_t)S * g->networks * ((inputs + 127) / 128) * ((outputs + 127) / 128);
+    TRY(grid_fits(blocks));
+    if (type == PNN_FP32) group_tile_kernel<GR_DW, float, float><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks, 256, 0, s>>>(a);
+    TRY(launched("grouped weight gradient"));
+    if (S > 1) {
+        GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, upd, shadow};
+        const int64_t all = (int64_t)g->networks * outputs * (inputs + 1);
+        group_join_kernel<<<(unsigned)std::min<int64_t>((all + 255) / 256, 8192), 256, 0, s>>>(j);
+        TRY(launched("sum of a grouped weight gradient"));
+    }
+    return PNN_OK;
+}
+
+int64_t group_input_ws(const pnn_groups* g, int32_t inputs) {
+    return g->per_row > 1 ? g->n * g->per_row * (int64_t)inputs * 4 : 0;
+}
+int64_t group_weights_ws(const pnn_groups* g, int32_t inputs, int32_t outputs) {
+    const int S = group_splits(g->n * g->per_row, g->networks, inputs, outputs);
+    return S > 1 ? (int64_t)S * g->networks * outputs * ((int64_t)inputs + 1) * 4 : 0;
+}
+
+pnn_status check_ws(const void* ws, int64_t have, int64_t need) {
+    if (need == 0) return PNN_OK;
+    if (!ws || have < need) return fail(nullptr, PNN_ESHAPE, "the call needs %lld bytes of workspace and has %lld", (long long)need, (long long)(ws ? have : 0));
+    if (!aligned16(ws)) return fail(nullptr, PNN_EINVAL, "ws_dev is not 16-byte aligned");
+    return PNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+pnn_status pnn_group_bytes(int64_t n, int32_t per_row, int32_t networks, int64_t* bytes) {
+    TRY(check_groups(n, per_row, networks));
+    if (!bytes) return fail(nullptr, PNN_EINVAL, "bytes is NULL");
+    *bytes = group_plan(n, per_row, networks).words * 4;
+    return PNN_OK;
+}
+
+pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, int32_t networks, void* plan_dev,
+                          int64_t plan_bytes, void* hip_stream) {
+    TRY(check_groups(n, per_row, networks));
+    const GroupPlan p = group_plan(n, per_row, networks);
+    if (!plan_dev || (n > 0 && !ids_dev)) return fail(nullptr, PNN_EINVAL, "ids_dev / plan_dev is NULL");
+    if (!aligned16(plan_dev)) return fail(nullptr, PNN_EINVAL, "plan_dev is not 16-byte aligned");
+    if (((uintptr_t)ids_dev & 3) != 0) return fail(nullptr, PNN_EINVAL, "ids_dev is not aligned to its type");
+    if (plan_bytes < p.words * 4)
+        return fail(nullptr, PNN_ESHAPE, "the plan needs %lld bytes and has %lld", (long long)p.words * 4, (long long)plan_bytes);
+    hipStream_t s = (hipStream_t)hip_stream;
+    OnDeviceOf dev(s);
+    int32_t* w = (int32_t*)plan_dev;
+    GroupArgs a = {ids_dev, w, w + p.o_pairs, w + p.o_hist, (int2*)(w + p.o_small), (int2*)(w + p.o_large),
+                   p.P, p.chunk, p.n_small, p.n_large, p.K, p.blocks};
+    if (p.blocks > 1) {
+        group_count_kernel<<<(unsigned)p.blocks, GR_THREADS, 0, s>>>(a);
+        TRY(launched("counting the groups"));
+    }
+    group_place_kernel<<<(unsigned)std::max(p.blocks, 1), GR_THREADS, group_lds(p.K), s>>>(a);
+    return launched("placing the groups");
+}
+
+pnn_status pnn_grouped_forward(const pnn_groups* groups, const pnn_group_layer* layer, const void* x_dev, int64_t x_ld,
+                               int32_t act, void* y_dev, int64_t y_ld, int32_t y_type, void* hip_stream) {
+    TRY(check_groups(groups));
+    TRY(check_layer(layer, true));
+    TRY(check_act(act));
+    if (groups->n == 0) return PNN_OK;
+    TRY(check_rows("x_dev", x_dev, x_ld, layer->inputs, layer->type));
+    TRY(check_rows("y_dev", y_dev, y_ld, layer->outputs, y_type));
+    hipStream_t s = (hipStream_t)hip_stream;
+    OnDeviceOf dev(s);
+    const bool few = few_pairs(groups);
+    GroupGemm a = group_base(groups, few);
+    a.M = layer->outputs; a.Kx = layer->inputs;
+    a.p = x_dev; a.ldp = x_ld; a.pdiv = groups->per_row;
+    a.w = layer->w_dev; a.wnet = layer->w_net; a.ldw = layer->w_ld;
+    a.b = layer->b_dev; a.bnet = layer->b_net;
+    a.act = act;
+    a.y = y_dev; a.ldy = y_ld;
+    a.vec = store4_ok(y_dev, y_ld, 0, y_type);
+    return run_group_pairs<GR_FWD>(a, layer->type, y_type, few, s);
+}
+
+pnn_status pnn_grouped_workspace(const pnn_groups* groups, const pnn_group_layer* layer, int64_t* input_bytes,
+                                 int64_t* weights_bytes) {
+    if (!groups) return fail(nullptr, PNN_EINVAL, "groups is NULL");
+    TRY(check_groups(groups->n, groups->per_row, groups->networks));
+    TRY(check_layer(layer, false));
+    if (input_bytes) *input_bytes = group_input_ws(groups, layer->inputs);
+    if (weights_bytes) *weights_bytes = group_weights_ws(groups, layer->inputs, layer->outputs);
+    return PNN_OK;
+}
+
+pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_layer* layer, const void* dy_dev, int64_t dy_ld,
+                                      const void* a_dev, int64_t a_ld, int32_t act, void* dx_dev, int64_t dx_ld,
+                                      int32_t dx_type, void* ws_dev, int64_t ws_bytes, void* hip_stream) {
+    TRY(check_groups(groups));
+    TRY(check_layer(layer, true));
+    TRY(check_act(act));
+    if (groups->n == 0) return PNN_OK;
+    TRY(check_rows("dy_dev", dy_dev, dy_ld, layer->outputs, layer->type));
+    TRY(check_rows("dx_dev", dx_dev, dx_ld, layer->inputs, dx_type));
+    if (act >= 0) TRY(check_rows("a_dev", a_dev, a_ld, layer->inputs, layer->type));
+    TRY(check_ws(ws_dev, ws_bytes, group_input_ws(groups, layer->inputs)));
+    hipStream_t s = (hipStream_t)hip_stream;
+    OnDeviceOf dev(s);
+    const bool few = few_pairs(groups), sum = groups->per_row > 1;
+    GroupGemm a = group_base(groups, few);
+    a.M = layer->inputs; a.Kx = layer->outputs;
+    a.p = dy_dev; a.ldp = dy_ld;
+    a.w = layer->w_dev; a.wnet = layer->w_net; a.ldw = layer->w_ld;
+    if (!sum) {
+        a.a = act >= 0 ? a_dev : nullptr; a.lda = a_ld; a.act = act;
+        a.y = dx_dev; a.ldy = dx_ld;
+        a.vec = store4_ok(dx_dev, dx_ld, 0, dx_type);
+        return run_group_pairs<GR_DX>(a, layer->type, dx_type, few, s);
+    }
+    a.y = ws_dev; a.ldy = layer->inputs;
+    a.vec = store4_ok(ws_dev, layer->inputs, 0, PNN_FP32);
+    TRY(run_group_pairs<GR_DX>(a, layer->type, PNN_FP32, few, s));
+    const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * layer->inputs + 255) / 256, 8192);
+    const float* part = (const float*)ws_dev;
+    const void* ad = act >= 0 ? a_dev : nullptr;
+#define PNN_SUM_PAIRS(T, TO) \
+    group_sum_pairs_kernel<T, TO><<<blocks, 256, 0, s>>>(part, groups->n, groups->per_row, layer->inputs, (const T*)ad, a_ld, act, (TO*)dx_dev, dx_ld)
+    if (layer->type == PNN_FP32) { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(float, float); else PNN_SUM_PAIRS(float, bf16_t); }
+    else { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(bf16_t, float); else PNN_SUM_PAIRS(bf16_t, bf16_t); }
+#undef PNN_SUM_PAIRS
+    return launched("sum over the pairs of a row");
+}
+
+pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_group_layer* layer, const void* dy_dev,
+                                        int64_t dy_ld, const void* x_dev, int64_t x_ld, float* dw_dev, int64_t dw_net,
+                                        int64_t dw_ld, float* db_dev, int64_t db_net, void* ws_dev, int64_t ws_bytes,
+                                        void* hip_stream) {
+    TRY(check_groups(groups));
+    TRY(check_layer(layer, false));
+    if (!groups->plan_dev) return fail(nullptr, PNN_EINVAL, "plan_dev is NULL");  // (no rows still give zeros)
+    if (groups->n > 0) {
+        TRY(check_rows("dy_dev", dy_dev, dy_ld, layer->outputs, layer->type));
+        TRY(check_rows("x_dev", x_dev, x_ld, layer->inputs, layer->type));
+    }
+    TRY(check_rows("dw_dev", dw_dev, dw_ld, layer->inputs, PNN_FP32));
+    if (((uintptr_t)db_dev & 3) != 0) return fail(nullptr, PNN_EINVAL, "db_dev is not aligned to its type");
+    if (dw_net < (layer->outputs - 1) * dw_ld + layer->inputs && groups->networks > 1)
+        return fail(nullptr, PNN_EINVAL, "the networks of dw_dev overlap");
+    if (db_dev && db_net < layer->outputs && groups->networks > 1) return fail(nullptr, PNN_EINVAL, "the networks of db_dev overlap");
+    TRY(check_ws(ws_dev, ws_bytes, group_weights_ws(groups, layer->inputs, layer->outputs)));
+    hipStream_t s = (hipStream_t)hip_stream;
+    OnDeviceOf dev(s);
+    return run_group_weights(groups, layer->inputs, layer->outputs, layer->type, dy_dev, dy_ld, x_dev, x_ld, groups->per_row, dw_dev,
+                             dw_net, dw_ld, db_dev, db_net, 0.0f, nullptr, ws_dev, s);
+}
+
+}  // extern "C"

@@ -34,6 +34,7 @@
 
 #include "../../include/pnn.h"
 #include "kernels.hpp"
+#include "groups.hpp"
 
 using namespace pnn;
 
@@ -1791,3 +1792,5 @@ void pnn_destroy(pnn_net* n) {
 }
 
 }  // extern "C"
+
+#include "groups_host.hpp"

@@ -36,6 +36,17 @@ class PnnConfig(ctypes.Structure):
     ]
 
 
+class PnnGroups(ctypes.Structure):
+    _fields_ = [("plan", ctypes.c_void_p), ("n", ctypes.c_int64), ("per_row", ctypes.c_int32),
+                ("networks", ctypes.c_int32)]
+
+
+class PnnGroupLayer(ctypes.Structure):
+    _fields_ = [("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("w", ctypes.c_void_p), ("w_net", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("b", ctypes.c_void_p),
+                ("b_net", ctypes.c_int64)]
+
+
 class PnnError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -92,6 +103,16 @@ def lib() -> ctypes.CDLL:
         L.pnn_profile_read.restype = i32
         L.pnn_destroy.argtypes = [vp]
         L.pnn_destroy.restype = None
+        groups, layer = P(PnnGroups), P(PnnGroupLayer)
+        L.pnn_group_bytes.argtypes = [i64, i32, i32, P(i64)]
+        L.pnn_group_rows.argtypes = [vp, i64, i32, i32, vp, i64, vp]
+        L.pnn_grouped_forward.argtypes = [groups, layer, vp, i64, i32, vp, i64, i32, vp]
+        L.pnn_grouped_workspace.argtypes = [groups, layer, P(i64), P(i64)]
+        L.pnn_grouped_backward_input.argtypes = [groups, layer, vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp]
+        L.pnn_grouped_backward_weights.argtypes = [groups, layer, vp, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
+        for name in ("pnn_group_bytes", "pnn_group_rows", "pnn_grouped_forward", "pnn_grouped_workspace",
+                     "pnn_grouped_backward_input", "pnn_grouped_backward_weights"):
+            getattr(L, name).restype = i32
         _lib = L
     return _lib
 
@@ -256,3 +277,186 @@ class PNN:
             self.close()
         except Exception:
             pass
+
+
+# ---- rows that name their network, without a handle (group_rows and the grouped products) ----
+
+def _call(fn, what: str, *args) -> None:
+    st = fn(*args)
+    if st != PNN_OK:
+        raise PnnError(st, f"{what}: {lib().pnn_last_error(None).decode()}")
+
+
+class _On:
+    """The device of a call's tensors made current, with the call's stream current for allocations."""
+
+    def __init__(self, tensors, stream):
+        import torch
+        given = [t for t in tensors if t is not None]
+        for t in given:
+            if not t.is_cuda:
+                raise ValueError(f"expected CUDA tensors, got one on {t.device}")
+            if t.device != given[0].device:
+                raise ValueError(f"tensors on {given[0].device} and on {t.device}")
+        self.device = given[0].device
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        if stream is not None and stream.device != self.device:
+            raise ValueError(f"a stream of {stream.device} for tensors on {self.device}")
+        self._given = stream
+        self._contexts = []
+
+    def __enter__(self):
+        import torch
+        if torch.cuda.current_device() != self.device.index:
+            self._contexts.append(torch.cuda.device(self.device))
+        if self._given is not None:
+            self._contexts.append(torch.cuda.stream(self._given))
+        for c in self._contexts:
+            c.__enter__()
+        self.stream = torch.cuda.current_stream().cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        for c in reversed(self._contexts):
+            c.__exit__(*exc)
+
+
+def _type_of(t) -> int:
+    code = {"torch.float32": FP32, "torch.bfloat16": BF16_MIXED}.get(str(t.dtype))
+    if code is None:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _rows(t, name: str, shape, dtype=None):
+    """(pointer, distance between rows) of a matrix whose rows' values are contiguous."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the values of a row of {name} are not contiguous")
+    ld = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+    return t.data_ptr(), ld
+
+
+def _values(t, name: str, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, expected {tuple(shape)} of {dtype}, contiguous")
+    return t.data_ptr()
+
+
+class RowGroups:
+    """Rows grouped by the networks that they name (pnn_group_rows)."""
+
+    def __init__(self, plan, n: int, per_row: int, networks: int):
+        self.plan, self.n, self.per_row, self.networks = plan, n, per_row, networks
+        self.struct = PnnGroups(plan.data_ptr(), n, per_row, networks)
+
+    @property
+    def offsets(self):
+        """[networks + 1] int32: network e's pairs are positions offsets[e] to offsets[e + 1]."""
+        return self.plan[:self.networks + 1]
+
+    @property
+    def pairs(self):
+        """[n * per_row] int32 pair numbers by network, the dropped ones last."""
+        first = -(-(self.networks + 1) // 4) * 4
+        return self.plan[first:first + self.n * self.per_row]
+
+
+def group_rows(ids, networks: int, stream=None) -> RowGroups:
+    """Group rows by network: ids int32 [n] or [n, per_row], an id outside [0, networks) drops the pair."""
+    import torch
+    if str(ids.dtype) != "torch.int32" or ids.dim() not in (1, 2) or not ids.is_contiguous():
+        raise ValueError(f"ids: expected contiguous int32 [n] or [n, per_row], got {tuple(ids.shape)} of {ids.dtype}")
+    n, per_row = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
+    with _On([ids], stream) as on:
+        size = ctypes.c_int64()
+        _call(lib().pnn_group_bytes, "pnn_group_bytes", n, per_row, networks, ctypes.byref(size))
+        plan = torch.empty(size.value // 4, dtype=torch.int32, device=on.device)
+        _call(lib().pnn_group_rows, "pnn_group_rows", ids.data_ptr(), n, per_row, networks, plan.data_ptr(), size.value,
+              on.stream)
+    return RowGroups(plan, n, per_row, networks)
+
+
+def _weights(groups: RowGroups, w, b=None) -> PnnGroupLayer:
+    import torch
+    if w.dim() != 3 or w.shape[0] != groups.networks:
+        raise ValueError(f"w has shape {tuple(w.shape)}, expected ({groups.networks}, outputs, inputs)")
+    ptr, ld = _rows(w, "w", w.shape)
+    layer = PnnGroupLayer(w.shape[2], w.shape[1], _type_of(w), ptr, w.stride(0), ld, None, 0)
+    if b is not None:
+        layer.b, layer.b_net = _rows(b, "b", w.shape[:2], torch.float32)
+    return layer
+
+
+def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, out=None, out_dtype=None, stream=None):
+    """y[p] = act(w[e] x[p // per_row] + b[e]) for every pair p of network e; dropped pairs give 0.
+    x [n, inputs], w [networks, outputs, inputs] of x's type (float32 or bfloat16), b fp32."""
+    import torch
+    layer = _weights(groups, w, b)
+    with _On([groups.plan, x, w, b, out], stream) as on:
+        px, ldx = _rows(x, "x", (groups.n, layer.inputs), w.dtype)
+        shape = (groups.n * groups.per_row, layer.outputs)
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype or x.dtype, device=on.device)
+        py, ldy = _rows(out, "out", shape, out_dtype)
+        _call(lib().pnn_grouped_forward, "pnn_grouped_forward", ctypes.byref(groups.struct), ctypes.byref(layer), px, ldx,
+              -1 if act is None else act, py, ldy, _type_of(out), on.stream)
+    return out
+
+
+def _workspace(groups, layer, on, which: int):
+    import torch
+    size = (ctypes.c_int64(), ctypes.c_int64())
+    _call(lib().pnn_grouped_workspace, "pnn_grouped_workspace", ctypes.byref(groups.struct), ctypes.byref(layer),
+          ctypes.byref(size[0]), ctypes.byref(size[1]))
+    if size[which].value == 0:
+        return None, None, 0
+    ws = torch.empty(size[which].value, dtype=torch.uint8, device=on.device)
+    return ws, ws.data_ptr(), size[which].value
+
+
+def grouped_backward_input(groups: RowGroups, dy, w, a=None, act: Optional[int] = None, out=None, out_dtype=None,
+                           stream=None):
+    """dx[r] = (sum over row r's pairs of w[e]^T dy[pair]) * act'(a[r]) (the slope from stored activations)."""
+    import torch
+    layer = _weights(groups, w)
+    with _On([groups.plan, dy, w, a, out], stream) as on:
+        pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), w.dtype)
+        shape = (groups.n, layer.inputs)
+        if (a is None) != (act is None):
+            raise ValueError("a and act go together")
+        pa, lda = _rows(a, "a", shape, w.dtype) if a is not None else (None, 0)
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype or dy.dtype, device=on.device)
+        po, ldo = _rows(out, "out", shape, out_dtype)
+        ws, pw, size = _workspace(groups, layer, on, 0)
+        _call(lib().pnn_grouped_backward_input, "pnn_grouped_backward_input", ctypes.byref(groups.struct),
+              ctypes.byref(layer), pd, ldd, pa, lda, -1 if act is None else act, po, ldo, _type_of(out), pw, size, on.stream)
+    return out
+
+
+def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: bool = True, stream=None):
+    """(dw, db): dw[e] = sum over network e's pairs of dy[p] x[p // per_row]^T and db[e] = sum of dy[p], fp32;
+    zeros for a network without pairs; bias=False leaves db out (None)."""
+    import torch
+    if dy.dim() != 2 or x.dim() != 2:
+        raise ValueError("dy and x are matrices")
+    layer = PnnGroupLayer(x.shape[1], dy.shape[1], _type_of(x), None, 0, 0, None, 0)
+    with _On([groups.plan, dy, x, dw, db], stream) as on:
+        pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), x.dtype)
+        px, ldx = _rows(x, "x", (groups.n, layer.inputs))
+        f32 = torch.float32
+        if dw is None:
+            dw = torch.empty((groups.networks, layer.outputs, layer.inputs), dtype=f32, device=on.device)
+        if db is None and bias:
+            db = torch.empty((groups.networks, layer.outputs), dtype=f32, device=on.device)
+        pw, ldw = _rows(dw, "dw", (groups.networks, layer.outputs, layer.inputs), f32)
+        pb, netb = _rows(db, "db", (groups.networks, layer.outputs), f32) if db is not None else (None, 0)
+        ws, ps, size = _workspace(groups, layer, on, 1)
+        _call(lib().pnn_grouped_backward_weights, "pnn_grouped_backward_weights", ctypes.byref(groups.struct),
+              ctypes.byref(layer), pd, ldd, px, ldx, pw, dw.stride(0), ldw, pb, netb, ps, size, on.stream)
+    return dw, db

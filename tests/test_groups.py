@@ -1,0 +1,386 @@
+"""Rows that name their network: the grouping, and the grouped products with both gradients,
+against the formulas in 64 bits."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2304_09590_amd import pnn
+
+gpu = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+# ---- refusals, on the host: the pointers are never read -----------------------------------------
+
+FAKE = 1 << 20
+
+
+def groups_of(n=4, per_row=1, networks=3, plan=FAKE):
+    return pnn.PnnGroups(plan, n, per_row, networks)
+
+
+def layer_of(inputs=8, outputs=5, kind=pnn.FP32, w=FAKE, w_net=40, w_ld=8, b=None, b_net=0):
+    return pnn.PnnGroupLayer(inputs, outputs, kind, w, w_net, w_ld, b, b_net)
+
+
+def forward(g=None, layer=None, x=FAKE, x_ld=8, act=-1, y=FAKE, y_ld=5, kind=pnn.FP32):
+    g, layer = g or groups_of(), layer or layer_of()
+    return pnn.lib().pnn_grouped_forward(ctypes.byref(g), ctypes.byref(layer), x, x_ld, act, y, y_ld, kind, None)
+
+
+def backward_input(g=None, layer=None, dy=FAKE, dy_ld=5, a=None, a_ld=0, act=-1, dx=FAKE, dx_ld=8, kind=pnn.FP32, ws=None,
+                   size=0):
+    g, layer = g or groups_of(), layer or layer_of()
+    return pnn.lib().pnn_grouped_backward_input(ctypes.byref(g), ctypes.byref(layer), dy, dy_ld, a, a_ld, act, dx, dx_ld,
+                                                kind, ws, size, None)
+
+
+def backward_weights(g=None, layer=None, dy=FAKE, dy_ld=5, x=FAKE, x_ld=8, dw=FAKE, dw_net=40, dw_ld=8, db=FAKE, db_net=5,
+                     ws=None, size=0):
+    g, layer = g or groups_of(), layer or layer_of(w=None)
+    return pnn.lib().pnn_grouped_backward_weights(ctypes.byref(g), ctypes.byref(layer), dy, dy_ld, x, x_ld, dw, dw_net,
+                                                  dw_ld, db, db_net, ws, size, None)
+
+
+@pytest.mark.parametrize("n,per_row,networks,status", [
+    (-1, 1, 4, pnn.PNN_ESHAPE), (4, 0, 4, pnn.PNN_EINVAL), (4, -2, 4, pnn.PNN_EINVAL), (4, 1, 0, pnn.PNN_EINVAL),
+    (4, 1, 1025, pnn.PNN_EINVAL), ((1 << 30) + 1, 1, 4, pnn.PNN_ESHAPE), (1 << 29, 3, 4, pnn.PNN_ESHAPE),
+    ((1 << 62), 1 << 30, 4, pnn.PNN_ESHAPE)])
+def test_sizes_are_refused(n, per_row, networks, status):
+    size = ctypes.c_int64(-7)
+    assert pnn.lib().pnn_group_bytes(n, per_row, networks, ctypes.byref(size)) == status
+    assert size.value == -7
+    assert pnn.lib().pnn_group_rows(FAKE, n, per_row, networks, FAKE, 1 << 40, None) == status
+    assert forward(g=groups_of(n, per_row, networks)) == status
+    assert pnn.lib().pnn_last_error(None)
+
+
+def test_grouping_refuses_missing_or_small_memory():
+    L, size = pnn.lib(), ctypes.c_int64()
+    assert L.pnn_group_bytes(100, 2, 7, ctypes.byref(size)) == pnn.PNN_OK and size.value >= 4 * 208
+    assert L.pnn_group_bytes(100, 2, 7, None) == pnn.PNN_EINVAL
+    assert L.pnn_group_rows(None, 100, 2, 7, FAKE, size, None) == pnn.PNN_EINVAL
+    assert L.pnn_group_rows(FAKE, 100, 2, 7, None, size, None) == pnn.PNN_EINVAL
+    assert L.pnn_group_rows(FAKE, 100, 2, 7, FAKE + 4, size, None) == pnn.PNN_EINVAL
+    assert L.pnn_group_rows(FAKE + 2, 100, 2, 7, FAKE, size, None) == pnn.PNN_EINVAL
+    assert L.pnn_group_rows(FAKE, 100, 2, 7, FAKE, size.value - 4, None) == pnn.PNN_ESHAPE
+
+
+@pytest.mark.parametrize("call", [
+    lambda: forward(layer=layer_of(inputs=0)), lambda: forward(layer=layer_of(outputs=(1 << 20) + 1)),
+    lambda: forward(layer=layer_of(kind=2)), lambda: forward(kind=-1), lambda: forward(act=pnn.SOFTMAX),
+    lambda: forward(act=-2), lambda: forward(layer=layer_of(w=None)), lambda: forward(layer=layer_of(w=FAKE + 2)),
+    lambda: forward(layer=layer_of(w_ld=7)), lambda: forward(layer=layer_of(w_net=-1)),
+    lambda: forward(layer=layer_of(b=FAKE + 1)), lambda: forward(x=None), lambda: forward(x=FAKE + 1),
+    lambda: forward(x_ld=7), lambda: forward(y=None), lambda: forward(y_ld=4), lambda: forward(g=groups_of(plan=None)),
+    lambda: forward(g=groups_of(plan=FAKE + 8)),
+    lambda: backward_input(dy=None), lambda: backward_input(dy_ld=4), lambda: backward_input(dx=None),
+    lambda: backward_input(act=pnn.RELU), lambda: backward_input(act=pnn.RELU, a=FAKE, a_ld=7),
+    lambda: backward_input(kind=9),
+    lambda: backward_weights(dy=None), lambda: backward_weights(x=None), lambda: backward_weights(dw=None),
+    lambda: backward_weights(dw=FAKE + 2), lambda: backward_weights(dw_ld=7), lambda: backward_weights(dw_net=39),
+    lambda: backward_weights(db_net=4), lambda: backward_weights(db=FAKE + 2),
+    lambda: backward_weights(g=groups_of(n=0, plan=None))])
+def test_arguments_are_refused(call):
+    assert call() == pnn.PNN_EINVAL
+    assert pnn.lib().pnn_last_error(None)
+
+
+def test_missing_workspaces_are_refused():
+    L, one, two = pnn.lib(), ctypes.c_int64(), ctypes.c_int64()
+    g = groups_of(n=5000, per_row=2, networks=1)
+    assert L.pnn_grouped_workspace(ctypes.byref(g), ctypes.byref(layer_of()), ctypes.byref(one), ctypes.byref(two)) == pnn.PNN_OK
+    assert one.value == 5000 * 2 * 8 * 4 and two.value > 0
+    assert L.pnn_grouped_workspace(ctypes.byref(g), ctypes.byref(layer_of()), None, None) == pnn.PNN_OK
+    assert L.pnn_grouped_workspace(None, ctypes.byref(layer_of()), None, None) == pnn.PNN_EINVAL
+    assert backward_input(g=g) == pnn.PNN_ESHAPE
+    assert backward_input(g=g, ws=FAKE, size=one.value - 1) == pnn.PNN_ESHAPE
+    assert backward_input(g=g, ws=FAKE + 4, size=one.value) == pnn.PNN_EINVAL
+    assert backward_weights(g=g) == pnn.PNN_ESHAPE
+    assert backward_weights(g=g, ws=FAKE, size=two.value - 1) == pnn.PNN_ESHAPE
+
+
+def test_no_rows_need_no_device():
+    assert forward(g=groups_of(n=0, plan=None), x=None, y=None) == pnn.PNN_OK
+    assert backward_input(g=groups_of(n=0, plan=None), dy=None, dx=None) == pnn.PNN_OK
+
+
+def test_the_binding_refuses_what_it_cannot_pass():
+    with pytest.raises(ValueError):
+        pnn.group_rows(torch.zeros(4, dtype=torch.int64), 2)
+    with pytest.raises(ValueError):
+        pnn.group_rows(torch.zeros(4, dtype=torch.int32), 2)  # host memory
+    with pytest.raises(ValueError):
+        pnn.group_rows(torch.zeros(4, 4, dtype=torch.int32)[:, ::2], 2)
+
+
+# ---- grouping ------------------------------------------------------------------------------------
+
+def ids_of(n, per_row, networks, seed, kind="mixed"):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "one":  # every pair goes through the last network
+        return torch.full((n, per_row), networks - 1, dtype=torch.int32)
+    if kind == "none":
+        return torch.full((n, per_row), -1, dtype=torch.int32)
+    ids = torch.randint(0, networks, (n, per_row), generator=g, dtype=torch.int32)
+    if kind == "few":  # most networks have no pair
+        ids = ids // max(1, networks // 3) * max(1, networks // 3)
+    drop = torch.rand(n, per_row, generator=g) < 0.1
+    ids[drop] = torch.tensor([-1, networks, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)[
+        torch.randint(0, 4, (int(drop.sum()),), generator=g)]
+    return ids
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["mixed", "one", "none", "few"])
+@pytest.mark.parametrize("n,per_row,networks", [
+    (0, 1, 3), (1, 1, 1), (1, 3, 2), (5, 1, 1024), (64, 2, 16), (63, 1, 65), (1365, 3, 31), (4096, 1, 256), (4097, 1, 256),
+    (20011, 2, 1024), (60000, 2, 256), (300000, 4, 5)])
+def test_grouping(n, per_row, networks, kind):
+    ids = ids_of(n, per_row, networks, 1, kind)
+    for got in (pnn.group_rows(ids.cuda(), networks) for _ in range(2)):
+        flat = ids.reshape(-1).long()
+        key = torch.where((flat < 0) | (flat >= networks), networks, flat)
+        want, order = torch.sort(key, stable=True)
+        counts = torch.bincount(want, minlength=networks + 1)
+        assert torch.equal(got.pairs.cpu().long(), order)
+        assert torch.equal(got.offsets.cpu().long(), counts.cumsum(0) - counts)
+
+
+# ---- products ------------------------------------------------------------------------------------
+
+ACTS = {None: lambda z: z, pnn.SIGMOID: torch.sigmoid, pnn.TANH: torch.tanh, pnn.RELU: lambda z: z.clamp(min=0),
+        pnn.LEAKY_RELU: lambda z: torch.where(z < 0, 0.01 * z, z)}
+
+
+def slope(act, a):
+    neg = torch.signbit(a)
+    return {None: torch.ones_like(a), pnn.SIGMOID: a * (1 - a), pnn.TANH: 1 - a * a,
+            pnn.RELU: torch.where(neg, 0.0, 1.0).to(a.dtype), pnn.LEAKY_RELU: torch.where(neg, 0.01, 1.0).to(a.dtype)}[act]
+
+
+def steps(k):
+    """Roundings of a sum of k products, in units of one step of fp32: the fp32 operands' six partial products are
+    added 32 terms at a time (two steps each, were the sum cut instead of rounded), and inside an instruction and in
+    the sums of waves and parts a few more.  The parts left out of a product are below one step of it."""
+    return 2.0 * (6 * math.ceil(k / 32) + 24)
+
+
+def check(got, want, size, k, act=None, what=""):
+    """size: the sum of the products' magnitudes; the activations' slopes are at most 1, their own errors 4 steps."""
+    got, want, size = got.double().cpu(), want.cpu(), size.cpu()
+    tol = steps(k) * 2.0 ** -24 * (size + 1e-30)
+    if act is not None:
+        tol = tol + 4 * 2.0 ** -24 * (1 + want.abs())
+    return got, want, tol
+
+
+def close(got, want, size, k, act=None):
+    dtype = got.dtype
+    got, want, tol = check(got, want, size, k, act)
+    if dtype == BF16:
+        tol = tol + (want.abs() + tol) * torch.finfo(BF16).eps / 2
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}, largest {((got - want).abs() / tol).max():.3g} of the tolerance"
+
+
+class Case:
+    """Operands (padded rows where `pad`: strides beyond the widths and rows off 16 bytes) and values in 64 bits."""
+
+    def __init__(self, n, per_row, networks, inputs, outputs, dtype, kind="mixed", pad=0, seed=3):
+        g = torch.Generator().manual_seed(seed)
+        self.ids = ids_of(n, per_row, networks, seed, kind)
+        self.n, self.per_row, self.networks, self.i, self.o = n, per_row, networks, inputs, outputs
+
+        def make(*shape):
+            t = torch.randn(*shape[:-1], shape[-1] + pad, generator=g).to(dtype).cuda()
+            return t[..., pad:]
+
+        self.x, self.w, self.dy = make(n, inputs), make(networks, outputs, inputs), make(n * per_row, outputs)
+        self.b = torch.randn(networks, outputs + pad, generator=g).cuda()[:, pad:]
+        self.groups = pnn.group_rows(self.ids.cuda(), networks)
+        flat = self.ids.reshape(-1)
+        self.kept = ((flat >= 0) & (flat < networks)).cuda()
+        self.members = [torch.nonzero(flat == e)[:, 0].cuda() for e in range(networks)]
+
+    def forward(self, act, bias):
+        z = torch.zeros(self.n * self.per_row, self.o, dtype=torch.float64, device="cuda")
+        size = z.clone()
+        for e, m in enumerate(self.members):
+            x, w, b = self.x[m // self.per_row].double(), self.w[e].double(), self.b[e].double() * bias
+            z[m] = ACTS[act](x @ w.T + b)
+            size[m] = x.abs() @ w.abs().T + b.abs()
+        return z, size
+
+    def backward_input(self):
+        dx = torch.zeros(self.n * self.per_row, self.i, dtype=torch.float64, device="cuda")
+        size = dx.clone()
+        for e, m in enumerate(self.members):
+            dx[m], size[m] = self.dy[m].double() @ self.w[e].double(), self.dy[m].double().abs() @ self.w[e].double().abs()
+        return dx.view(self.n, self.per_row, self.i).sum(1), size.view(self.n, self.per_row, self.i).sum(1)
+
+    def backward_weights(self):
+        out = []
+        for m in self.members:
+            d, x = self.dy[m].double(), self.x[m // self.per_row].double()
+            out.append((d.T @ x, d.abs().T @ x.abs(), d.sum(0), d.abs().sum(0)))
+        return [torch.stack(t) for t in zip(*out)]
+
+
+SHAPES = [  # n, per_row, networks, inputs, outputs, kind, pad
+    (1, 1, 1, 1, 1, "mixed", 0), (1, 2, 64, 784, 512, "mixed", 0), (3, 1, 2, 7, 5, "mixed", 0), (17, 1, 1, 33, 31, "mixed", 3),
+    (50, 2, 7, 100, 131, "mixed", 1), (40, 1, 3, 8, 8, "none", 0), (24, 1, 1, 784, 16, "one", 0), (25, 1, 1, 784, 16, "one", 0),
+    (300, 1, 5, 64, 128, "mixed", 0), (129, 3, 3, 129, 127, "mixed", 0), (1000, 1, 4, 200, 104, "few", 0),
+    (257, 1, 1, 65, 257, "one", 2), (2000, 2, 3, 96, 40, "mixed", 8), (3000, 1, 2, 20, 12, "mixed", 0)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,per_row,networks,inputs,outputs,kind,pad", SHAPES)
+def test_forward(n, per_row, networks, inputs, outputs, kind, pad, dtype):
+    c = Case(n, per_row, networks, inputs, outputs, dtype, kind, pad)
+    for act, bias, out_dtype in ((None, 0.0, None), (pnn.SIGMOID, 1.0, F32), (pnn.RELU, 1.0, None), (pnn.TANH, 1.0, BF16),
+                                 (pnn.LEAKY_RELU, 1.0, None)):
+        got = pnn.grouped_forward(c.groups, c.x, c.w, c.b if bias else None, act=act, out_dtype=out_dtype)
+        assert got.dtype == (out_dtype or dtype)
+        want, size = c.forward(act, bias)
+        close(got, want, size, inputs, act)
+        assert (got[~c.kept] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,per_row,networks,inputs,outputs,kind,pad", SHAPES)
+def test_backward_input(n, per_row, networks, inputs, outputs, kind, pad, dtype):
+    c = Case(n, per_row, networks, inputs, outputs, dtype, kind, pad)
+    want, size = c.backward_input()
+    for out_dtype in (F32, BF16):
+        close(pnn.grouped_backward_input(c.groups, c.dy, c.w, out_dtype=out_dtype), want, size, outputs * per_row)
+    for act in (pnn.SIGMOID, pnn.TANH, pnn.RELU, pnn.LEAKY_RELU):
+        a = ACTS[act](c.x.double())
+        a = torch.where(c.x < 0, -a.abs(), a).to(dtype) if act in (pnn.RELU, pnn.LEAKY_RELU) else a.to(dtype)
+        s = slope(act, a.double())
+        # (the slope is rounded once or twice, and the product)
+        close(pnn.grouped_backward_input(c.groups, c.dy, c.w, a=a, act=act), want * s, size * (s.abs() + 2.0 ** -23), outputs * per_row + 64)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,per_row,networks,inputs,outputs,kind,pad", SHAPES + [(0, 1, 3, 9, 4, "mixed", 0)])
+def test_backward_weights(n, per_row, networks, inputs, outputs, kind, pad, dtype):
+    c = Case(n, per_row, networks, inputs, outputs, dtype, kind, pad)
+    dw, db = pnn.grouped_backward_weights(c.groups, c.dy, c.x)
+    want, size, bwant, bsize = c.backward_weights()
+    close(dw, want, size, n * per_row)
+    close(db, bwant, bsize, n * per_row)
+    again, none = pnn.grouped_backward_weights(c.groups, c.dy, c.x, bias=False)
+    assert none is None and torch.equal(again, dw)
+
+
+@gpu
+@pytest.mark.parametrize("few", [True, False])
+def test_results_stay_inside_their_rows(few):
+    """Outputs with wider strides: what lies between rows and networks, and behind the last, is left as it was."""
+    c = Case(30 if few else 400, 1, 4, 44, 52, F32)
+    for width, call in ((52, lambda out: pnn.grouped_forward(c.groups, c.x, c.w, out=out)),
+                        (44, lambda out: pnn.grouped_backward_input(c.groups, c.dy, c.w, out=out))):
+        whole = torch.full((c.n + 2, width + 5), 7.0, device="cuda")
+        call(whole[1:-1, 2:-3])
+        plain = torch.full_like(whole, 7.0)
+        plain[1:-1, 2:-3] = call(None)
+        assert torch.equal(whole, plain)
+    whole = torch.full((6, 54, 48), 7.0, device="cuda")
+    bwhole = torch.full((6, 54), 7.0, device="cuda")
+    pnn.grouped_backward_weights(c.groups, c.dy, c.x, dw=whole[1:5, 1:53, 3:47], db=bwhole[1:5, 1:53])
+    dw, db = pnn.grouped_backward_weights(c.groups, c.dy, c.x)
+    plain, bplain = torch.full_like(whole, 7.0), torch.full_like(bwhole, 7.0)
+    plain[1:5, 1:53, 3:47], bplain[1:5, 1:53] = dw, db
+    assert torch.equal(whole, plain) and torch.equal(bwhole, bplain)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [30, 400])
+def test_rows_without_a_network_are_not_read(n, dtype):
+    """NaN in the rows of dropped pairs, and in networks that no pair names, reaches nothing."""
+    c = Case(n, 1, 6, 40, 24, dtype, kind="few")
+    x, w, dy = c.x.clone(), c.w.clone(), c.dy.clone()
+    x[~c.kept], dy[~c.kept] = math.nan, math.nan
+    unused = [e for e, m in enumerate(c.members) if m.numel() == 0]
+    assert unused
+    w[unused] = math.nan
+    assert torch.equal(pnn.grouped_forward(c.groups, x, w), pnn.grouped_forward(c.groups, c.x, c.w))
+    assert torch.equal(pnn.grouped_backward_input(c.groups, dy, w), pnn.grouped_backward_input(c.groups, c.dy, c.w))
+    for got, want in zip(pnn.grouped_backward_weights(c.groups, dy, x), pnn.grouped_backward_weights(c.groups, c.dy, c.x)):
+        assert torch.equal(got, want)
+
+
+@gpu
+@pytest.mark.parametrize("n", [30, 400])
+def test_a_nan_stays_in_its_row(n):
+    c = Case(n, 1, 3, 40, 24, BF16)
+    row = int(torch.nonzero(c.kept)[0])
+    x = c.x.clone()
+    x[row, 5] = math.nan
+    for act in (None, pnn.RELU, pnn.SIGMOID):
+        bad = pnn.grouped_forward(c.groups, x, c.w, act=act)
+        good = pnn.grouped_forward(c.groups, c.x, c.w, act=act)
+        assert torch.isnan(bad[row]).all()
+        good[row] = 0
+        bad[row] = 0
+        assert torch.equal(bad, good)
+
+
+@gpu
+def test_rows_behind_32_bits():
+    """The last rows of a matrix of more than 2^31 values, and one network's weights that far away."""
+    rows, width = (1 << 25) + 3, 72
+    x = torch.zeros(rows, width, dtype=BF16, device="cuda")
+    x[-1] = 1
+    ids = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    ids[-1], ids[5] = 1, 0
+    groups = pnn.group_rows(ids, 2)
+    w = torch.ones(2, 8, width, dtype=BF16, device="cuda")
+    w[1] *= 2
+    y = pnn.grouped_forward(groups, x, w)
+    assert (y[-1] == 2 * width).all() and (y[:-1] == 0).all()
+    dw, db = pnn.grouped_backward_weights(groups, y, x)
+    assert (dw[1] == 2 * width).all() and (dw[0] == 0).all() and (db[1] == 2 * width).all()
+    far = torch.empty((1 << 31) + 8 * width, dtype=BF16, device="cuda").as_strided((2, 8, width), (1 << 31, width, 1))
+    far.copy_(w)
+    ids = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    y = pnn.grouped_forward(pnn.group_rows(ids, 2), torch.ones(2, width, dtype=BF16, device="cuda"), far)
+    assert (y[0] == width).all() and (y[1] == 2 * width).all()
+
+
+@gpu
+@pytest.mark.parametrize("n", [20, 700])
+def test_another_stream_and_a_graph(n):
+    """A step recorded into a graph, replayed with new contents between the program's own work."""
+    c = Case(n, 2, 3, 48, 56, BF16)
+    ids = c.ids.cuda()
+
+    def step():
+        g = pnn.group_rows(ids, 3)
+        y = pnn.grouped_forward(g, c.x, c.w, c.b, act=pnn.RELU)
+        return (y, pnn.grouped_backward_input(g, y, c.w), *pnn.grouped_backward_weights(g, y, c.x))
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = pnn.group_rows(ids, 3, stream=side)
+    got = pnn.grouped_forward(g, c.x, c.w, c.b, act=pnn.RELU, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for r in range(4):
+        ids.copy_(ids_of(n, 2, 3, 50 + r).cuda())
+        c.x.mul_(-0.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(kept, step()):
+            assert torch.equal(a, b)
