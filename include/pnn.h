@@ -316,6 +316,45 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
                                         int64_t dw_ld, float* db_dev, int64_t db_net, void* ws_dev, int64_t ws_bytes,
                                         void* hip_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Distillation: a network learns another's answers (a way to combine CNs beside averaging them).
+ * Row r has `classes` logits z, a teacher's `top` entries (class idx, logit t) and a label y.
+ *   p = softmax(t / T) over the row's entries, q = softmax(z / T), s = softmax(z):
+ *   loss = (1 - alpha) T^2 sum_j p_j (log p_j - log q_{idx_j}) - alpha log s_y
+ *   dz_v = g [ (1 - alpha) T (q_v - sum_{j: idx_j = v} p_j) + alpha (s_v - [v = y]) ]
+ * (with alpha = 1 the cross-entropy cost of eq. (6) and the output error of eq. (10)).  An entry
+ * whose class lies outside [0, classes) is padding; one class may stand twice; a teacher logit of
+ * -inf has no weight.  A label outside [0, classes) is none.  A row without entries and without a
+ * label, and one whose logits are all -inf, has loss 0 and gradient 0; its logits may hold
+ * anything in the first case.  z, t and dz are of `type`; sums and statistics are fp32, and the
+ * maximum is subtracted first, so logits near the type's limits do not overflow.  The order of the
+ * sums depends on the sizes alone.  No handle, as for the grouped products above. */
+typedef struct {
+    const void* z_dev;      /* [n][classes] */
+    int64_t z_ld;
+    int32_t type;
+    int32_t classes;        /* 1..2^30 */
+    int64_t n;
+    const int32_t* idx_dev; /* [n][top] */
+    const void* t_dev;      /* [n][top] */
+    int32_t top;            /* 0..1024 */
+    const int32_t* y_dev;   /* [n]; read if alpha > 0 */
+    float temperature;      /* T, 1e-6..1e6 */
+    float alpha;            /* 0..1 */
+} pnn_distill;
+
+/* Size of the statistics that pnn_distill_loss leaves for pnn_distill_grad. */
+pnn_status pnn_distill_bytes(int64_t n, int32_t classes, int64_t* bytes);
+
+/* loss_dev [n] fp32, and the statistics (16-byte aligned). */
+pnn_status pnn_distill_loss(const pnn_distill* args, float* loss_dev, void* stats_dev, int64_t stats_bytes, void* hip_stream);
+
+/* dz_dev [n][classes] from the same arguments and their statistics; g_dev [n] is the gradient of
+ * each row's loss (NULL: 1).  A row whose g is 0 gets 0, whatever its logits.  dz_dev may be z_dev
+ * (with the same distance between rows). */
+pnn_status pnn_distill_grad(const pnn_distill* args, const float* g_dev, const void* stats_dev, int64_t stats_bytes, void* dz_dev,
+                            int64_t dz_ld, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,388 @@
+// distill.hpp -- the loss of a network's logits against a teacher's top logits, and its gradient.
+//
+// Row r of the student has V logits z; its teacher gives k entries (class i_j, logit t_j), entries
+// whose class lies outside [0, V) are padding.  With p = softmax(t / T) over the row's entries,
+// q = softmax(z / T) and s = softmax(z) over all classes, and a label y (none if outside [0, V)):
+//   loss = (1 - alpha) T^2 sum_j p_j (log p_j - log q_{i_j}) - alpha log s_y
+//   dz_v = g [ (1 - alpha) T (q_v - sum_{j: i_j = v} p_j) + alpha (s_v - [v = y]) ]
+// Both passes stream z: one running maximum and one or two running sums of exponentials forward,
+// which the gradient then only has to divide by.  The maximum is subtracted before anything is
+// scaled, and log q is formed as (z - m) / T - log sum, so logits near the type's ends lose nothing.
+// Bound by the bytes of z (read twice) and dz; statistics and sums are fp32.
+#pragma once
+#include "groups.hpp"
+
+namespace pnn {
+
+constexpr int DL_MAX_TOP = 1024;  // most entries of a row (they are staged in LDS)
+constexpr int DL_WAVE_TOP = 64;   // most entries of a row that one wave takes
+constexpr int DL_TINY_TOP = 16, DL_TINY = 128;  // most entries and classes of a row that 16 lanes take
+
+// what a row has: bit 0 teacher entries, bit 1 a label
+struct DistillArgs {
+    const void* z;
+    int64_t ldz, n;
+    int V, k;
+    const int32_t* idx;
+    const void* t;
+    const int32_t* y;         // nullable
+    float ct, cs;             // log2(e) / T, and of the one sum or of the second: log2(e)
+    float inv_t, wt, ws;      // 1 / T; weights of the two losses
+    float gt, gs;             // weights of the two gradients: (1 - alpha) T, alpha
+    int S, part;              // parts of a row and classes of a part
+    float4* stats;            // [n] maximum, reciprocals of the sums at T and at 1, what the row has
+    float4* parts;            // [n][S] maximum, sums
+    float* loss;
+    const float* g;
+    void* dz;
+    int64_t lddz;
+};
+
+constexpr float DL_INF = __builtin_huge_valf();
+
+// running maximum and sums of exponentials; MODE 1: one sum (at the scale ct), 2: at ct and at cs
+struct Sums { float m, a, b; };
+
+__device__ inline float dl_ref(float m) { return m == -DL_INF ? 0.0f : m; }
+
+template <int MODE>
+__device__ inline void dl_raise(Sums& s, float m, const DistillArgs& d) {
+    if (m > s.m) {
+        const float by = s.m - m;  // (-inf before the first value: the sums are 0, or NaN, and stay so)
+        s.a *= exp2f(by * d.ct);
+        if (MODE == 2) s.b *= exp2f(by * d.cs);
+        s.m = m;
+    }
+}
+
+template <int MODE, int N>
+__device__ inline void dl_add(Sums& s, const float (&z)[N], const DistillArgs& d) {
+    float m = z[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
+    dl_raise<MODE>(s, m, d);
+    const float ref = dl_ref(s.m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        s.a += __builtin_amdgcn_exp2f((z[i] - ref) * d.ct);
+        if (MODE == 2) s.b += __builtin_amdgcn_exp2f((z[i] - ref) * d.cs);
+    }
+}
+
+template <int MODE>
+__device__ inline void dl_join(Sums& s, float m, float a, float b, const DistillArgs& d) {
+    const float top = fmaxf(s.m, m), ref = dl_ref(top);
+    const float f = s.m - ref, h = m - ref;
+    s.a = s.a * __builtin_amdgcn_exp2f(f * d.ct) + a * __builtin_amdgcn_exp2f(h * d.ct);
+    if (MODE == 2) s.b = s.b * __builtin_amdgcn_exp2f(f * d.cs) + b * __builtin_amdgcn_exp2f(h * d.cs);
+    s.m = top;
+}
+
+template <int MODE, int G>
+__device__ inline void dl_join_lanes(Sums& s, const DistillArgs& d) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) {
+        const float m = __shfl_xor(s.m, o), a = __shfl_xor(s.a, o), b = MODE == 2 ? __shfl_xor(s.b, o) : 0.0f;
+        dl_join<MODE>(s, m, a, b, d);
+    }
+}
+
+template <int G> __device__ inline float dl_max(float v) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+template <int G> __device__ inline float dl_sum(float v) {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// The teacher's distribution of a row, as G lanes see it: maximum and sum of the entries'
+// exponentials.  A sum of 0: the row has no entries (or only ones of -inf).
+struct Teacher { float ref, mass; };
+
+template <typename T, int G>
+__device__ inline Teacher dl_teacher(const DistillArgs& d, int64_t row, int lane) {
+    const int32_t* idx = d.idx + row * d.k;
+    const T* t = (const T*)d.t + row * d.k;
+    float m = -DL_INF;
+    for (int j = lane; j < d.k; j += G)
+        if ((unsigned)idx[j] < (unsigned)d.V) m = fmaxf(m, to_f<T>(t[j]));
+    const float ref = dl_ref(dl_max<G>(m));
+    float s = 0.0f;
+    for (int j = lane; j < d.k; j += G)
+        if ((unsigned)idx[j] < (unsigned)d.V) s += exp2f((to_f<T>(t[j]) - ref) * d.ct);
+    return {ref, dl_sum<G>(s)};
+}
+
+// loss and statistics of a row from its sums, by G lanes
+template <typename T, int G>
+__device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, const Teacher& te, int has, const Sums& s, bool two) {
+    const T* z = (const T*)d.z + row * d.ldz;
+    const float la = logf(s.a), lb = two ? logf(s.b) : la;
+    float kl = 0.0f;
+    if (has & 1) {
+        const int32_t* idx = d.idx + row * d.k;
+        const T* t = (const T*)d.t + row * d.k;
+        const float lm = logf(te.mass), im = 1.0f / te.mass;
+        for (int j = lane; j < d.k; j += G) {
+            const int i = idx[j];
+            if ((unsigned)i >= (unsigned)d.V) continue;
+            const float e = to_f<T>(t[j]) - te.ref, p = exp2f(e * d.ct) * im;
+            if (p == 0.0f) continue;  // an entry without weight, whatever the student gives it
+            kl += p * ((e * d.inv_t - lm) - ((to_f<T>(z[i]) - s.m) * d.inv_t - la));
+        }
+    }
+    kl = dl_sum<G>(kl);
+    if (lane != 0) return;
+    float loss = 0.0f;
+    if (s.a == 0.0f) has = 0;  // every logit is -inf: nothing to learn from
+    if (has & 1) loss += d.wt * kl;
+    if (has & 2) loss += d.ws * (lb - (to_f<T>(z[d.y[row]]) - s.m));
+    d.loss[row] = loss;
+    d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (two ? s.b : s.a), (float)has);
+}
+
+__device__ inline int dl_label(const DistillArgs& d, int64_t row) {
+    if (!d.y) return -1;
+    const int y = d.y[row];
+    return (unsigned)y < (unsigned)d.V ? y : -1;
+}
+
+template <typename T>
+__device__ inline void dl_load8(float (&v)[8], const T* p, int nv, float fill) {
+    Raw8<T> r;
+    load8(r, p, nv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = r.v[i >> 2][i & 3];
+        else v[i] = i & 1 ? bf_hi(r.v[i >> 1]) : bf_lo(r.v[i >> 1]);
+    }
+    if (nv < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < nv ? v[i] : fill;
+    }
+}
+
+__device__ inline void store8(float* p, const float (&v)[8], int nv) {
+    if (nv >= 8) {
+        *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
+        *(f4_a4*)(p + 4) = f4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < nv) p[i] = v[i];
+    }
+}
+__device__ inline void store8(bf16_t* p, const float (&v)[8], int nv) {
+    if (nv >= 8) {
+        *(u4v_a2*)p = u4v{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < nv) p[i] = f2bf(v[i]);
+    }
+}
+
+// dz of one value
+__device__ inline float dl_grad(const DistillArgs& d, float z, const float4& st, float ea, float eb, float gt, float gs, float g,
+                                float psum, bool label) {
+    const float q = __builtin_amdgcn_exp2f((z - st.x) * d.ct) * ea;
+    const float s = __builtin_amdgcn_exp2f((z - st.x) * d.cs) * eb;
+    return g * (gt * (q - psum) + gs * (s - (label ? 1.0f : 0.0f)));
+}
+
+// Loss, W waves a row (256 / (64 W) rows a workgroup), or one part of a row per workgroup (S > 1).
+template <typename T, int MODE, int W>
+__global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
+    __shared__ Sums across[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0;
+    if (row >= d.n) return;
+    const int in = W == 4 ? tid : lane;
+    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
+    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    if (has == 0) {  // a padding row: its logits are not read
+        if (in == 0 && part == 0) {
+            d.loss[row] = 0.0f;
+            d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        return;
+    }
+    const T* z = (const T*)d.z + row * d.ldz;
+    const int64_t lo = (int64_t)part * d.part;
+    const int len = (int)(d.V - lo < d.part ? d.V - lo : d.part);
+    Sums s = {-DL_INF, 0.0f, 0.0f};
+    for (int v = in * 8; v < len; v += W * 512) {
+        float x[8];
+        dl_load8<T>(x, z + lo + v, len - v, -DL_INF);
+        dl_add<MODE>(s, x, d);
+    }
+    dl_join_lanes<MODE, 64>(s, d);
+    if (W == 4) {
+        if (lane == 0) across[wave] = s;
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) dl_join<MODE>(s, across[w].m, across[w].a, across[w].b, d);
+        if (d.S > 1) {
+            if (lane == 0) d.parts[row * d.S + part] = make_float4(s.m, s.a, s.b, 0.0f);
+            return;
+        }
+    }
+    dl_finish<T, 64>(d, row, lane, te, has, s, MODE == 2);
+}
+
+// joins the parts of a row, one wave a row
+template <typename T, int MODE>
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
+    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    if (has == 0) return;  // (written with the parts)
+    Sums s = {-DL_INF, 0.0f, 0.0f};
+    for (int p = lane; p < d.S; p += 64) {
+        const float4 v = d.parts[row * d.S + p];
+        dl_join<MODE>(s, v.x, v.y, v.z, d);
+    }
+    dl_join_lanes<MODE, 64>(s, d);
+    dl_finish<T, 64>(d, row, lane, te, has, s, MODE == 2);
+}
+
+// Gradient, W waves a row or one part of a row per workgroup.  The entries' classes (and the label)
+// are written again after the stream has passed, from logits read before it: so dz may be z.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
+    constexpr int TOP = W == 4 ? DL_MAX_TOP : DL_WAVE_TOP;
+    __shared__ int sidx[4 / W][TOP];
+    __shared__ float sp[4 / W][TOP], sz[4 / W][TOP + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0, slot = W == 4 ? 0 : wave;
+    if (row >= d.n) return;
+    const int in = W == 4 ? tid : lane;
+    const T* z = (const T*)d.z + row * d.ldz;
+    T* dz = (T*)d.dz + row * d.lddz;
+    const int lo = part * d.part, hi = d.V - lo < d.part ? d.V : lo + d.part;
+    const float4 st = d.stats[row];
+    const float g = d.g ? d.g[row] : 1.0f;
+    const int has = g == 0.0f ? 0 : (int)st.w;
+    if (has == 0) {
+        const float none[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int v = lo + in * 8; v < hi; v += W * 512) store8(dz + v, none, hi - v);
+        return;
+    }
+    auto meet = [] {
+        if (W == 4) __syncthreads();
+        else __threadfence_block();
+    };
+    const float gt = has & 1 ? d.gt : 0.0f, gs = has & 2 ? d.gs : 0.0f;
+    const float ea = has & 1 ? st.y : 0.0f, eb = has & 2 ? st.z : 0.0f;
+    const int label = has & 2 ? dl_label(d, row) : -1;
+    const int k = has & 1 ? d.k : 0;
+    if (has & 1) {
+        const Teacher te = dl_teacher<T, 64>(d, row, lane);
+        const float im = 1.0f / te.mass;
+        for (int j = in; j < k; j += 64 * W) {
+            const int i = d.idx[row * d.k + j];
+            const bool mine = i >= lo && i < hi;
+            sidx[slot][j] = mine ? i : -1;
+            sp[slot][j] = mine ? exp2f((to_f<T>(((const T*)d.t)[row * d.k + j]) - te.ref) * d.ct) * im : 0.0f;
+            sz[slot][j] = mine ? to_f<T>(z[i]) : 0.0f;
+        }
+    }
+    const bool own_label = label >= lo && label < hi;
+    if (in == 0) sz[slot][TOP] = own_label ? to_f<T>(z[label]) : 0.0f;
+    meet();
+    for (int v = lo + in * 8; v < hi; v += W * 512) {
+        float x[8];
+        dl_load8<T>(x, z + v, hi - v, 0.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = dl_grad(d, x[i], st, ea, eb, gt, gs, g, 0.0f, false);
+        store8(dz + v, x, hi - v);
+    }
+    meet();  // (waits for the stores: those below come after them)
+    for (int j = in; j < k; j += 64 * W) {
+        const int i = sidx[slot][j];
+        if (i < 0) continue;
+        float p = 0.0f;
+        bool first = true;
+        for (int o = 0; o < k; ++o)
+            if (sidx[slot][o] == i) {
+                p += sp[slot][o];
+                if (o < j) first = false;
+            }
+        if (first) dz[i] = from_f<T>(dl_grad(d, sz[slot][j], st, ea, eb, gt, gs, g, p, i == label));
+    }
+    if (in == 0 && own_label) {
+        bool listed = false;
+        for (int o = 0; o < k; ++o) listed |= sidx[slot][o] == label;
+        if (!listed) dz[label] = from_f<T>(dl_grad(d, sz[slot][TOP], st, ea, eb, gt, gs, g, 0.0f, true));
+    }
+}
+
+// Few classes: 16 lanes a row, at most eight values a lane in registers.
+template <typename T, int MODE>
+__global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
+    const int lane = threadIdx.x & 15;
+    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (row >= d.n) return;
+    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 16>(d, row, lane) : Teacher{0.0f, 0.0f};
+    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    if (has == 0) {
+        if (lane == 0) {
+            d.loss[row] = 0.0f;
+            d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        return;
+    }
+    const T* z = (const T*)d.z + row * d.ldz;
+    Sums s = {-DL_INF, 0.0f, 0.0f};
+    for (int v = lane; v < d.V; v += 16) {
+        const float x[1] = {to_f<T>(z[v])};
+        dl_add<MODE>(s, x, d);
+    }
+    dl_join_lanes<MODE, 16>(s, d);
+    dl_finish<T, 16>(d, row, lane, te, has, s, MODE == 2);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void distill_grad_tiny_kernel(DistillArgs d) {
+    const int lane = threadIdx.x & 15;
+    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (row >= d.n) return;
+    const T* z = (const T*)d.z + row * d.ldz;
+    T* dz = (T*)d.dz + row * d.lddz;
+    const float4 st = d.stats[row];
+    const float g = d.g ? d.g[row] : 1.0f;
+    const int has = g == 0.0f ? 0 : (int)st.w;
+    const float gt = has & 1 ? d.gt : 0.0f, gs = has & 2 ? d.gs : 0.0f;
+    const float ea = has & 1 ? st.y : 0.0f, eb = has & 2 ? st.z : 0.0f;
+    const int label = has & 2 ? dl_label(d, row) : -1;
+    int i = -1;
+    float p = 0.0f;
+    if (has & 1) {  // (k <= 16: an entry a lane)
+        const Teacher te = dl_teacher<T, 16>(d, row, lane);
+        if (lane < d.k) {
+            i = d.idx[row * d.k + lane];
+            if ((unsigned)i < (unsigned)d.V) p = exp2f((to_f<T>(((const T*)d.t)[row * d.k + lane]) - te.ref) * d.ct) / te.mass;
+            else i = -1;
+        }
+    }
+    const int k = d.k;
+    for (int b = 0; b < d.V; b += 16) {
+        const int v = b + lane;
+        float sum = 0.0f;
+        for (int j = 0; j < k; ++j) {
+            const int ij = __shfl(i, j, 16);
+            const float pj = __shfl(p, j, 16);
+            if (ij == v) sum += pj;
+        }
+        if (v < d.V) dz[v] = has == 0 ? from_f<T>(0.0f) : from_f<T>(dl_grad(d, to_f<T>(z[v]), st, ea, eb, gt, gs, g, sum, v == label));
+    }
+}
+
+}  // namespace pnn

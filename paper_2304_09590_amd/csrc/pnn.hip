@@ -35,6 +35,7 @@
 #include "../../include/pnn.h"
 #include "kernels.hpp"
 #include "groups.hpp"
+#include "distill.hpp"
 
 using namespace pnn;
 
@@ -1794,3 +1795,4 @@ void pnn_destroy(pnn_net* n) {
 }  // extern "C"
 
 #include "groups_host.hpp"
+#include "distill_host.hpp"

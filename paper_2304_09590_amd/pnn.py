@@ -47,6 +47,12 @@ class PnnGroupLayer(ctypes.Structure):
                 ("b_net", ctypes.c_int64)]
 
 
+class PnnDistill(ctypes.Structure):
+    _fields_ = [("z", ctypes.c_void_p), ("z_ld", ctypes.c_int64), ("type", ctypes.c_int32), ("classes", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("idx", ctypes.c_void_p), ("t", ctypes.c_void_p), ("top", ctypes.c_int32),
+                ("y", ctypes.c_void_p), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
+
+
 class PnnError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -112,6 +118,12 @@ def lib() -> ctypes.CDLL:
         L.pnn_grouped_backward_weights.argtypes = [groups, layer, vp, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
         for name in ("pnn_group_bytes", "pnn_group_rows", "pnn_grouped_forward", "pnn_grouped_workspace",
                      "pnn_grouped_backward_input", "pnn_grouped_backward_weights"):
+            getattr(L, name).restype = i32
+        distill = P(PnnDistill)
+        L.pnn_distill_bytes.argtypes = [i64, i32, P(i64)]
+        L.pnn_distill_loss.argtypes = [distill, vp, vp, i64, vp]
+        L.pnn_distill_grad.argtypes = [distill, vp, vp, i64, vp, i64, vp]
+        for name in ("pnn_distill_bytes", "pnn_distill_loss", "pnn_distill_grad"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -460,3 +472,49 @@ def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: b
         _call(lib().pnn_grouped_backward_weights, "pnn_grouped_backward_weights", ctypes.byref(groups.struct),
               ctypes.byref(layer), pd, ldd, px, ldx, pw, dw.stride(0), ldw, pb, netb, ps, size, on.stream)
     return dw, db
+
+
+# ---- distillation from a teacher's top logits, without a handle ------------------------------
+
+def _distill(z, idx, t, y, temperature, alpha) -> PnnDistill:
+    import torch
+    if z.dim() != 2:
+        raise ValueError(f"z has shape {tuple(z.shape)}, expected a matrix")
+    n, top = z.shape[0], (idx.shape[-1] if idx is not None else 0)
+    pz, ldz = _rows(z, "z", z.shape)
+    a = PnnDistill(pz, ldz, _type_of(z), z.shape[1], n, None, None, top, None, temperature, alpha)
+    if idx is not None:
+        a.idx, a.t = _values(idx, "idx", (n, top), torch.int32), _values(t, "t", (n, top), z.dtype)
+    if y is not None:
+        a.y = _values(y, "y", (n,), torch.int32)
+    return a
+
+
+def distill_loss(z, idx, t, y=None, temperature: float = 1.0, alpha: float = 0.0, stream=None):
+    """(loss [n] fp32, stats for distill_grad) of logits z [n, classes] against the teacher's entries: classes
+    idx int32 [n, top], logits t [n, top] of z's type; labels y int32 [n] weigh alpha (see pnn_distill in pnn.h)."""
+    import torch
+    a = _distill(z, idx, t, y, temperature, alpha)
+    with _On([z, idx, t, y], stream) as on:
+        size = ctypes.c_int64()
+        _call(lib().pnn_distill_bytes, "pnn_distill_bytes", a.n, a.classes, ctypes.byref(size))
+        loss = torch.empty(a.n, dtype=torch.float32, device=on.device)
+        stats = torch.empty(size.value // 4, dtype=torch.float32, device=on.device)
+        _call(lib().pnn_distill_loss, "pnn_distill_loss", ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), size.value,
+              on.stream)
+    return loss, stats
+
+
+def distill_grad(z, idx, t, stats, g=None, y=None, temperature: float = 1.0, alpha: float = 0.0, out=None, stream=None):
+    """The gradient of z from distill_loss's arguments and statistics; g fp32 [n] is the gradient of each row's
+    loss (None: 1).  out may be z."""
+    import torch
+    a = _distill(z, idx, t, y, temperature, alpha)
+    with _On([z, idx, t, stats, g, y, out], stream) as on:
+        pg = _values(g, "g", (a.n,), torch.float32) if g is not None else None
+        ps = _values(stats, "stats", stats.shape, torch.float32)
+        if out is None:
+            out = torch.empty(z.shape, dtype=z.dtype, device=on.device)
+        po, ldo = _rows(out, "out", z.shape, z.dtype)
+        _call(lib().pnn_distill_grad, "pnn_distill_grad", ctypes.byref(a), pg, ps, 4 * stats.numel(), po, ldo, on.stream)
+    return out
