@@ -19,8 +19,8 @@
  *    and a pnn_infer call with correct_host != NULL wait for the device.  After a training
  *    epoch on a persistent plan (pnn_plan), the next call that consumes the CNs other than
  *    pnn_train_epoch first waits for that epoch to end, to read its failure flag.
- *  - pnn_train_epoch, pnn_train_epoch_order, pnn_merge and pnn_infer (without a count) may be
- *    recorded into a graph, after a call of the same kind with at least as many rows has sized the
+ *  - pnn_train_epoch, pnn_train_epoch_order, pnn_merge, pnn_infer (without a count), pnn_infer_routed
+ *    and pnn_train_routed may be recorded into a graph, after a call of the same kind with at least as many rows has sized the
  *    handle's workspace (growth is refused while the stream records: PNN_EHIP, nothing recorded).  The
  *    graph may be replayed until pnn_destroy, also after later calls with more rows.
  *  - Errors are returned as a pnn_status; the message of the last failure is available
@@ -354,6 +354,32 @@ pnn_status pnn_distill_loss(const pnn_distill* args, float* loss_dev, void* stat
  * (with the same distance between rows). */
 pnn_status pnn_distill_grad(const pnn_distill* args, const float* g_dev, const void* stats_dev, int64_t stats_bytes, void* dz_dev,
                             int64_t dz_ld, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * A handle's child networks on rows that name them (at most 1,024 CNs: PNN_EINVAL otherwise).  Both
+ * calls keep their grouping, activations and errors in one workspace of the handle that grows with the
+ * pairs of a call, so calls of one handle on different streams have to be ordered by the caller; they
+ * may be recorded into a graph as the other calls are (see the top).  x_dev
+ * [rows][sizes[0]] fp32, ids_dev [rows][per_row] as in pnn_group_rows.  Products, activations and
+ * roundings are those of pnn_infer and pnn_train_epoch up to the order of the fp32 sums. */
+
+/* Answers of several networks combined (a combination of outputs where pnn_merge combines weights):
+ * out_dev[r] (nullable) [rows][sizes[L]] = sum_j weights_dev[r per_row + j] x^L of pair j over the
+ * row's pairs that are not dropped (weights NULL: their mean); pred_dev[r] its argmax (lowest index
+ * on ties).  A row whose pairs are all dropped gets 0 and the class -1. */
+pnn_status pnn_infer_routed(pnn_net* net, const float* x_dev, int64_t rows, const int32_t* ids_dev, int32_t per_row,
+                            const float* weights_dev, int32_t* pred_dev, float* out_dev, void* hip_stream);
+
+/* One mini-batch step of every CN on the pairs that name it (the configured batch size plays no
+ * part), towards a teacher's top logits and labels: the loss of pnn_distill_loss at the pair's
+ * output sums z^L, gradients averaged over the CN's pairs, W <- W - eta / pairs * gradient.  Row r's
+ * pairs share its entries idx_dev, t_dev [rows][top] (fp32) and its label y_dev [rows] (read if
+ * alpha > 0).  alpha = 1 is the step of pnn_train_epoch.  Needs a softmax output layer (PNN_EINVAL).
+ * A CN without pairs keeps its parameters; the merged network keeps its own.  loss_dev (nullable)
+ * [rows per_row] receives the pairs' losses before the step, 0 for dropped ones. */
+pnn_status pnn_train_routed(pnn_net* net, const float* x_dev, int64_t rows, const int32_t* ids_dev, int32_t per_row,
+                            const int32_t* idx_dev, const float* t_dev, int32_t top, const int32_t* y_dev, float temperature,
+                            float alpha, float* loss_dev, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,6 @@ constexpr int DL_MAX_TOP = 1024;  // most entries of a row (they are staged in L
 constexpr int DL_WAVE_TOP = 64;   // most entries of a row that one wave takes
 constexpr int DL_TINY_TOP = 16, DL_TINY = 128;  // most entries and classes of a row that 16 lanes take
 
-// what a row has: bit 0 teacher entries, bit 1 a label
 struct DistillArgs {
     const void* z;
     int64_t ldz, n;
@@ -29,6 +28,9 @@ struct DistillArgs {
     float ct, cs;             // log2(e) / T, and of the one sum or of the second: log2(e)
     float inv_t, wt, ws;      // 1 / T; weights of the two losses
     float gt, gs;             // weights of the two gradients: (1 - alpha) T, alpha
+    int rows_per;             // rows that share entries and a label: those of row / rows_per
+    const int32_t* ids;       // (nullable) a row whose id lies outside [0, K) has neither
+    int K;
     int S, part;              // parts of a row and classes of a part
     float4* stats;            // [n] maximum, reciprocals of the sums at T and at 1, what the row has
     float4* parts;            // [n][S] maximum, sums
@@ -104,8 +106,8 @@ struct Teacher { float ref, mass; };
 
 template <typename T, int G>
 __device__ inline Teacher dl_teacher(const DistillArgs& d, int64_t row, int lane) {
-    const int32_t* idx = d.idx + row * d.k;
-    const T* t = (const T*)d.t + row * d.k;
+    const int32_t* idx = d.idx + row / d.rows_per * d.k;
+    const T* t = (const T*)d.t + row / d.rows_per * d.k;
     float m = -DL_INF;
     for (int j = lane; j < d.k; j += G)
         if ((unsigned)idx[j] < (unsigned)d.V) m = fmaxf(m, to_f<T>(t[j]));
@@ -123,8 +125,8 @@ __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, co
     const float la = logf(s.a), lb = two ? logf(s.b) : la;
     float kl = 0.0f;
     if (has & 1) {
-        const int32_t* idx = d.idx + row * d.k;
-        const T* t = (const T*)d.t + row * d.k;
+        const int32_t* idx = d.idx + row / d.rows_per * d.k;
+        const T* t = (const T*)d.t + row / d.rows_per * d.k;
         const float lm = logf(te.mass), im = 1.0f / te.mass;
         for (int j = lane; j < d.k; j += G) {
             const int i = idx[j];
@@ -139,15 +141,21 @@ __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, co
     float loss = 0.0f;
     if (s.a == 0.0f) has = 0;  // every logit is -inf: nothing to learn from
     if (has & 1) loss += d.wt * kl;
-    if (has & 2) loss += d.ws * (lb - (to_f<T>(z[d.y[row]]) - s.m));
+    if (has & 2) loss += d.ws * (lb - (to_f<T>(z[d.y[row / d.rows_per]]) - s.m));
     d.loss[row] = loss;
     d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (two ? s.b : s.a), (float)has);
 }
 
 __device__ inline int dl_label(const DistillArgs& d, int64_t row) {
     if (!d.y) return -1;
-    const int y = d.y[row];
+    const int y = d.y[row / d.rows_per];
     return (unsigned)y < (unsigned)d.V ? y : -1;
+}
+
+// what a row learns from (bit 0 entries, bit 1 a label)
+__device__ inline int dl_has(const DistillArgs& d, int64_t row, const Teacher& te) {
+    if (d.ids && (unsigned)d.ids[row] >= (unsigned)d.K) return 0;
+    return (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
 }
 
 template <typename T>
@@ -203,7 +211,7 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
     const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    const int has = dl_has(d, row, te);
     if (has == 0) {  // a padding row: its logits are not read
         if (in == 0 && part == 0) {
             d.loss[row] = 0.0f;
@@ -241,7 +249,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
     const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    const int has = dl_has(d, row, te);
     if (has == 0) return;  // (written with the parts)
     Sums s = {-DL_INF, 0.0f, 0.0f};
     for (int p = lane; p < d.S; p += 64) {
@@ -286,11 +294,12 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     if (has & 1) {
         const Teacher te = dl_teacher<T, 64>(d, row, lane);
         const float im = 1.0f / te.mass;
+        const int64_t first = row / d.rows_per * d.k;
         for (int j = in; j < k; j += 64 * W) {
-            const int i = d.idx[row * d.k + j];
+            const int i = d.idx[first + j];
             const bool mine = i >= lo && i < hi;
             sidx[slot][j] = mine ? i : -1;
-            sp[slot][j] = mine ? exp2f((to_f<T>(((const T*)d.t)[row * d.k + j]) - te.ref) * d.ct) * im : 0.0f;
+            sp[slot][j] = mine ? exp2f((to_f<T>(((const T*)d.t)[first + j]) - te.ref) * d.ct) * im : 0.0f;
             sz[slot][j] = mine ? to_f<T>(z[i]) : 0.0f;
         }
     }
@@ -331,7 +340,7 @@ __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
     const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (row >= d.n) return;
     const Teacher te = d.wt != 0.0f ? dl_teacher<T, 16>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    const int has = dl_has(d, row, te);
     if (has == 0) {
         if (lane == 0) {
             d.loss[row] = 0.0f;
@@ -367,8 +376,9 @@ __global__ __launch_bounds__(256) void distill_grad_tiny_kernel(DistillArgs d) {
     if (has & 1) {  // (k <= 16: an entry a lane)
         const Teacher te = dl_teacher<T, 16>(d, row, lane);
         if (lane < d.k) {
-            i = d.idx[row * d.k + lane];
-            if ((unsigned)i < (unsigned)d.V) p = exp2f((to_f<T>(((const T*)d.t)[row * d.k + lane]) - te.ref) * d.ct) / te.mass;
+            const int64_t first = row / d.rows_per * d.k;
+            i = d.idx[first + lane];
+            if ((unsigned)i < (unsigned)d.V) p = exp2f((to_f<T>(((const T*)d.t)[first + lane]) - te.ref) * d.ct) / te.mass;
             else i = -1;
         }
     }

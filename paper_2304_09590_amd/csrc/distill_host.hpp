@@ -63,6 +63,7 @@ DistillArgs distill_args(const pnn_distill* a, void* stats, int width) {
     d.wt = a->top > 0 ? (float)((1.0 - alpha) * T * T) : 0.0f; d.ws = (float)alpha;
     d.gt = (float)((1.0 - alpha) * T); d.gs = (float)alpha;
     if (d.wt == 0.0f) d.ct = d.cs;  // the label alone: the one sum is at 1
+    d.rows_per = 1;
     d.S = 1; d.part = a->classes;
     if (width == DL_BLOCK) distill_parts(a->n, a->classes, &d.S, &d.part);
     d.stats = (float4*)stats;

@@ -206,8 +206,8 @@ struct GroupGemm {
     float* db;                 // (weight gradient) bias gradient, nullable
     int64_t dbnet;
     int splits;                // (weight gradient) parts of a group, summed by group_join_kernel
-    float upd;                 // (weight gradient) != 0: y -= upd / pairs * sum instead of y = sum
-    bf16_t* shadow;            // (with upd) bf16 copy of y, same strides
+    float lr;                  // (weight gradient) != 0: y -= lr / pairs * sum instead of y = sum
+    bf16_t* shadow;            // (with lr) bf16 copy of y, same strides
 };
 
 // The activations of act_fn; a NaN stays one (the rectifiers' comparison is z < 0).
@@ -451,18 +451,18 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     // a lane holds results m0 + wm + 16 i + 4 kg + r of column n = wn + 16 j + l15
     if (DIR == GR_DW) {
         const int pairs = g.off[e + 1] - g.off[e];
-        const float scale = g.upd != 0.0f && pairs > 0 ? g.upd / (float)pairs : 0.0f;
+        const float scale = g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int n = wn + 16 * j + l15;
             if (n >= nv) continue;
             float* y = (float*)g.y + ((int64_t)split * g.K + e) * g.ynet + (int64_t)(n0 + n) * g.ldy;
-            if (g.upd != 0.0f && pairs == 0) continue;
+            if (g.lr != 0.0f && pairs == 0) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int m = m0 + wm + 16 * i + 4 * kg, left = g.M - m;
                 float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                if (g.upd != 0.0f)
+                if (g.lr != 0.0f)
                     for (int r = 0; r < 4; ++r)
                         if (r < left) {
                             v[r] = y[m + r] - scale * v[r];
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             }
             if (bias_rows && kg == 0) {
                 float* db = g.db + ((int64_t)split * g.K + e) * g.dbnet + n0 + n;
-                *db = g.upd != 0.0f ? *db - scale * accb[j][0] : accb[j][0];
+                *db = g.lr != 0.0f ? *db - scale * accb[j][0] : accb[j][0];
             }
         }
         return;
@@ -503,7 +503,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     }
 }
 
-// the sum of a weight gradient's parts, in their order; with upd the update
+// the sum of a weight gradient's parts, in their order; with lr the update
 struct GroupJoin {
     const int32_t* off;
     const float *part, *dbpart;   // [splits][K][N][M], [splits][K][N]
@@ -512,7 +512,7 @@ struct GroupJoin {
     int64_t ldy, ynet;
     float* db;
     int64_t dbnet;
-    float upd;
+    float lr;
     bf16_t* shadow;
 };
 
@@ -527,10 +527,10 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupJoin g) {
         const int e = (int)(w ? q / per : q / g.N);
         const int64_t in = w ? q - e * per : q - (int64_t)e * g.N;
         float* out = w ? g.y + e * g.ynet + in / g.M * g.ldy + in % g.M : g.db + e * g.dbnet + in;
-        if (g.upd != 0.0f) {
+        if (g.lr != 0.0f) {
             const int pairs = g.off[e + 1] - g.off[e];
             if (pairs == 0) continue;
-            s = *out - g.upd / (float)pairs * s;
+            s = *out - g.lr / (float)pairs * s;
             if (w && g.shadow) g.shadow[out - g.y] = f2bf(s);
         }
         *out = s;
@@ -709,6 +709,55 @@ __global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
         }
         ((TO*)g.y)[pair * g.ldy + m] = from_f<TO>(v);
     }
+}
+
+// A row's answer: the outputs x^L of its pairs, weighted (without weights each counts the same), and
+// the class of the largest (lowest index on ties).  A row without a network: outputs 0, class -1.
+__global__ __launch_bounds__(256) void routed_answer_kernel(const float* z, const int32_t* ids, const float* weights, int64_t n,
+                                                            int per_row, int K, int O, int act, int32_t* pred, float* out) {
+    const int64_t r = blockIdx.x * 256ll + threadIdx.x;
+    if (r >= n) return;
+    float sum[MAX_OUT], total = 0.0f;
+#pragma unroll
+    for (int o = 0; o < MAX_OUT; ++o) sum[o] = 0.0f;
+    int kept = 0;
+    for (int j = 0; j < per_row; ++j) {
+        const int64_t p = r * per_row + j;
+        if ((unsigned)ids[p] >= (unsigned)K) continue;
+        ++kept;
+        const float w = weights ? weights[p] : 1.0f;
+        float v[MAX_OUT], m = -__builtin_huge_valf(), s = 0.0f;
+#pragma unroll
+        for (int o = 0; o < MAX_OUT; ++o)
+            if (o < O) {
+                v[o] = z[p * O + o];
+                m = fmaxf(m, v[o]);
+            }
+#pragma unroll
+        for (int o = 0; o < MAX_OUT; ++o)
+            if (o < O) {
+                v[o] = act == ACT_SOFTMAX ? expf(v[o] - m) : group_act(act, v[o]);
+                s += v[o];
+            }
+        const float by = act == ACT_SOFTMAX ? w / s : w;
+#pragma unroll
+        for (int o = 0; o < MAX_OUT; ++o)
+            if (o < O) sum[o] += v[o] * by;
+    }
+    total = weights || kept == 0 ? 1.0f : 1.0f / (float)kept;
+    int best = kept ? 0 : -1;
+    float top = 0.0f;
+#pragma unroll
+    for (int o = 0; o < MAX_OUT; ++o)
+        if (o < O) {
+            const float v = sum[o] * total;
+            if (out) out[r * O + o] = v;
+            if (kept && (o == 0 || v > top)) {
+                top = v;
+                best = o;
+            }
+        }
+    pred[r] = best;
 }
 
 }  // namespace pnn

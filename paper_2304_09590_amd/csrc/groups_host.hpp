@@ -133,10 +133,10 @@ pnn_status run_group_pairs(const GroupGemm& a, int32_t type, int32_t out_type, b
     return out_type == PNN_FP32 ? run_group_pairs<DIR, bf16_t, float>(a, few, s) : run_group_pairs<DIR, bf16_t, bf16_t>(a, few, s);
 }
 
-// weight gradient (upd = 0), or the update y -= upd / pairs * gradient
+// weight gradient (lr = 0), or the update y -= lr / pairs * gradient
 pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t outputs, int32_t type, const void* dy, int64_t dy_ld,
                              const void* x, int64_t x_ld, int xdiv, float* dw, int64_t dw_net, int64_t dw_ld, float* db,
-                             int64_t db_net, float upd, bf16_t* shadow, void* ws, hipStream_t s) {
+                             int64_t db_net, float lr, bf16_t* shadow, void* ws, hipStream_t s) {
     GroupGemm a = group_base(g, false);
     const int S = group_splits((int64_t)g->n * g->per_row, g->networks, inputs, outputs);
     a.M = inputs; a.N = outputs;
@@ -150,7 +150,7 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
     } else {
         a.y = dw; a.ldy = dw_ld; a.ynet = dw_net;
         a.db = db; a.dbnet = db_net;
-        a.upd = upd; a.shadow = shadow;
+        a.lr = lr; a.shadow = shadow;
     }
     a.vec = store4_ok(a.y, a.ldy, a.ynet, PNN_FP32);
     const int64_t blocks = (int64_t)S * g->networks * ((inputs + 127) / 128) * ((outputs + 127) / 128);
@@ -159,7 +159,7 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
     else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks, 256, 0, s>>>(a);
     TRY(launched("grouped weight gradient"));
     if (S > 1) {
-        GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, upd, shadow};
+        GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, lr, shadow};
         const int64_t all = (int64_t)g->networks * outputs * (inputs + 1);
         group_join_kernel<<<(unsigned)std::min<int64_t>((all + 255) / 256, 8192), 256, 0, s>>>(j);
         TRY(launched("sum of a grouped weight gradient"));

@@ -101,6 +101,9 @@ struct pnn_net {
     int32_t* ord_y = nullptr;
     int64_t ord_rows = 0;
 
+    char* routed_ws = nullptr;    // rows that name their CNs: grouping, activations, errors
+    size_t routed_bytes = 0;
+
     // chunked per-sample plan
     bool psgd = false;
     int T = 0, ksplit = 1, kchunk = 0;
@@ -1079,7 +1082,7 @@ void free_all(pnn_net* n) {
     auto f = [](void* p) { if (p) (void)hipFree(p); };
     f(n->theta); f(n->merged); f(n->shadow); f(n->mshadow);
     for (int l = 0; l < 9; ++l) { f(n->act_ws[l]); f(n->del_ws[l]); f(n->inf_ws[l]); }
-    f(n->d_correct); f(n->d_cost); f(n->d_cost_sum); f(n->d_mw); f(n->ord_x); f(n->ord_y); f(n->ppart); f(n->d1); f(n->gram); f(n->flags); f(n->qbuf); f(n->gramx); f(n->zpart); f(n->fx3_zpart); f(n->fx3_dout);
+    f(n->d_correct); f(n->d_cost); f(n->d_cost_sum); f(n->d_mw); f(n->ord_x); f(n->ord_y); f(n->ppart); f(n->d1); f(n->gram); f(n->flags); f(n->qbuf); f(n->gramx); f(n->zpart); f(n->fx3_zpart); f(n->fx3_dout); f(n->routed_ws);
     for (void* p : n->retired) f(p);
     if (n->abort_ev) (void)hipEventDestroy(n->abort_ev);
     for (auto& r : n->pending) { (void)hipEventDestroy(r.a); (void)hipEventDestroy(r.b); }
@@ -1796,3 +1799,4 @@ void pnn_destroy(pnn_net* n) {
 
 #include "groups_host.hpp"
 #include "distill_host.hpp"
+#include "routed_host.hpp"

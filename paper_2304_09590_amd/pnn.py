@@ -125,6 +125,10 @@ def lib() -> ctypes.CDLL:
         L.pnn_distill_grad.argtypes = [distill, vp, vp, i64, vp, i64, vp]
         for name in ("pnn_distill_bytes", "pnn_distill_loss", "pnn_distill_grad"):
             getattr(L, name).restype = i32
+        L.pnn_infer_routed.argtypes = [vp, vp, i64, vp, i32, vp, vp, vp, vp]
+        L.pnn_infer_routed.restype = i32
+        L.pnn_train_routed.argtypes = [vp, vp, i64, vp, i32, vp, vp, i32, vp, ctypes.c_float, ctypes.c_float, vp, vp]
+        L.pnn_train_routed.restype = i32
         _lib = L
     return _lib
 
@@ -262,6 +266,32 @@ class PNN:
         assert th.size == self.P
         self._check(self._lib.pnn_set_params(self.h, which, th.ctypes.data_as(ctypes.POINTER(ctypes.c_float))),
                     "pnn_set_params")
+
+    def infer_routed(self, x, ids, pred, weights=None, out=None, stream=None) -> None:
+        """Answers of the CNs that each row names (ids int32 [rows, per_row]), combined by weights (None: the mean)."""
+        rows, per_row = ids.shape
+        self._shapes((x, (rows, self.cfg.sizes[0])), (pred, (rows,)), (weights, (rows, per_row)),
+                     (out, (rows, self.cfg.sizes[self.cfg.n_layers])))
+        self._check(self._lib.pnn_infer_routed(self.h, _dev_ptr(x, "torch.float32"), rows, _dev_ptr(ids, "torch.int32"), per_row,
+                                               _dev_ptr(weights, "torch.float32"), _dev_ptr(pred, "torch.int32"),
+                                               _dev_ptr(out, "torch.float32"), _stream_handle(stream)), "pnn_infer_routed")
+
+    def train_routed(self, x, ids, idx=None, t=None, y=None, temperature: float = 1.0, alpha: float = 0.0, loss=None,
+                     stream=None) -> None:
+        """One mini-batch step of every CN on the rows that name it, towards a teacher's top logits (idx, t) and labels."""
+        rows, per_row = ids.shape
+        top = idx.shape[1] if idx is not None else 0
+        self._shapes((x, (rows, self.cfg.sizes[0])), (idx, (rows, top)), (t, (rows, top)), (y, (rows,)), (loss, (rows, per_row)))
+        self._check(self._lib.pnn_train_routed(self.h, _dev_ptr(x, "torch.float32"), rows, _dev_ptr(ids, "torch.int32"), per_row,
+                                               _dev_ptr(idx, "torch.int32"), _dev_ptr(t, "torch.float32"), top,
+                                               _dev_ptr(y, "torch.int32"), temperature, alpha, _dev_ptr(loss, "torch.float32"),
+                                               _stream_handle(stream)), "pnn_train_routed")
+
+    @staticmethod
+    def _shapes(*given) -> None:
+        for t, shape in given:
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"a tensor of shape {tuple(t.shape)}, expected {shape}")
 
     def profile(self, enable: bool) -> None:
         self._check(self._lib.pnn_profile(self.h, 1 if enable else 0), "pnn_profile")
