@@ -158,38 +158,13 @@ __device__ inline int dl_has(const DistillArgs& d, int64_t row, const Teacher& t
     return (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
 }
 
+// eight values, those from the nv-th on `fill`
 template <typename T>
 __device__ inline void dl_load8(float (&v)[8], const T* p, int nv, float fill) {
-    Raw8<T> r;
-    load8(r, p, nv);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 4) v[i] = r.v[i >> 2][i & 3];
-        else v[i] = i & 1 ? bf_hi(r.v[i >> 1]) : bf_lo(r.v[i >> 1]);
-    }
+    load8_f<T>(v, p, nv);
     if (nv < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < nv ? v[i] : fill;
-    }
-}
-
-__device__ inline void store8(float* p, const float (&v)[8], int nv) {
-    if (nv >= 8) {
-        *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
-        *(f4_a4*)(p + 4) = f4{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < nv) p[i] = v[i];
-    }
-}
-__device__ inline void store8(bf16_t* p, const float (&v)[8], int nv) {
-    if (nv >= 8) {
-        *(u4v_a2*)p = u4v{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < nv) p[i] = f2bf(v[i]);
     }
 }
 

@@ -178,6 +178,18 @@ __host__ inline size_t group_lds(int K) { return sizeof(int) * ((size_t)GR_WAVES
 // ------------------------------------------------------------------------------------
 // products
 
+// pair / per_row by a product: exact for pairs below 2^30 (l = ceil(log2 d), m = ceil(2^(30 + l) / d))
+struct Div {
+    uint32_t m;
+    int s;
+    __device__ inline uint32_t of(int pair) const { return (uint32_t)(((uint64_t)(uint32_t)pair * m) >> s); }
+};
+__host__ inline Div div_by(int d) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    return {(uint32_t)(((1ull << (30 + l)) + (uint64_t)d - 1) / (uint64_t)d), 30 + l};
+}
+
 enum { GR_FWD = 0, GR_DX = 1, GR_DW = 2 };
 
 // m is the result's contiguous extent (outputs of a forward product, inputs of both gradients), n
@@ -191,10 +203,10 @@ struct GroupGemm {
                                // and k of a weight gradient the group's pairs
     const void* p;             // rows of pairs: x (forward), dy (gradients); row (pair / pdiv)
     int64_t ldp;
-    int pdiv;
+    Div pdiv;
     const void* w;             // weights; x of a weight gradient, row (pair / wdiv)
     int64_t wnet, ldw;
-    int wdiv;
+    Div wdiv;
     const float* b;            // bias (nullable)
     int64_t bnet;
     int act;                   // activation (forward), or the one whose slope at a scales the result; -1 none
@@ -202,7 +214,6 @@ struct GroupGemm {
     int64_t lda;
     void* y;                   // result; fp32 gradients of a weight gradient
     int64_t ldy, ynet;
-    int vec;                   // the result's rows may be stored four values at a time
     float* db;                 // (weight gradient) bias gradient, nullable
     int64_t dbnet;
     int splits;                // (weight gradient) parts of a group, summed by group_join_kernel
@@ -256,14 +267,35 @@ __device__ inline void load8(Raw8<float>& r, const float* p, int nv) {
     }
 }
 
-template <typename TO>
-__device__ inline void store_row4(TO* p, const float (&v)[4], int nv, bool vec) {
-    if (vec && nv >= 4) {
-        store4<TO>(p, make_float4(v[0], v[1], v[2], v[3]));
+template <typename T>
+__device__ inline void load8_f(float (&v)[8], const T* p, int nv) {
+    Raw8<T> r;
+    load8(r, p, nv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = r.v[i >> 2][i & 3];
+        else v[i] = i & 1 ? bf_hi(r.v[i >> 1]) : bf_lo(r.v[i >> 1]);
+    }
+}
+
+// the first nv of eight values
+__device__ inline void store8(float* p, const float (&v)[8], int nv) {
+    if (nv >= 8) {
+        *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
+        *(f4_a4*)(p + 4) = f4{v[4], v[5], v[6], v[7]};
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (r < nv) p[r] = from_f<TO>(v[r]);
+        for (int i = 0; i < 7; ++i)
+            if (i < nv) p[i] = v[i];
+    }
+}
+__device__ inline void store8(bf16_t* p, const float (&v)[8], int nv) {
+    if (nv >= 8) {
+        *(u4v_a2*)p = u4v{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < nv) p[i] = f2bf(v[i]);
     }
 }
 
@@ -318,6 +350,102 @@ __device__ inline void gt_store(bf16_t* lds, int plane, const Raw8<float>& r) {
     *(u4v*)(lds + 2 * plane) = u4v{l[0], l[1], l[2], l[3]};
 }
 
+// activations / slopes of eight neighbouring values (the choice outside the loops: one copy of each)
+__device__ inline void group_act8(int act, float (&v)[8]) {
+    switch (act) {
+    case ACT_SIGMOID:
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = group_act(ACT_SIGMOID, v[r]);
+        break;
+    case ACT_TANH:
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = group_act(ACT_TANH, v[r]);
+        break;
+    case ACT_RELU:
+    case ACT_LEAKY: {
+        const float low = act == ACT_RELU ? 0.0f : 0.01f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = v[r] < 0.0f ? (act == ACT_RELU ? -0.0f : low * v[r]) : v[r] + 0.0f;
+        break;
+    }
+    default: break;
+    }
+}
+__device__ inline void group_slope8(int act, float (&v)[8], const float (&a)[8]) {
+    if (act == ACT_SIGMOID || act == ACT_TANH) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] *= act == ACT_TANH ? 1.0f - a[r] * a[r] : a[r] * (1.0f - a[r]);
+    } else if (act == ACT_RELU || act == ACT_LEAKY) {
+        const float low = act == ACT_RELU ? 0.0f : 0.01f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] *= signbit(a[r]) ? low : 1.0f;
+    }
+}
+
+// The results of a wave: a lane holds m0 + wm + 16 i + 4 kg + r of column n = wn + 16 j + l15.  Sixteen
+// columns at a time go through the wave's own part of LDS (`turn`, no longer used by anyone), from where
+// a lane takes eight neighbouring results of one column: rows leave in stores of 16 or 32 bytes a lane.
+template <int MI> constexpr int group_turn() { return 16 * (16 * MI + 4); }  // floats of a wave
+template <int DIR, typename T, typename TO, int MI, int NJ>
+__device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], const f4 (&accb)[NJ], int e, int split, int p0, int m0,
+                                   int n0, int nv, int wm, int wn, int lane, bool bias_rows, float* turn) {
+    constexpr int LD = 16 * MI + 4, PER = 2 * MI, COLS = 64 / PER;  // lanes of a column, columns at a time
+    const int l15 = lane & 15, kg = lane >> 4, part = lane % PER * 8, m = m0 + wm + part, left = g.M - m;
+    const int pairs = DIR == GR_DW ? g.off[e + 1] - g.off[e] : 0;
+    const float scale = DIR == GR_DW && g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
+    if (DIR == GR_DW && g.lr != 0.0f && pairs == 0) return;  // no update
+    float bias[8];
+    if (DIR == GR_FWD) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) bias[r] = g.b && r < left && e < g.K ? g.b[e * g.bnet + m + r] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int c = 0; c < 16; c += COLS) {
+            const int col = c + lane / PER, n = wn + 16 * j + col;
+            if (n >= nv || left <= 0) continue;
+            const f4 lo = *(const f4*)(turn + col * LD + part), hi = *(const f4*)(turn + col * LD + part + 4);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (DIR == GR_DW) {
+                const int64_t at = (int64_t)(n0 + n) * g.ldy + m;
+                float* y = (float*)g.y + ((int64_t)split * g.K + e) * g.ynet + at;
+                if (g.lr != 0.0f) {
+                    Raw8<float> old;
+                    load8(old, y, left);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) v[r] = old.v[r >> 2][r & 3] - scale * v[r];
+                    if (g.shadow) store8(g.shadow + e * g.ynet + at, v, left);
+                }
+                store8(y, v, left);
+                continue;
+            }
+            const int64_t pair = g.pairs[p0 + n];
+            if (e == g.K) {  // dropped
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = 0.0f;
+            } else if (DIR == GR_FWD) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] += bias[r];
+                group_act8(g.act, v);
+            } else if (g.a) {
+                float a[8];
+                load8_f<T>(a, (const T*)g.a + pair * g.lda + m, left);
+                group_slope8(g.act, v, a);
+            }
+            store8((TO*)g.y + pair * g.ldy + m, v, left);
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (bias_rows && kg == 0 && wn + 16 * j + l15 < nv) {
+            float* db = g.db + ((int64_t)split * g.K + e) * g.dbnet + n0 + wn + 16 * j + l15;
+            *db = g.lr != 0.0f ? *db - scale * accb[j][0] : accb[j][0];
+        }
+    }
+}
+
 // 128 x 128 tiles of one network's product, four waves of 64 x 64.
 template <int DIR, typename T, typename TO>
 __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
@@ -328,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     constexpr int U = TA::ELEMS / 8 / 256;
     __shared__ __align__(16) bf16_t lds[2 * PL * TA::ELEMS];
     bf16_t *la = lds, *lb = lds + PL * TA::ELEMS;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l15 = lane & 15, kg = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mt = (g.M + 127) / 128;
     const int64_t id = group_xcd(blockIdx.x, gridDim.x);
     int e, m0, n0 = 0, nv, split = 0, p0, Kx;
@@ -378,7 +506,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         }
         if (DIR != GR_DW) {
             const int r = TB::row(s);
-            pb[u] = r < nv && Kx > 0 ? (const T*)g.p + (int64_t)(g.pairs[p0 + r] / g.pdiv) * g.ldp + TB::chunk(s) * 8 : nullptr;
+            pb[u] = r < nv && Kx > 0 ? (const T*)g.p + (int64_t)(g.pdiv.of(g.pairs[p0 + r])) * g.ldp + TB::chunk(s) * 8 : nullptr;
         }
     }
     Raw8<T> ra[U], rb[U];
@@ -397,7 +525,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             } else {
                 const int r = TA::row(s), c = TA::chunk(s) * 8;
                 const int pair = k0 + r < Kx ? g.pairs[p0 + k0 + r] : 0;
-                load8(ra[u], (const T*)g.w + (int64_t)(pair / g.wdiv) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
+                load8(ra[u], (const T*)g.w + (int64_t)g.wdiv.of(pair) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
                 load8(rb[u], (const T*)g.p + (int64_t)pair * g.ldp + n0 + c, k0 + r < Kx ? nv - c : 0);
             }
         }
@@ -448,59 +576,222 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             }
         }
     }
-    // a lane holds results m0 + wm + 16 i + 4 kg + r of column n = wn + 16 j + l15
+    __syncthreads();
+    group_store<DIR, T, TO, 4, 4>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
+                                  (float*)lds + wave * group_turn<4>());
+}
+
+// ------------------------------------------------------------------------------------
+// bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, four waves of BM / 2 x BN / 2,
+// a ring of stages of 32 k in LDS that global memory fills directly.
+
+static __device__ __align__(64) uint32_t group_zeros[16];  // what lies outside an operand
+
+// BYTES a lane from global memory to lds + BYTES lane.  In asm: the compiler, which cannot tell the ring's
+// stages apart, waits for all copies in flight before a transposing read of LDS.  No register is written
+// but m0, which nothing else in these kernels uses (and the compiler never allocates).
+template <int BYTES>
+__device__ inline void copy_to_lds(const void* src, uint32_t lds) {
+    if (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory");
+}
+// waits until at most N of the wave's copies are in flight, and for all other waves to have done so
+template <int N>
+__device__ inline void ring_wait() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// An operand's stage: T values wide, 32 k deep; KC and NC as in GTile.
+template <bool KC, int T>
+struct RTile {
+    static constexpr int ELEMS = T * 32, CHUNKS = ELEMS / 8;
+    static __device__ inline int row(int s) { return KC ? s >> 2 : s / (T / 8); }  // (NC: the k)
+    static __device__ inline int key(int r) { return KC ? ((r >> 1) & 3) ^ ((r >> 3) & 1) : (r & 3) | ((r >> 1) & 4); }
+    // the chunk of the row that belongs at place s
+    static __device__ inline int chunk(int s) {
+        const int r = row(s), c = KC ? s & 3 : s % (T / 8);
+        return KC ? c ^ key(r) : ((c >> 1) ^ key(r)) << 1 | (c & 1);
+    }
+    static __device__ inline bf8v frag(const bf16_t* lds, int t0, int lane) {
+        const int l15 = lane & 15, kg = lane >> 4;
+        if (KC) {
+            const int r = t0 + l15;
+            return *(const bf8v*)(lds + r * 32 + ((kg ^ key(r)) << 3));
+        }
+        const int r = 8 * kg + (l15 >> 2);
+        const bf16_t* q = lds + r * T + (((t0 >> 4) ^ key(r)) << 4) + (l15 & 3) * 4;
+        const s4v both[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)q),
+                             __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(q + 4 * T))};
+        return __builtin_bit_cast(bf8v, both);
+    }
+};
+
+template <int DIR, typename TO, int BM, int BN, int NST>
+__global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
+    typedef RTile<DIR == GR_FWD, BM> TA;
+    typedef RTile<DIR != GR_DW, BN> TB;
+    constexpr int UA = TA::CHUNKS / 256, UB = TB::CHUNKS / 256, STAGE = TA::ELEMS + TB::ELEMS;
+    constexpr int MI = BM / 32, NJ = BN / 32;  // 16 x 16 blocks of a wave
+    extern __shared__ __align__(16) bf16_t ring[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int mt = (g.M + BM - 1) / BM;
+    const int64_t id = group_xcd(blockIdx.x, gridDim.x);
+    int e, m0, n0 = 0, nv, split = 0, p0, Kx;
     if (DIR == GR_DW) {
-        const int pairs = g.off[e + 1] - g.off[e];
-        const float scale = g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
+        const int nt = (g.N + BN - 1) / BN;
+        m0 = (int)(id % mt) * BM;
+        n0 = (int)(id / mt % nt) * BN;
+        e = (int)(id / mt / nt % g.K);
+        split = (int)(id / mt / nt / g.K);
+        nv = g.N - n0 < BN ? g.N - n0 : BN;
+        const int first = g.off[e], all = g.off[e + 1] - first;
+        const int part = (all + g.splits * 32 - 1) / (g.splits * 32) * 32;
+        p0 = first + (split * part < all ? split * part : all);
+        Kx = first + all - p0 < part ? first + all - p0 : part;
+    } else {
+        const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
+        const int64_t left = g.n_tiles - grp * 8, wide = left < 8 ? left : 8;
+        const int2 t = g.tiles[grp * 8 + in % wide];
+        m0 = (int)(in / wide) * BM;
+        e = t.x;
+        if (e < 0) return;
+        p0 = t.y;
+        const int end = e < g.K ? g.off[e + 1] : g.N;
+        nv = end - p0 < BN ? end - p0 : BN;
+        Kx = e < g.K ? g.Kx : 0;
+    }
+    const int mv = g.M - m0 < BM ? g.M - m0 : BM;
+    const bf16_t* zeros = (const bf16_t*)group_zeros;
+    f4 acc[MI][NJ], accb[NJ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = wn + 16 * j + l15;
-            if (n >= nv) continue;
-            float* y = (float*)g.y + ((int64_t)split * g.K + e) * g.ynet + (int64_t)(n0 + n) * g.ldy;
-            if (g.lr != 0.0f && pairs == 0) continue;
+    for (int j = 0; j < NJ; ++j) {
+        accb[j] = f4{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int m = m0 + wm + 16 * i + 4 * kg, left = g.M - m;
-                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                if (g.lr != 0.0f)
-                    for (int r = 0; r < 4; ++r)
-                        if (r < left) {
-                            v[r] = y[m + r] - scale * v[r];
-                            if (g.shadow) g.shadow[e * g.ynet + (int64_t)(n0 + n) * g.ldy + m + r] = f2bf(v[r]);
-                        }
-                store_row4<float>(y + m, v, left, g.vec);
-            }
-            if (bias_rows && kg == 0) {
-                float* db = g.db + ((int64_t)split * g.K + e) * g.dbnet + n0 + n;
-                *db = g.lr != 0.0f ? *db - scale * accb[j][0] : accb[j][0];
-            }
-        }
-        return;
+        for (int i = 0; i < MI; ++i) acc[i][j] = f4{0, 0, 0, 0};
+    }
+    const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
+    const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
+
+    // Addresses of this thread's chunks (of the weight gradient's rows: what does not depend on k).  Rows and
+    // columns outside the tile repeat the last one inside: they reach only results that are not stored.
+    const bf16_t *pa[UA], *pb[UB];
+    int ka[UA], kb[UB];  // KC: k of the chunk in its stage; NC: the row's k
+#pragma unroll
+    for (int u = 0; u < UA; ++u) {
+        const int s = u * 256 + tid, r = TA::row(s), c = TA::chunk(s) * 8;
+        ka[u] = DIR == GR_FWD ? c : r;
+        const int rm = r < mv ? r : mv - 1, cm = c < mv ? c : mv - 8;
+        pa[u] = (const bf16_t*)g.w + (DIR == GR_DW ? 0 : e * g.wnet) +
+                (DIR == GR_FWD ? (int64_t)(m0 + rm) * g.ldw + c : DIR == GR_DX ? (int64_t)r * g.ldw + m0 + cm : (int64_t)(m0 + cm));
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = wn + 16 * j + l15;
-        if (n >= nv) continue;
-        const int64_t pair = g.pairs[p0 + n];
-        TO* y = (TO*)g.y + pair * g.ldy;
+    for (int u = 0; u < UB; ++u) {
+        const int s = u * 256 + tid, r = TB::row(s), c = TB::chunk(s) * 8;
+        kb[u] = DIR != GR_DW ? c : r;
+        pb[u] = (const bf16_t*)g.p;
+        if (DIR == GR_DW) pb[u] += n0 + (c < nv ? c : nv - 8);
+        else if (Kx > 0) pb[u] += (int64_t)g.pdiv.of(g.pairs[p0 + (r < nv ? r : nv - 1)]) * g.ldp + c;
+    }
+    const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(lds_void*)ring);
+    constexpr int IST = 2 * (NST - 1);  // stages of a wave's own ring of pair numbers (weight gradient)
+    const int* numbers = (const int*)(ring + NST * STAGE) + wave * IST * 64;
+    const uint32_t numbers_at = base + NST * STAGE * 2 + wave * IST * 256;
+    // copies the numbers of the pairs k0 .. k0 + 31 (and more, not used)
+    auto number = [&](int stage, int k0) {
+        const int k = k0 + lane < Kx ? k0 + lane : Kx - 1;
+        copy_to_lds<4>(g.pairs + p0 + k, numbers_at + stage * 256);
+    };
+    const int64_t step_a = DIR == GR_FWD ? 32 : 32 * g.ldw;
+    // fills a stage with k0 .. k0 + 31 (zeros behind the last k); stages are filled in their order
+    auto fill_as = [&](auto whole, int stage, int k0, int istage) {
+        const uint32_t to = base + stage * (STAGE * 2) + wave * 1024;
+        int na[UA], nb[UB];
+        if (DIR == GR_DW) {  // (the numbers of pairs behind the last are the last one's)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = m0 + wm + 16 * i + 4 * kg, left = g.M - m;
-            float v[4];
+            for (int u = 0; u < UA; ++u) na[u] = numbers[istage * 64 + ka[u]];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                v[r] = acc[i][j][r];
-                if (r >= left || e == g.K) continue;
-                if (DIR == GR_FWD) {
-                    if (g.b) v[r] += g.b[e * g.bnet + m + r];
-                    v[r] = group_act(g.act, v[r]);
-                } else if (g.a) {
-                    v[r] *= act_deriv(g.act, to_f<T>(((const T*)g.a)[pair * g.lda + m + r]));
-                }
-            }
-            store_row4<TO>(y + m, v, left, g.vec);
+            for (int u = 0; u < UB; ++u) nb[u] = numbers[istage * 64 + kb[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < UA; ++u) {
+            const bf16_t* q = pa[u];
+            if (DIR == GR_DW) q += (uint64_t)g.wdiv.of(na[u]) * (uint32_t)g.ldw;
+            else pa[u] += step_a;
+            if (!whole && k0 + ka[u] >= Kx) q = zeros;
+            copy_to_lds<16>(q, to + u * 4096);
+        }
+#pragma unroll
+        for (int u = 0; u < UB; ++u) {
+            const bf16_t* q = pb[u];
+            if (DIR == GR_DW) q += (uint64_t)(uint32_t)nb[u] * (uint32_t)g.ldp;
+            else pb[u] += 32;
+            if (!whole && k0 + kb[u] >= Kx) q = zeros;
+            copy_to_lds<16>(q, to + TA::ELEMS * 2 + u * 4096);
+        }
+    };
+    auto fill = [&](int stage, int k0, int istage) {
+        if (k0 + 32 <= Kx) fill_as(std::true_type{}, stage, k0, istage);
+        else fill_as(std::false_type{}, stage, k0, istage);
+    };
+    constexpr int COPIES = UA + UB + (DIR == GR_DW ? 1 : 0);  // of a wave and stage
+    const int steps = (Kx + 31) / 32;
+    int at = 0, nat = NST - 1;  // the stage that is read, that of the numbers of the stage that is filled
+    if (Kx > 0) {
+        if (DIR == GR_DW) {
+#pragma unroll
+            for (int t = 0; t < IST; ++t) number(t, t * 32);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+#pragma unroll
+        for (int t = 0; t < NST - 1; ++t) fill(t, t * 32, t);  // (what lies behind the last k is filled with zeros)
+        if (DIR == GR_DW) {  // (as many copies in flight as in the loop)
+#pragma unroll
+            for (int t = 0; t < NST - 1; ++t) number(t, (IST + t) * 32);
         }
     }
+    for (int t = 0; t < steps; ++t) {
+        ring_wait<(NST - 2) * COPIES>();
+        const int next = at == 0 ? NST - 1 : at - 1;
+        fill(next, (t + NST - 1) * 32, nat);
+        if (DIR == GR_DW) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the numbers are read: their place is free)
+            number(nat, (t + NST - 1 + IST) * 32);
+            nat = nat == IST - 1 ? 0 : nat + 1;
+        }
+        const bf16_t *la = ring + at * STAGE, *lb = la + TA::ELEMS;
+        bf8v fa[MI], fb[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[j] = TB::frag(lb, wn + 16 * j, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[i] = TA::frag(la, wm + 16 * i, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        // reads two operands ahead of the products that take them
+        constexpr int RA = DIR == GR_FWD ? 1 : 2, RB = DIR == GR_DW ? 2 : 1;
+        __builtin_amdgcn_sched_group_barrier(0x100, RB * NJ + 2 * RA, 0);
+#pragma unroll
+        for (int i = 0; i < MI - 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * NJ, 0);
+        if (bias_rows) {  // sums over k: a product with ones
+            const uint32_t two = 0x3f803f80;
+            const u4v ones4 = {two, two, two, two};
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, ones4), fb[j], accb[j], 0, 0, 0);
+        }
+        at = at == NST - 1 ? 0 : at + 1;
+    }
+    ring_wait<0>();  // (no copy outlives its workgroup)
+    group_store<DIR, bf16_t, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
+                                         (float*)ring + wave * group_turn<MI>());
 }
 
 // the sum of a weight gradient's parts, in their order; with lr the update
@@ -577,7 +868,7 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
     if (e < g.K) {
         const int share = (g.Kx + 4 * STEP - 1) / (4 * STEP) * STEP;
         const int k1 = (wave + 1) * share < g.Kx ? (wave + 1) * share : g.Kx;
-        const T* x = l15 < nv ? (const T*)g.p + (int64_t)(g.pairs[p0 + l15] / g.pdiv) * g.ldp : nullptr;
+        const T* x = l15 < nv ? (const T*)g.p + (int64_t)(g.pdiv.of(g.pairs[p0 + l15])) * g.ldp : nullptr;
         const T* w[GS_OUT / 16];
 #pragma unroll
         for (int i = 0; i < GS_OUT / 16; ++i)
@@ -649,7 +940,7 @@ __global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
     if (e < g.K) {
         const int share = (g.Kx + 4 * STEP - 1) / (4 * STEP) * STEP;
         const int k1 = (wave + 1) * share < g.Kx ? (wave + 1) * share : g.Kx;
-        const T* d = l15 < nv ? (const T*)g.p + (int64_t)(g.pairs[p0 + l15] / g.pdiv) * g.ldp : nullptr;
+        const T* d = l15 < nv ? (const T*)g.p + (int64_t)(g.pdiv.of(g.pairs[p0 + l15])) * g.ldp : nullptr;
         const int cols = g.M - m0 - C * l15;
         const T* w = (const T*)g.w + e * g.wnet + m0 + C * l15;
         for (int kk = wave * share; kk < k1; kk += STEP) {

@@ -87,7 +87,7 @@ GroupGemm group_base(const pnn_groups* g, bool few) {
     a.n_tiles = few ? p.n_small : p.n_large;
     a.K = g->networks;
     a.N = (int)p.P;
-    a.pdiv = a.wdiv = 1;
+    a.pdiv = a.wdiv = div_by(1);
     a.act = -1;
     a.splits = 1;
     return a;
@@ -95,11 +95,6 @@ GroupGemm group_base(const pnn_groups* g, bool few) {
 
 // Tiles of 16 pairs re-read the weights for each of them, tiles of 128 multiply what is not there.
 bool few_pairs(const pnn_groups* g) { return g->n * g->per_row <= 24 * (int64_t)g->networks; }
-
-bool store4_ok(const void* p, int64_t ld, int64_t net, int32_t type) {
-    const int64_t a = 4 * (int64_t)type_size(type);
-    return (uintptr_t)p % a == 0 && ld % 4 == 0 && net % 4 == 0;
-}
 
 // parts of a group's pairs in a weight gradient: with fewer workgroups than two per CU the groups
 // are split until there are as many, as long as a part keeps 512 pairs in the mean
@@ -115,11 +110,29 @@ pnn_status grid_fits(int64_t blocks) {
     return PNN_OK;
 }
 
+// the ring kernels' copies: 16 bytes each, whole inside a row
+bool ring_ok(const void* p, int64_t ld, int64_t net, int width) {
+    return aligned16(p) && ld % 8 == 0 && ld < (int64_t(1) << 31) && net % 8 == 0 && width % 8 == 0;
+}
+
+template <int DIR, typename TO>
+void launch_ring(const GroupGemm& a, int64_t others, hipStream_t s) {
+    constexpr int BM = 256, BN = 128, NST = 3;
+    const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? 4 * 2 * (NST - 1) * 256 : 0);
+    (void)hipFuncSetAttribute((const void*)group_ring_kernel<DIR, TO, BM, BN, NST>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    group_ring_kernel<DIR, TO, BM, BN, NST><<<(unsigned)((a.M + BM - 1) / BM * others), 256, lds, s>>>(a);
+}
+
 template <int DIR, typename T, typename TO>
 pnn_status run_group_pairs(const GroupGemm& a, bool few, hipStream_t s) {
     const int band = !few ? 128 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128;
     const int64_t blocks = (a.M + band - 1) / band * a.n_tiles;
     TRY(grid_fits(blocks));
+    if constexpr (sizeof(T) == 2)
+        if (!few && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx)) {
+            launch_ring<DIR, TO>(a, a.n_tiles, s);
+            return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
+        }
     if (!few) group_tile_kernel<DIR, T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
     else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
     else group_few_dx_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
@@ -141,7 +154,7 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
     const int S = group_splits((int64_t)g->n * g->per_row, g->networks, inputs, outputs);
     a.M = inputs; a.N = outputs;
     a.p = dy; a.ldp = dy_ld;
-    a.w = x; a.ldw = x_ld; a.wdiv = xdiv;
+    a.w = x; a.ldw = x_ld; a.wdiv = div_by(xdiv);
     a.splits = S;
     float* dbpart = (float*)ws + (int64_t)S * g->networks * inputs * outputs;
     if (S > 1) {
@@ -152,10 +165,11 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
         a.db = db; a.dbnet = db_net;
         a.lr = lr; a.shadow = shadow;
     }
-    a.vec = store4_ok(a.y, a.ldy, a.ynet, PNN_FP32);
     const int64_t blocks = (int64_t)S * g->networks * ((inputs + 127) / 128) * ((outputs + 127) / 128);
     TRY(grid_fits(blocks));
     if (type == PNN_FP32) group_tile_kernel<GR_DW, float, float><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else if (ring_ok(a.w, a.ldw, 0, a.M) && ring_ok(a.p, a.ldp, 0, a.N))
+        launch_ring<GR_DW, float>(a, (int64_t)S * g->networks * ((outputs + 127) / 128), s);
     else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks, 256, 0, s>>>(a);
     TRY(launched("grouped weight gradient"));
     if (S > 1) {
@@ -228,12 +242,11 @@ pnn_status pnn_grouped_forward(const pnn_groups* groups, const pnn_group_layer* 
     const bool few = few_pairs(groups);
     GroupGemm a = group_base(groups, few);
     a.M = layer->outputs; a.Kx = layer->inputs;
-    a.p = x_dev; a.ldp = x_ld; a.pdiv = groups->per_row;
+    a.p = x_dev; a.ldp = x_ld; a.pdiv = div_by(groups->per_row);
     a.w = layer->w_dev; a.wnet = layer->w_net; a.ldw = layer->w_ld;
     a.b = layer->b_dev; a.bnet = layer->b_net;
     a.act = act;
     a.y = y_dev; a.ldy = y_ld;
-    a.vec = store4_ok(y_dev, y_ld, 0, y_type);
     return run_group_pairs<GR_FWD>(a, layer->type, y_type, few, s);
 }
 
@@ -268,11 +281,9 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     if (!sum) {
         a.a = act >= 0 ? a_dev : nullptr; a.lda = a_ld; a.act = act;
         a.y = dx_dev; a.ldy = dx_ld;
-        a.vec = store4_ok(dx_dev, dx_ld, 0, dx_type);
-        return run_group_pairs<GR_DX>(a, layer->type, dx_type, few, s);
+            return run_group_pairs<GR_DX>(a, layer->type, dx_type, few, s);
     }
     a.y = ws_dev; a.ldy = layer->inputs;
-    a.vec = store4_ok(ws_dev, layer->inputs, 0, PNN_FP32);
     TRY(run_group_pairs<GR_DX>(a, layer->type, PNN_FP32, few, s));
     const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * layer->inputs + 255) / 256, 8192);
     const float* part = (const float*)ws_dev;

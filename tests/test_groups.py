@@ -233,7 +233,8 @@ SHAPES = [  # n, per_row, networks, inputs, outputs, kind, pad
     (1, 1, 1, 1, 1, "mixed", 0), (1, 2, 64, 784, 512, "mixed", 0), (3, 1, 2, 7, 5, "mixed", 0), (17, 1, 1, 33, 31, "mixed", 3),
     (50, 2, 7, 100, 131, "mixed", 1), (40, 1, 3, 8, 8, "none", 0), (24, 1, 1, 784, 16, "one", 0), (25, 1, 1, 784, 16, "one", 0),
     (300, 1, 5, 64, 128, "mixed", 0), (129, 3, 3, 129, 127, "mixed", 0), (1000, 1, 4, 200, 104, "few", 0),
-    (257, 1, 1, 65, 257, "one", 2), (2000, 2, 3, 96, 40, "mixed", 8), (3000, 1, 2, 20, 12, "mixed", 0)]
+    (257, 1, 1, 65, 257, "one", 2), (2000, 2, 3, 96, 40, "mixed", 8), (3000, 1, 2, 20, 12, "mixed", 0),
+    (700, 1, 2, 520, 264, "mixed", 0), (1500, 3, 4, 264, 776, "mixed", 0), (400, 1, 3, 512, 257, "mixed", 0)]
 
 
 @gpu
