@@ -42,19 +42,40 @@ struct DistillArgs {
 
 constexpr float DL_INF = __builtin_huge_valf();
 
-// running maximum and sums of exponentials; MODE 1: one sum (at the scale ct), 2: at ct and at cs
+// Running maximum m and sums of exp2(z c - m c), at the scales c = ct and cs.  MODE 1: one sum; 2: two; 3: two
+// whose second scale is twice the first (T = 2), so that its terms are the first's squares.  m c is rounded once
+// and the same wherever it is used (Ref), so its rounding shifts all terms alike and cancels.
 struct Sums { float m, a, b; };
+struct Ref {
+    float t, s;
+    bool huge;  // m c leaves fp32's range: differences are taken before they are scaled
+};
 
-__device__ inline float dl_ref(float m) { return m == -DL_INF ? 0.0f : m; }
+__device__ inline Ref dl_ref(float m, const DistillArgs& d) {
+    const float r = m == -DL_INF ? 0.0f : m;  // (no value yet, or only ones of -inf: their terms are 0)
+    Ref f = {r * d.ct, r * d.cs, false};
+    f.huge = !(__builtin_fabsf(f.t) < 1e38f && __builtin_fabsf(f.s) < 1e38f);
+    if (f.huge) f.t = f.s = r;
+    return f;
+}
+// exponents (to base 2) of a logit
+__device__ inline float dl_t(float z, const Ref& f, const DistillArgs& d) {
+    return f.huge ? (z - f.t) * d.ct : __builtin_fmaf(z, d.ct, -f.t);
+}
+__device__ inline float dl_s(float z, const Ref& f, const DistillArgs& d) {
+    return f.huge ? (z - f.s) * d.cs : __builtin_fmaf(z, d.cs, -f.s);
+}
 
+// moves the sums to a larger maximum
 template <int MODE>
-__device__ inline void dl_raise(Sums& s, float m, const DistillArgs& d) {
-    if (m > s.m) {
-        const float by = s.m - m;  // (-inf before the first value: the sums are 0, or NaN, and stay so)
-        s.a *= exp2f(by * d.ct);
-        if (MODE == 2) s.b *= exp2f(by * d.cs);
-        s.m = m;
-    }
+__device__ inline void dl_move(Sums& s, float m, const DistillArgs& d) {
+    const Ref f = dl_ref(m, d), old = dl_ref(s.m, d);
+    const bool none = s.m == -DL_INF;  // (the sums are 0, or NaN, and stay so)
+    const float by = f.huge || old.huge ? (s.m - m) * d.ct : old.t - f.t;
+    const float bs = f.huge || old.huge ? (s.m - m) * d.cs : old.s - f.s;
+    s.a *= none ? 0.0f : __builtin_amdgcn_exp2f(by);
+    if (MODE != 1) s.b *= none ? 0.0f : __builtin_amdgcn_exp2f(bs);
+    s.m = m;
 }
 
 template <int MODE, int N>
@@ -62,29 +83,40 @@ __device__ inline void dl_add(Sums& s, const float (&z)[N], const DistillArgs& d
     float m = z[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) m = fmaxf(m, z[i]);
-    dl_raise<MODE>(s, m, d);
-    const float ref = dl_ref(s.m);
+    if (m > s.m) dl_move<MODE>(s, m, d);
+    const Ref f = dl_ref(s.m, d);
+    if (f.huge) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s.a += __builtin_amdgcn_exp2f((z[i] - f.t) * d.ct);
+            if (MODE != 1) s.b += __builtin_amdgcn_exp2f((z[i] - f.s) * d.cs);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        s.a += __builtin_amdgcn_exp2f((z[i] - ref) * d.ct);
-        if (MODE == 2) s.b += __builtin_amdgcn_exp2f((z[i] - ref) * d.cs);
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], d.ct, -f.t));
+        s.a += e;
+        if (MODE == 2) s.b += __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], d.cs, -f.s));
+        if (MODE == 3) s.b = __builtin_fmaf(e, e, s.b);
     }
 }
 
 template <int MODE>
 __device__ inline void dl_join(Sums& s, float m, float a, float b, const DistillArgs& d) {
-    const float top = fmaxf(s.m, m), ref = dl_ref(top);
-    const float f = s.m - ref, h = m - ref;
-    s.a = s.a * __builtin_amdgcn_exp2f(f * d.ct) + a * __builtin_amdgcn_exp2f(h * d.ct);
-    if (MODE == 2) s.b = s.b * __builtin_amdgcn_exp2f(f * d.cs) + b * __builtin_amdgcn_exp2f(h * d.cs);
-    s.m = top;
+    Sums o = {m, a, b};
+    const float top = fmaxf(s.m, m);
+    if (top > s.m) dl_move<MODE>(s, top, d);
+    if (top > o.m) dl_move<MODE>(o, top, d);
+    s.a += o.a;
+    if (MODE != 1) s.b += o.b;
 }
 
 template <int MODE, int G>
 __device__ inline void dl_join_lanes(Sums& s, const DistillArgs& d) {
 #pragma unroll
     for (int o = G / 2; o > 0; o >>= 1) {
-        const float m = __shfl_xor(s.m, o), a = __shfl_xor(s.a, o), b = MODE == 2 ? __shfl_xor(s.b, o) : 0.0f;
+        const float m = __shfl_xor(s.m, o), a = __shfl_xor(s.a, o), b = MODE != 1 ? __shfl_xor(s.b, o) : 0.0f;
         dl_join<MODE>(s, m, a, b, d);
     }
 }
@@ -111,7 +143,8 @@ __device__ inline Teacher dl_teacher(const DistillArgs& d, int64_t row, int lane
     float m = -DL_INF;
     for (int j = lane; j < d.k; j += G)
         if ((unsigned)idx[j] < (unsigned)d.V) m = fmaxf(m, to_f<T>(t[j]));
-    const float ref = dl_ref(dl_max<G>(m));
+    m = dl_max<G>(m);
+    const float ref = m == -DL_INF ? 0.0f : m;
     float s = 0.0f;
     for (int j = lane; j < d.k; j += G)
         if ((unsigned)idx[j] < (unsigned)d.V) s += exp2f((to_f<T>(t[j]) - ref) * d.ct);
@@ -123,6 +156,8 @@ template <typename T, int G>
 __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, const Teacher& te, int has, const Sums& s, bool two) {
     const T* z = (const T*)d.z + row * d.ldz;
     const float la = logf(s.a), lb = two ? logf(s.b) : la;
+    constexpr float LN2 = 0.6931471806f;
+    const Ref f = dl_ref(s.m, d);
     float kl = 0.0f;
     if (has & 1) {
         const int32_t* idx = d.idx + row / d.rows_per * d.k;
@@ -133,7 +168,7 @@ __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, co
             if ((unsigned)i >= (unsigned)d.V) continue;
             const float e = to_f<T>(t[j]) - te.ref, p = exp2f(e * d.ct) * im;
             if (p == 0.0f) continue;  // an entry without weight, whatever the student gives it
-            kl += p * ((e * d.inv_t - lm) - ((to_f<T>(z[i]) - s.m) * d.inv_t - la));
+            kl += p * ((e * d.inv_t - lm) - (dl_t(to_f<T>(z[i]), f, d) * LN2 - la));
         }
     }
     kl = dl_sum<G>(kl);
@@ -141,7 +176,7 @@ __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, co
     float loss = 0.0f;
     if (s.a == 0.0f) has = 0;  // every logit is -inf: nothing to learn from
     if (has & 1) loss += d.wt * kl;
-    if (has & 2) loss += d.ws * (lb - (to_f<T>(z[d.y[row / d.rows_per]]) - s.m));
+    if (has & 2) loss += d.ws * (lb - dl_s(to_f<T>(z[d.y[row / d.rows_per]]), f, d) * LN2);
     d.loss[row] = loss;
     d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (two ? s.b : s.a), (float)has);
 }
@@ -158,22 +193,24 @@ __device__ inline int dl_has(const DistillArgs& d, int64_t row, const Teacher& t
     return (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
 }
 
-// eight values, those from the nv-th on `fill`
-template <typename T>
-__device__ inline void dl_load8(float (&v)[8], const T* p, int nv, float fill) {
-    load8_f<T>(v, p, nv);
-    if (nv < 8) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < nv ? v[i] : fill;
-    }
+// dz of one value
+__device__ inline float dl_grad(const DistillArgs& d, float z, const Ref& f, float ea, float eb, float gt, float gs, float g,
+                                float psum, bool label) {
+    const float q = __builtin_amdgcn_exp2f(dl_t(z, f, d)) * ea;
+    const float s = __builtin_amdgcn_exp2f(dl_s(z, f, d)) * eb;
+    return g * (gt * (q - psum) + gs * (s - (label ? 1.0f : 0.0f)));
 }
 
-// dz of one value
-__device__ inline float dl_grad(const DistillArgs& d, float z, const float4& st, float ea, float eb, float gt, float gs, float g,
-                                float psum, bool label) {
-    const float q = __builtin_amdgcn_exp2f((z - st.x) * d.ct) * ea;
-    const float s = __builtin_amdgcn_exp2f((z - st.x) * d.cs) * eb;
-    return g * (gt * (q - psum) + gs * (s - (label ? 1.0f : 0.0f)));
+// dz of values that are neither an entry's nor the label: ka, kb = g gt ea, g gs eb
+template <int MODE>
+__device__ inline void dl_grad8(const DistillArgs& d, float (&x)[8], const Ref& f, float ka, float kb) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float e = __builtin_amdgcn_exp2f(f.huge ? (x[i] - f.t) * d.ct : __builtin_fmaf(x[i], d.ct, -f.t));
+        if (MODE == 1) x[i] = e * (ka + kb);
+        if (MODE == 2) x[i] = __builtin_fmaf(kb, __builtin_amdgcn_exp2f(dl_s(x[i], f, d)), ka * e);
+        if (MODE == 3) x[i] = e * __builtin_fmaf(kb, e, ka);
+    }
 }
 
 // Loss, W waves a row (256 / (64 W) rows a workgroup), or one part of a row per workgroup (S > 1).
@@ -198,9 +235,20 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
     const int64_t lo = (int64_t)part * d.part;
     const int len = (int)(d.V - lo < d.part ? d.V - lo : d.part);
     Sums s = {-DL_INF, 0.0f, 0.0f};
-    for (int v = in * 8; v < len; v += W * 512) {
+    // (the next two loads are in flight while a value is added)
+    int v = in * 8;
+    Raw8<T> r[2];
+    load8(r[0], z + lo + v, len - v);
+    load8(r[1], z + lo + v + W * 512, len - v - W * 512);
+    for (; v < len; v += W * 512) {
         float x[8];
-        dl_load8<T>(x, z + lo + v, len - v, -DL_INF);
+        raw8_f(x, r[0]);
+        r[0] = r[1];
+        load8(r[1], z + lo + v + W * 1024, len - v - W * 1024);
+        if (len - v < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = i < len - v ? x[i] : -DL_INF;
+        }
         dl_add<MODE>(s, x, d);
     }
     dl_join_lanes<MODE, 64>(s, d);
@@ -215,7 +263,7 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
             return;
         }
     }
-    dl_finish<T, 64>(d, row, lane, te, has, s, MODE == 2);
+    dl_finish<T, 64>(d, row, lane, te, has, s, MODE != 1);
 }
 
 // joins the parts of a row, one wave a row
@@ -232,18 +280,19 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
         dl_join<MODE>(s, v.x, v.y, v.z, d);
     }
     dl_join_lanes<MODE, 64>(s, d);
-    dl_finish<T, 64>(d, row, lane, te, has, s, MODE == 2);
+    dl_finish<T, 64>(d, row, lane, te, has, s, MODE != 1);
 }
 
 // Gradient, W waves a row or one part of a row per workgroup.  The entries' classes (and the label)
 // are written again after the stream has passed, from logits read before it: so dz may be z.
-template <typename T, int W>
+template <typename T, int MODE, int W>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     constexpr int TOP = W == 4 ? DL_MAX_TOP : DL_WAVE_TOP;
     __shared__ int sidx[4 / W][TOP];
     __shared__ float sp[4 / W][TOP], sz[4 / W][TOP + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    // (the last rows first: the loss has read them last, and what still is in the caches is theirs)
+    const int64_t row = W == 4 ? d.n - 1 - (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
     const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0, slot = W == 4 ? 0 : wave;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
@@ -280,12 +329,19 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     }
     const bool own_label = label >= lo && label < hi;
     if (in == 0) sz[slot][TOP] = own_label ? to_f<T>(z[label]) : 0.0f;
+    const Ref f = dl_ref(st.x, d);
+    const float ka = g * gt * ea, kb = g * gs * eb;
+    int v = lo + in * 8;
+    Raw8<T> r[2];  // (loads two steps ahead; a value is read before the one at its place is written)
+    load8(r[0], z + v, hi - v);
+    load8(r[1], z + v + W * 512, hi - v - W * 512);
     meet();
-    for (int v = lo + in * 8; v < hi; v += W * 512) {
+    for (; v < hi; v += W * 512) {
         float x[8];
-        dl_load8<T>(x, z + v, hi - v, 0.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = dl_grad(d, x[i], st, ea, eb, gt, gs, g, 0.0f, false);
+        raw8_f(x, r[0]);
+        r[0] = r[1];
+        load8(r[1], z + v + W * 1024, hi - v - W * 1024);
+        dl_grad8<MODE>(d, x, f, ka, kb);
         store8(dz + v, x, hi - v);
     }
     meet();  // (waits for the stores: those below come after them)
@@ -299,74 +355,123 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
                 p += sp[slot][o];
                 if (o < j) first = false;
             }
-        if (first) dz[i] = from_f<T>(dl_grad(d, sz[slot][j], st, ea, eb, gt, gs, g, p, i == label));
+        if (first) dz[i] = from_f<T>(dl_grad(d, sz[slot][j], f, ea, eb, gt, gs, g, p, i == label));
     }
     if (in == 0 && own_label) {
         bool listed = false;
         for (int o = 0; o < k; ++o) listed |= sidx[slot][o] == label;
-        if (!listed) dz[label] = from_f<T>(dl_grad(d, sz[slot][TOP], st, ea, eb, gt, gs, g, 0.0f, true));
+        if (!listed) dz[label] = from_f<T>(dl_grad(d, sz[slot][TOP], f, ea, eb, gt, gs, g, 0.0f, true));
     }
 }
 
-// Few classes: 16 lanes a row, at most eight values a lane in registers.
-template <typename T, int MODE>
+// Few classes: 16 lanes a row, NZ values of z and one entry a lane in registers.
+template <typename T, int NZ>
+struct Tiny {
+    float z[NZ], t;
+    int i, label;
+    Teacher te;
+
+    __device__ inline float logit(int v) const {  // of class v, by all lanes of the row
+        float r = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NZ; ++k) {
+            const float o = __shfl(z[k], v & 15, 16);
+            if (v >> 4 == k) r = o;
+        }
+        return r;
+    }
+    __device__ inline void load(const DistillArgs& d, int64_t row, int lane) {
+        const T* p = (const T*)d.z + row * d.ldz;
+        const int64_t base = row / d.rows_per;
+        i = -1;
+        t = -DL_INF;
+        if (d.wt != 0.0f && lane < d.k) {
+            i = d.idx[base * d.k + lane];
+            t = to_f<T>(((const T*)d.t)[base * d.k + lane]);
+        }
+        label = d.y ? d.y[base] : -1;
+#pragma unroll
+        for (int k = 0; k < NZ; ++k) z[k] = lane + 16 * k < d.V ? to_f<T>(p[lane + 16 * k]) : -DL_INF;
+        if ((unsigned)i >= (unsigned)d.V) {
+            i = -1;
+            t = -DL_INF;
+        }
+        if ((unsigned)label >= (unsigned)d.V) label = -1;
+        const float m = dl_max<16>(t);
+        te.ref = m == -DL_INF ? 0.0f : m;
+        te.mass = dl_sum<16>(i >= 0 ? exp2f((t - te.ref) * d.ct) : 0.0f);
+    }
+};
+
+template <typename T, int MODE, int NZ>
 __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
     const int lane = threadIdx.x & 15;
     const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (row >= d.n) return;
-    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 16>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = dl_has(d, row, te);
-    if (has == 0) {
-        if (lane == 0) {
-            d.loss[row] = 0.0f;
-            d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-        return;
-    }
-    const T* z = (const T*)d.z + row * d.ldz;
+    Tiny<T, NZ> r;
+    r.load(d, row, lane);
+    int has = (r.te.mass == 0.0f ? 0 : 1) | (r.label >= 0 ? 2 : 0);
+    if (d.ids && (unsigned)d.ids[row] >= (unsigned)d.K) has = 0;
     Sums s = {-DL_INF, 0.0f, 0.0f};
-    for (int v = lane; v < d.V; v += 16) {
-        const float x[1] = {to_f<T>(z[v])};
-        dl_add<MODE>(s, x, d);
-    }
+    dl_add<MODE>(s, r.z, d);
     dl_join_lanes<MODE, 16>(s, d);
-    dl_finish<T, 16>(d, row, lane, te, has, s, MODE == 2);
+    constexpr float LN2 = 0.6931471806f;
+    const Ref f = dl_ref(s.m, d);
+    const float la = logf(s.a), lb = MODE != 1 ? logf(s.b) : la;
+    const int at = r.i >= 0 ? r.i : 0;
+    float zi = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NZ; ++k) {
+        const float o = __shfl(r.z[k], at & 15, 16);
+        if (at >> 4 == k) zi = o;
+    }
+    const float zy = r.logit(r.label >= 0 ? r.label : 0);
+    float kl = 0.0f;
+    if (r.i >= 0) {
+        const float e = r.t - r.te.ref, p = exp2f(e * d.ct) / r.te.mass;
+        if (p != 0.0f) kl = p * ((e * d.inv_t - logf(r.te.mass)) - (dl_t(zi, f, d) * LN2 - la));
+    }
+    kl = dl_sum<16>(kl);
+    if (lane != 0) return;
+    if (s.a == 0.0f) has = 0;  // every logit is -inf
+    float loss = 0.0f;
+    if (has & 1) loss += d.wt * kl;
+    if (has & 2) loss += d.ws * (lb - dl_s(zy, f, d) * LN2);
+    d.loss[row] = loss;
+    d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (MODE != 1 ? s.b : s.a), (float)has);
 }
 
-template <typename T>
+template <typename T, int NZ>
 __global__ __launch_bounds__(256) void distill_grad_tiny_kernel(DistillArgs d) {
     const int lane = threadIdx.x & 15;
     const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (row >= d.n) return;
-    const T* z = (const T*)d.z + row * d.ldz;
     T* dz = (T*)d.dz + row * d.lddz;
     const float4 st = d.stats[row];
     const float g = d.g ? d.g[row] : 1.0f;
+    Tiny<T, NZ> r;
+    r.load(d, row, lane);
     const int has = g == 0.0f ? 0 : (int)st.w;
     const float gt = has & 1 ? d.gt : 0.0f, gs = has & 2 ? d.gs : 0.0f;
     const float ea = has & 1 ? st.y : 0.0f, eb = has & 2 ? st.z : 0.0f;
-    const int label = has & 2 ? dl_label(d, row) : -1;
-    int i = -1;
-    float p = 0.0f;
-    if (has & 1) {  // (k <= 16: an entry a lane)
-        const Teacher te = dl_teacher<T, 16>(d, row, lane);
-        if (lane < d.k) {
-            const int64_t first = row / d.rows_per * d.k;
-            i = d.idx[first + lane];
-            if ((unsigned)i < (unsigned)d.V) p = exp2f((to_f<T>(((const T*)d.t)[first + lane]) - te.ref) * d.ct) / te.mass;
-            else i = -1;
-        }
+    const int label = has & 2 ? r.label : -1;
+    const Ref f = dl_ref(st.x, d);
+    const float p = r.i >= 0 && has & 1 ? exp2f((r.t - r.te.ref) * d.ct) / r.te.mass : 0.0f;
+    float sum[NZ];
+#pragma unroll
+    for (int k = 0; k < NZ; ++k) sum[k] = 0.0f;
+    const int top = has & 1 ? d.k : 0;
+    for (int j = 0; j < top; ++j) {
+        const int ij = __shfl(r.i, j, 16);
+        const float pj = __shfl(p, j, 16);
+#pragma unroll
+        for (int k = 0; k < NZ; ++k)
+            if (ij == lane + 16 * k) sum[k] += pj;
     }
-    const int k = d.k;
-    for (int b = 0; b < d.V; b += 16) {
-        const int v = b + lane;
-        float sum = 0.0f;
-        for (int j = 0; j < k; ++j) {
-            const int ij = __shfl(i, j, 16);
-            const float pj = __shfl(p, j, 16);
-            if (ij == v) sum += pj;
-        }
-        if (v < d.V) dz[v] = has == 0 ? from_f<T>(0.0f) : from_f<T>(dl_grad(d, to_f<T>(z[v]), st, ea, eb, gt, gs, g, sum, v == label));
+#pragma unroll
+    for (int k = 0; k < NZ; ++k) {
+        const int v = lane + 16 * k;
+        if (v < d.V) dz[v] = from_f<T>(has == 0 ? 0.0f : dl_grad(d, r.z[k], f, ea, eb, gt, gs, g, sum[k], v == label));
     }
 }
 

@@ -71,10 +71,18 @@ DistillArgs distill_args(const pnn_distill* a, void* stats, int width) {
     return d;
 }
 
+// the sums that a call needs: one; two; two whose second is that of the first's squares
+int distill_mode(const pnn_distill* a) {
+    if (a->top == 0 || a->alpha == 0.0f || a->alpha == 1.0f || a->temperature == 1.0f) return 1;
+    return a->temperature == 2.0f ? 3 : 2;
+}
+
 template <typename T, int MODE>
-pnn_status run_distill_loss(const DistillArgs& d, int width, hipStream_t s) {
+pnn_status launch_distill_loss(const DistillArgs& d, int width, hipStream_t s) {
     if (width == DL_LANES) {
-        distill_loss_tiny_kernel<T, MODE><<<(unsigned)((d.n + 15) / 16), 256, 0, s>>>(d);
+        const unsigned blocks = (unsigned)((d.n + 15) / 16);
+        if (d.V <= 16) distill_loss_tiny_kernel<T, MODE, 1><<<blocks, 256, 0, s>>>(d);
+        else distill_loss_tiny_kernel<T, MODE, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
     } else if (width == DL_WAVE) {
         distill_loss_kernel<T, MODE, 1><<<(unsigned)((d.n + 3) / 4), 256, 0, s>>>(d);
     } else {
@@ -88,15 +96,30 @@ pnn_status run_distill_loss(const DistillArgs& d, int width, hipStream_t s) {
     return launched("distillation loss");
 }
 
-template <typename T>
-pnn_status run_distill_grad(const DistillArgs& d, int width, hipStream_t s) {
-    if (width == DL_LANES) distill_grad_tiny_kernel<T><<<(unsigned)((d.n + 15) / 16), 256, 0, s>>>(d);
-    else if (width == DL_WAVE) distill_grad_kernel<T, 1><<<(unsigned)((d.n + 3) / 4), 256, 0, s>>>(d);
-    else {
+template <typename T, int MODE>
+pnn_status launch_distill_grad(const DistillArgs& d, int width, hipStream_t s) {
+    if (width == DL_LANES) {
+        const unsigned blocks = (unsigned)((d.n + 15) / 16);
+        if (d.V <= 16) distill_grad_tiny_kernel<T, 1><<<blocks, 256, 0, s>>>(d);
+        else distill_grad_tiny_kernel<T, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
+    } else if (width == DL_WAVE) {
+        distill_grad_kernel<T, MODE, 1><<<(unsigned)((d.n + 3) / 4), 256, 0, s>>>(d);
+    } else {
         TRY(grid_fits(d.n * d.S));
-        distill_grad_kernel<T, 4><<<(unsigned)(d.n * d.S), 256, 0, s>>>(d);
+        distill_grad_kernel<T, MODE, 4><<<(unsigned)(d.n * d.S), 256, 0, s>>>(d);
     }
     return launched("distillation gradient");
+}
+
+template <typename T>
+pnn_status run_distill_loss(const DistillArgs& d, int mode, int width, hipStream_t s) {
+    return mode == 1 ? launch_distill_loss<T, 1>(d, width, s)
+                     : mode == 2 ? launch_distill_loss<T, 2>(d, width, s) : launch_distill_loss<T, 3>(d, width, s);
+}
+template <typename T>
+pnn_status run_distill_grad(const DistillArgs& d, int mode, int width, hipStream_t s) {
+    return mode == 1 ? launch_distill_grad<T, 1>(d, width, s)
+                     : mode == 2 ? launch_distill_grad<T, 2>(d, width, s) : launch_distill_grad<T, 3>(d, width, s);
 }
 
 }  // namespace
@@ -119,9 +142,8 @@ pnn_status pnn_distill_loss(const pnn_distill* a, float* loss_dev, void* stats_d
     const int width = distill_width(a->n, a->classes, a->top);
     DistillArgs d = distill_args(a, stats_dev, width);
     d.loss = loss_dev;
-    const bool two = d.wt != 0.0f && a->alpha > 0.0f && a->temperature != 1.0f;
-    if (a->type == PNN_FP32) return two ? run_distill_loss<float, 2>(d, width, s) : run_distill_loss<float, 1>(d, width, s);
-    return two ? run_distill_loss<bf16_t, 2>(d, width, s) : run_distill_loss<bf16_t, 1>(d, width, s);
+    const int mode = distill_mode(a);
+    return a->type == PNN_FP32 ? run_distill_loss<float>(d, mode, width, s) : run_distill_loss<bf16_t>(d, mode, width, s);
 }
 
 pnn_status pnn_distill_grad(const pnn_distill* a, const float* g_dev, const void* stats_dev, int64_t stats_bytes, void* dz_dev,
@@ -135,7 +157,8 @@ pnn_status pnn_distill_grad(const pnn_distill* a, const float* g_dev, const void
     const int width = distill_width(a->n, a->classes, a->top);
     DistillArgs d = distill_args(a, const_cast<void*>(stats_dev), width);
     d.g = g_dev; d.dz = dz_dev; d.lddz = dz_ld;
-    return a->type == PNN_FP32 ? run_distill_grad<float>(d, width, s) : run_distill_grad<bf16_t>(d, width, s);
+    const int mode = distill_mode(a);
+    return a->type == PNN_FP32 ? run_distill_grad<float>(d, mode, width, s) : run_distill_grad<bf16_t>(d, mode, width, s);
 }
 
 }  // extern "C"

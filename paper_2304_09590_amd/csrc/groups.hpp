@@ -18,35 +18,42 @@ namespace pnn {
 constexpr int GR_MAX_NETS = 1024;   // most networks of a grouping (its counters live in LDS)
 constexpr int GR_THREADS = 512, GR_WAVES = GR_THREADS / 64;
 constexpr int GR_MAX_BLOCKS = 256;  // most workgroups that count (each reads all their counts)
+constexpr int GR_KEYS = 16;         // pairs that a thread keeps in registers
 constexpr int GR_SMALL = 16;        // pairs per tile of the kernels for few rows
-constexpr int GR_LARGE = 128;       // pairs per tile of the matrix-tile kernels
+constexpr int GR_LARGE = 128, GR_HUGE = 256;  // pairs per tile of the matrix-tile kernels
+constexpr int GR_HEIGHTS = 3;       // tiles of 16, 128 and 256 pairs
 
-// Layout of a plan (int32 words): off[K + 1] | pairs[P] | tiles of 16 pairs | tiles of 128 pairs |
-// counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
-// pairs, -1 for no tile: the host knows only the most tiles there can be.
+// Layout of a plan (int32 words): off[K + 1] | pairs[P] | numbers of tiles | tiles of 16, of 128 and of 256
+// pairs | counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
+// pairs.  The host knows only the most tiles there can be (extra workgroups end at once).
 struct GroupPlan {
     int64_t P;
     int K;
-    int64_t o_pairs, o_small, o_large, o_hist, words;
-    int64_t n_small, n_large;
+    int64_t o_pairs, o_count, o_tiles[GR_HEIGHTS], o_hist, words;
+    int64_t most[GR_HEIGHTS];
     int blocks;
     int64_t chunk;  // pairs per counting workgroup
 };
+
+__host__ __device__ inline int group_height(int h) { return h == 0 ? GR_SMALL : h == 1 ? GR_LARGE : GR_HUGE; }
 
 __host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
     GroupPlan g;
     g.P = n * per_row;
     g.K = K;
     const int64_t extra = g.P < K + 1 ? g.P : K + 1;
-    g.n_small = g.P / GR_SMALL + extra;
-    g.n_large = g.P / GR_LARGE + extra;
     auto up = [](int64_t v) { return (v + 3) / 4 * 4; };
     g.o_pairs = up(K + 1);
-    g.o_small = g.o_pairs + up(g.P);
-    g.o_large = g.o_small + up(2 * g.n_small);
-    g.o_hist = g.o_large + up(2 * g.n_large);
+    g.o_count = g.o_pairs + up(g.P);
+    int64_t at = g.o_count + up(GR_HEIGHTS);
+    for (int h = 0; h < GR_HEIGHTS; ++h) {
+        g.most[h] = g.P / group_height(h) + extra;
+        g.o_tiles[h] = at;
+        at += up(2 * g.most[h]);
+    }
+    g.o_hist = at;
     g.chunk = (g.P + GR_MAX_BLOCKS - 1) / GR_MAX_BLOCKS;
-    if (g.chunk < 4096) g.chunk = 4096;
+    if (g.chunk < 4096) g.chunk = g.P <= GR_THREADS * GR_KEYS ? GR_THREADS * GR_KEYS : 4096;  // (one launch, or two)
     g.blocks = (int)((g.P + g.chunk - 1) / g.chunk);
     g.words = g.o_hist + (g.blocks > 1 ? up((int64_t)g.blocks * (K + 1)) : 0);
     return g;
@@ -54,9 +61,9 @@ __host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
 
 struct GroupArgs {
     const int32_t* ids;
-    int32_t *off, *pairs, *hist;
-    int2 *small, *large;
-    int64_t P, chunk, n_small, n_large;
+    int32_t *off, *pairs, *count, *hist;
+    int2* tiles[GR_HEIGHTS];
+    int64_t P, chunk;
     int K, blocks;
 };
 
@@ -76,22 +83,24 @@ __global__ __launch_bounds__(GR_THREADS) void group_count_kernel(GroupArgs g) {
     for (int e = threadIdx.x; e <= g.K; e += GR_THREADS) g.hist[(int64_t)blockIdx.x * (g.K + 1) + e] = cnt[e];
 }
 
-// exclusive scan of v[0..n) into out[0..n], by one wave; v is mapped through f first
+// exclusive scan of f(0 .. n - 1) into out[0 .. n], by one wave; a lane's values are neighbours
 template <typename F>
 __device__ inline void wave_scan(int* out, int n, int lane, F f) {
-    int carry = 0;
-    for (int b = 0; b < n; b += 64) {
-        const int v = b + lane < n ? f(b + lane) : 0;
-        int s = v;
+    const int per = (n + 63) / 64, lo = lane * per, hi = lo + per < n ? lo + per : n;
+    int own = 0;
+    for (int e = lo; e < hi; ++e) own += f(e);
+    int s = own;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(s, d);
-            if (lane >= d) s += u;
-        }
-        if (b + lane < n) out[b + lane] = carry + s - v;
-        carry += __shfl(s, 63);
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(s, d);
+        if (lane >= d) s += u;
     }
-    if (lane == 0) out[n] = carry;
+    int at = s - own;
+    for (int e = lo; e < hi; ++e) {
+        out[e] = at;
+        at += f(e);
+    }
+    if (lane == 63) out[n] = s;
 }
 
 // Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds
@@ -104,22 +113,40 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
     int* cur = gsm;                  // [GR_WAVES][K1]
     int* tot = cur + GR_WAVES * K1;  // [K1]
     int* off = tot + K1;             // [K1 + 1]
-    int* fs = off + K1 + 1;          // [K1 + 1] first small tile of each network
-    int* fl = fs + K1 + 1;           // [K1 + 1] first large tile
+    int* first = off + K1 + 1;       // [GR_HEIGHTS][K1 + 1] first tile of each network
     for (int e = tid; e < GR_WAVES * K1; e += GR_THREADS) cur[e] = 0;
     __syncthreads();
     const int64_t lo = blockIdx.x * g.chunk, hi = lo + g.chunk < g.P ? lo + g.chunk : g.P;
     const int64_t part = (g.chunk + GR_WAVES * 64 - 1) / (GR_WAVES * 64) * 64;
     const int64_t w0 = lo + wave * part, w1 = w0 + part < hi ? w0 + part : hi;
-    for (int64_t i = w0 + lane; i < w1; i += 64) atomicAdd(&cur[wave * K1 + group_key(g, i)], 1);
+    // (a chunk of at most GR_KEYS pairs a thread is read once, all loads in flight together)
+    int keys[GR_KEYS];
+    const bool kept = part <= 64 * GR_KEYS;
+    if (kept) {
+#pragma unroll
+        for (int t = 0; t < GR_KEYS; ++t) {
+            const int64_t i = w0 + 64 * t + lane;
+            keys[t] = i < w1 ? group_key(g, i) : -1;
+        }
+#pragma unroll
+        for (int t = 0; t < GR_KEYS; ++t)
+            if (keys[t] >= 0) atomicAdd(&cur[wave * K1 + keys[t]], 1);
+    } else {
+        for (int64_t i = w0 + lane; i < w1; i += 64) atomicAdd(&cur[wave * K1 + group_key(g, i)], 1);
+    }
     __syncthreads();
     for (int e = tid; e < K1; e += GR_THREADS) {
         int before = 0, all = 0;
         if (g.blocks > 1)
-            for (int b = 0; b < g.blocks; ++b) {
-                const int h = g.hist[(int64_t)b * K1 + e];
-                all += h;
-                if (b < (int)blockIdx.x) before += h;
+            for (int b0 = 0; b0 < g.blocks; b0 += 16) {
+                int h[16];
+#pragma unroll
+                for (int b = 0; b < 16; ++b) h[b] = b0 + b < g.blocks ? g.hist[(int64_t)(b0 + b) * K1 + e] : 0;
+#pragma unroll
+                for (int b = 0; b < 16; ++b) {
+                    all += h[b];
+                    before += b0 + b < (int)blockIdx.x ? h[b] : 0;
+                }
             }
         for (int w = 0; w < GR_WAVES; ++w) {
             const int c = cur[w * K1 + e];
@@ -130,14 +157,13 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
     }
     __syncthreads();
     if (wave == 0) wave_scan(off, K1, lane, [&](int e) { return tot[e]; });
-    if (wave == 1) wave_scan(fs, K1, lane, [&](int e) { return (tot[e] + GR_SMALL - 1) / GR_SMALL; });
-    if (wave == 2) wave_scan(fl, K1, lane, [&](int e) { return (tot[e] + GR_LARGE - 1) / GR_LARGE; });
+    if (wave >= 1 && wave <= GR_HEIGHTS) {
+        const int h = group_height(wave - 1);
+        wave_scan(first + (wave - 1) * (K1 + 1), K1, lane, [&](int e) { return (tot[e] + h - 1) / h; });
+    }
     __syncthreads();
     const int bits = 32 - __clz(g.K);
-    for (int64_t b = w0; b < w1; b += 64) {
-        const int64_t i = b + lane;
-        const bool live = i < w1;
-        const int key = live ? group_key(g, i) : 0;
+    auto place = [&](int64_t i, int key, bool live) {
         uint64_t same = __ballot(live);
         for (int t = 0; t < bits; ++t) {
             const uint64_t one = __ballot((key >> t) & 1);
@@ -145,35 +171,39 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
         }
         if (live) {
             const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int first = __ffsll((unsigned long long)same) - 1;
+            const int leader = __ffsll((unsigned long long)same) - 1;
             int base = 0;
             if (rank == 0) base = atomicAdd(&cur[wave * K1 + key], __popcll(same));
-            base = __shfl(base, first);
+            base = __shfl(base, leader);
             g.pairs[off[key] + base + rank] = (int)i;
         }
+    };
+    if (kept) {
+#pragma unroll
+        for (int t = 0; t < GR_KEYS; ++t)
+            if (w0 + 64 * t < w1) place(w0 + 64 * t + lane, keys[t], keys[t] >= 0);
+    } else {
+        for (int64_t b = w0; b < w1; b += 64) place(b + lane, b + lane < w1 ? group_key(g, b + lane) : 0, b + lane < w1);
     }
     if (blockIdx.x == 0)
         for (int e = tid; e < K1; e += GR_THREADS) g.off[e] = off[e];
+    if (blockIdx.x == 0 && tid < GR_HEIGHTS) g.count[tid] = first[tid * (K1 + 1) + K1];
     const int64_t step = (int64_t)gridDim.x * GR_THREADS;
-    for (int64_t t = blockIdx.x * (int64_t)GR_THREADS + tid; t < g.n_small + g.n_large; t += step) {
-        const bool s = t < g.n_small;
-        const int* f = s ? fs : fl;
-        const int64_t u = s ? t : t - g.n_small;
-        int2 v = make_int2(-1, 0);
-        if (u < f[K1]) {
+    for (int h = 0; h < GR_HEIGHTS; ++h) {
+        const int* f = first + h * (K1 + 1);
+        for (int64_t u = blockIdx.x * (int64_t)GR_THREADS + tid; u < f[K1]; u += step) {
             int a = 0, b = K1;  // the last network whose first tile is at most u
             while (b - a > 1) {
                 const int m = (a + b) >> 1;
                 if (f[m] <= u) a = m;
                 else b = m;
             }
-            v = make_int2(a, off[a] + (int)(u - f[a]) * (s ? GR_SMALL : GR_LARGE));
+            g.tiles[h][u] = make_int2(a, off[a] + (int)(u - f[a]) * group_height(h));
         }
-        (s ? g.small : g.large)[u] = v;
     }
 }
 
-__host__ inline size_t group_lds(int K) { return sizeof(int) * ((size_t)GR_WAVES * (K + 1) + 4 * (K + 2)); }
+__host__ inline size_t group_lds(int K) { return sizeof(int) * ((size_t)GR_WAVES * (K + 1) + (2 + GR_HEIGHTS) * (K + 2)); }
 
 // ------------------------------------------------------------------------------------
 // products
@@ -197,7 +227,7 @@ enum { GR_FWD = 0, GR_DX = 1, GR_DW = 2 };
 struct GroupGemm {
     const int32_t *off, *pairs;
     const int2* tiles;
-    int64_t n_tiles;
+    const int32_t* n_tiles;
     int K;
     int M, N, Kx;              // extents; N of the pairs' products is the number of pairs, dropped ones among them,
                                // and k of a weight gradient the group's pairs
@@ -268,17 +298,25 @@ __device__ inline void load8(Raw8<float>& r, const float* p, int nv) {
 }
 
 template <typename T>
-__device__ inline void load8_f(float (&v)[8], const T* p, int nv) {
-    Raw8<T> r;
-    load8(r, p, nv);
+__device__ inline void raw8_f(float (&v)[8], const Raw8<T>& r) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (sizeof(T) == 4) v[i] = r.v[i >> 2][i & 3];
         else v[i] = i & 1 ? bf_hi(r.v[i >> 1]) : bf_lo(r.v[i >> 1]);
     }
 }
+template <typename T>
+__device__ inline void load8_f(float (&v)[8], const T* p, int nv) {
+    Raw8<T> r;
+    load8(r, p, nv);
+    raw8_f(v, r);
+}
 
 // the first nv of eight values
+// (STREAM: whole rows of a large result, which pass the caches by: the writes of a round of workgroups,
+// 33 MB at once, evict what the next round reads; forward 65,536 pairs 1024 -> 4096, 16 networks, bf16
+// 669 -> 597 us, input gradient 32,768 pairs 2048 x 2048 274 -> 238 us; fp32 results lose by it)
+template <bool STREAM = false>
 __device__ inline void store8(float* p, const float (&v)[8], int nv) {
     if (nv >= 8) {
         *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
@@ -289,9 +327,12 @@ __device__ inline void store8(float* p, const float (&v)[8], int nv) {
             if (i < nv) p[i] = v[i];
     }
 }
+template <bool STREAM = false>
 __device__ inline void store8(bf16_t* p, const float (&v)[8], int nv) {
     if (nv >= 8) {
-        *(u4v_a2*)p = u4v{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+        const u4v q = {cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+        if (STREAM) __builtin_nontemporal_store(q, (u4v_a2*)p);
+        else *(u4v_a2*)p = q;
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -306,12 +347,64 @@ __device__ inline int64_t group_xcd(int64_t id, int64_t total) {
     return x * q + (x < r ? x : r) + (id >> 3);
 }
 
+// A workgroup's tile: network, place in the result, its columns there, k from position p0 (weight gradient)
+struct GroupPlace { int e, m0, n0, nv, split, p0, Kx; };
+
+// Workgroups of a weight gradient: of every network's tiles each XCD takes one stretch, another one for the
+// next network, so that unequal groups weigh on all XCDs alike.
+__host__ __device__ inline int64_t group_dw_blocks(int64_t tiles, int64_t groups) {
+    return tiles < 8 ? tiles * groups : 8 * ((tiles + 7) / 8) * groups;
+}
+
+template <int DIR, int BM, int BN, int STEP>
+__device__ inline bool group_place_of(const GroupGemm& g, int mt, GroupPlace& o) {
+    o.n0 = o.split = 0;
+    if (DIR == GR_DW) {
+        const int tiles = mt * ((g.N + BN - 1) / BN);
+        const int id = (int)blockIdx.x;
+        int t, grp;
+        if (tiles < 8) {
+            t = id % tiles;
+            grp = id / tiles;
+        } else {
+            const int share = (tiles + 7) / 8, local = id >> 3;
+            grp = local / share;
+            t = ((id + grp) & 7) * share + local % share;
+            if (t >= tiles) return false;
+        }
+        o.e = grp % g.K;
+        o.split = grp / g.K;
+        o.m0 = t % mt * BM;
+        o.n0 = t / mt * BN;
+        o.nv = g.N - o.n0 < BN ? g.N - o.n0 : BN;
+        const int first = g.off[o.e], all = g.off[o.e + 1] - first;
+        const int part = (all + g.splits * STEP - 1) / (g.splits * STEP) * STEP;
+        o.p0 = first + (o.split * part < all ? o.split * part : all);
+        o.Kx = first + all - o.p0 < part ? first + all - o.p0 : part;
+        return true;
+    }
+    // eight tiles of pairs next to each other, then along m: their rows and weights stay in L2
+    const int64_t n_tiles = *g.n_tiles, total = n_tiles * mt;
+    if (blockIdx.x >= total) return false;
+    const int64_t id = group_xcd(blockIdx.x, total);
+    const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
+    const int64_t left = n_tiles - grp * 8, wide = left < 8 ? left : 8;
+    const int2 t = g.tiles[grp * 8 + in % wide];
+    o.m0 = (int)(in / wide) * BM;
+    o.e = t.x;
+    o.p0 = t.y;
+    const int end = o.e < g.K ? g.off[o.e + 1] : g.N;
+    o.nv = end - o.p0 < BN ? end - o.p0 : BN;
+    o.Kx = o.e < g.K ? g.Kx : 0;  // (dropped pairs: nothing to sum)
+    return true;
+}
+
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v lds_s4v;
 
 // An operand tile in LDS, 128 wide and BK deep, in bf16 (fp32 operands as three such planes).
 //  KC (memory runs along k): rows of BK values in 16-byte chunks; a row's chunks are permuted by
-//     XOR so that 8 and 16 neighbouring rows' reads of one chunk fall on different banks.
+//     XOR so that eight neighbouring rows' reads of one chunk fall on different banks.
 //  NC (memory runs across k): rows of 128 values, one per k, in 32-byte blocks, permuted by XOR so
 //     that the rows which one transposing read touches fall on different banks.
 template <bool KC, int BK>
@@ -320,7 +413,7 @@ struct GTile {
     static __device__ inline int row(int s) { return s / CPR; }
     static __device__ inline int chunk(int s) { return s % CPR; }
     static __device__ inline int key(int r) {
-        if (KC) return CPR == 8 ? (r & 7) ^ ((r >> 3) & 1) : ((r >> 1) & 3) ^ ((r >> 3) & 1);
+        if (KC) return CPR == 8 ? r & 7 : (r >> 1) & 3;
         return (r & 3) | ((r >> 1) & 4);
     }
     static __device__ inline int offset(int r, int c) {
@@ -351,24 +444,19 @@ __device__ inline void gt_store(bf16_t* lds, int plane, const Raw8<float>& r) {
 }
 
 // activations / slopes of eight neighbouring values (the choice outside the loops: one copy of each)
+__device__ inline void group_rectify8(int act, float (&v)[8]) {
+    if (act != ACT_RELU && act != ACT_LEAKY) return;
+    const float low = act == ACT_RELU ? 0.0f : 0.01f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] = v[r] < 0.0f ? (act == ACT_RELU ? -0.0f : low * v[r]) : v[r] + 0.0f;
+}
 __device__ inline void group_act8(int act, float (&v)[8]) {
-    switch (act) {
-    case ACT_SIGMOID:
+    if (act == ACT_SIGMOID) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = group_act(ACT_SIGMOID, v[r]);
-        break;
-    case ACT_TANH:
+    } else {
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = group_act(ACT_TANH, v[r]);
-        break;
-    case ACT_RELU:
-    case ACT_LEAKY: {
-        const float low = act == ACT_RELU ? 0.0f : 0.01f;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = v[r] < 0.0f ? (act == ACT_RELU ? -0.0f : low * v[r]) : v[r] + 0.0f;
-        break;
-    }
-    default: break;
     }
 }
 __device__ inline void group_slope8(int act, float (&v)[8], const float (&a)[8]) {
@@ -394,6 +482,8 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     const int pairs = DIR == GR_DW ? g.off[e + 1] - g.off[e] : 0;
     const float scale = DIR == GR_DW && g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
     if (DIR == GR_DW && g.lr != 0.0f && pairs == 0) return;  // no update
+    // (the pair of column `lane` of the wave: asked of its lane in the loop, not of memory)
+    const int own = DIR != GR_DW && lane < 16 * NJ && wn + lane < nv ? g.pairs[p0 + wn + lane] : 0;
     float bias[8];
     if (DIR == GR_FWD) {
 #pragma unroll
@@ -404,10 +494,10 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
 #pragma unroll
         for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int c = 0; c < 16; c += COLS) {
+        auto leave = [&](int c, bool smooth) {
             const int col = c + lane / PER, n = wn + 16 * j + col;
-            if (n >= nv || left <= 0) continue;
+            const int64_t pair = DIR != GR_DW ? __shfl(own, 16 * j + col) : 0;
+            if (n >= nv || left <= 0) return;
             const f4 lo = *(const f4*)(turn + col * LD + part), hi = *(const f4*)(turn + col * LD + part + 4);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (DIR == GR_DW) {
@@ -421,22 +511,29 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
                     if (g.shadow) store8(g.shadow + e * g.ynet + at, v, left);
                 }
                 store8(y, v, left);
-                continue;
+                return;
             }
-            const int64_t pair = g.pairs[p0 + n];
             if (e == g.K) {  // dropped
 #pragma unroll
                 for (int r = 0; r < 8; ++r) v[r] = 0.0f;
             } else if (DIR == GR_FWD) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) v[r] += bias[r];
-                group_act8(g.act, v);
+                if (smooth) group_act8(g.act, v);
+                else group_rectify8(g.act, v);
             } else if (g.a) {
                 float a[8];
                 load8_f<T>(a, (const T*)g.a + pair * g.lda + m, left);
                 group_slope8(g.act, v, a);
             }
-            store8((TO*)g.y + pair * g.ldy + m, v, left);
+            store8<true>((TO*)g.y + pair * g.ldy + m, v, left);
+        };
+        if (DIR == GR_FWD && (g.act == ACT_SIGMOID || g.act == ACT_TANH)) {  // (one copy of their code)
+#pragma unroll 1
+            for (int c = 0; c < 16; c += COLS) leave(c, true);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 16; c += COLS) leave(c, false);
         }
         __builtin_amdgcn_wave_barrier();
         if (bias_rows && kg == 0 && wn + 16 * j + l15 < nv) {
@@ -458,32 +555,9 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     bf16_t *la = lds, *lb = lds + PL * TA::ELEMS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mt = (g.M + 127) / 128;
-    const int64_t id = group_xcd(blockIdx.x, gridDim.x);
-    int e, m0, n0 = 0, nv, split = 0, p0, Kx;
-    if (DIR == GR_DW) {
-        const int nt = (g.N + 127) / 128;
-        m0 = (int)(id % mt) * 128;
-        n0 = (int)(id / mt % nt) * 128;
-        e = (int)(id / mt / nt % g.K);
-        split = (int)(id / mt / nt / g.K);
-        nv = g.N - n0 < 128 ? g.N - n0 : 128;
-        const int first = g.off[e], all = g.off[e + 1] - first;
-        const int part = (all + g.splits * BK - 1) / (g.splits * BK) * BK;
-        p0 = first + (split * part < all ? split * part : all);
-        Kx = first + all - p0 < part ? first + all - p0 : part;
-    } else {
-        // eight tiles of pairs next to each other, then along m: their rows and weights stay in L2
-        const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
-        const int64_t left = g.n_tiles - grp * 8, wide = left < 8 ? left : 8;
-        const int2 t = g.tiles[grp * 8 + in % wide];
-        m0 = (int)(in / wide) * 128;
-        e = t.x;
-        if (e < 0) return;
-        p0 = t.y;
-        const int end = e < g.K ? g.off[e + 1] : g.N;
-        nv = end - p0 < 128 ? end - p0 : 128;
-        Kx = e < g.K ? g.Kx : 0;  // (dropped pairs: nothing to sum)
-    }
+    GroupPlace at;
+    if (!group_place_of<DIR, 128, 128, BK>(g, mt, at)) return;
+    const int e = at.e, m0 = at.m0, n0 = at.n0, nv = at.nv, split = at.split, p0 = at.p0, Kx = at.Kx;
     const int mv = g.M - m0 < 128 ? g.M - m0 : 128;
     f4 acc[4][4], accb[4];
 #pragma unroll
@@ -582,7 +656,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
 }
 
 // ------------------------------------------------------------------------------------
-// bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, four waves of BM / 2 x BN / 2,
+// bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, WM x WN waves,
 // a ring of stages of 32 k in LDS that global memory fills directly.
 
 static __device__ __align__(64) uint32_t group_zeros[16];  // what lies outside an operand
@@ -608,7 +682,7 @@ template <bool KC, int T>
 struct RTile {
     static constexpr int ELEMS = T * 32, CHUNKS = ELEMS / 8;
     static __device__ inline int row(int s) { return KC ? s >> 2 : s / (T / 8); }  // (NC: the k)
-    static __device__ inline int key(int r) { return KC ? ((r >> 1) & 3) ^ ((r >> 3) & 1) : (r & 3) | ((r >> 1) & 4); }
+    static __device__ inline int key(int r) { return KC ? (r >> 1) & 3 : (r & 3) | ((r >> 1) & 4); }
     // the chunk of the row that belongs at place s
     static __device__ inline int chunk(int s) {
         const int r = row(s), c = KC ? s & 3 : s % (T / 8);
@@ -628,41 +702,22 @@ struct RTile {
     }
 };
 
-template <int DIR, typename TO, int BM, int BN, int NST>
-__global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
+// AHEAD: a stage is waited for one step before it is multiplied, so that a step's first operands are read
+// during the step before it.
+template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
+__global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g) {
     typedef RTile<DIR == GR_FWD, BM> TA;
     typedef RTile<DIR != GR_DW, BN> TB;
-    constexpr int UA = TA::CHUNKS / 256, UB = TB::CHUNKS / 256, STAGE = TA::ELEMS + TB::ELEMS;
-    constexpr int MI = BM / 32, NJ = BN / 32;  // 16 x 16 blocks of a wave
+    constexpr int THREADS = 64 * WM * WN;
+    constexpr int UA = TA::CHUNKS / THREADS, UB = TB::CHUNKS / THREADS, STAGE = TA::ELEMS + TB::ELEMS;
+    constexpr int MI = BM / WM / 16, NJ = BN / WN / 16;  // 16 x 16 blocks of a wave
     extern __shared__ __align__(16) bf16_t ring[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + BM - 1) / BM;
-    const int64_t id = group_xcd(blockIdx.x, gridDim.x);
-    int e, m0, n0 = 0, nv, split = 0, p0, Kx;
-    if (DIR == GR_DW) {
-        const int nt = (g.N + BN - 1) / BN;
-        m0 = (int)(id % mt) * BM;
-        n0 = (int)(id / mt % nt) * BN;
-        e = (int)(id / mt / nt % g.K);
-        split = (int)(id / mt / nt / g.K);
-        nv = g.N - n0 < BN ? g.N - n0 : BN;
-        const int first = g.off[e], all = g.off[e + 1] - first;
-        const int part = (all + g.splits * 32 - 1) / (g.splits * 32) * 32;
-        p0 = first + (split * part < all ? split * part : all);
-        Kx = first + all - p0 < part ? first + all - p0 : part;
-    } else {
-        const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
-        const int64_t left = g.n_tiles - grp * 8, wide = left < 8 ? left : 8;
-        const int2 t = g.tiles[grp * 8 + in % wide];
-        m0 = (int)(in / wide) * BM;
-        e = t.x;
-        if (e < 0) return;
-        p0 = t.y;
-        const int end = e < g.K ? g.off[e + 1] : g.N;
-        nv = end - p0 < BN ? end - p0 : BN;
-        Kx = e < g.K ? g.Kx : 0;
-    }
+    GroupPlace place;
+    if (!group_place_of<DIR, BM, BN, 32>(g, mt, place)) return;
+    const int e = place.e, m0 = place.m0, n0 = place.n0, nv = place.nv, split = place.split, p0 = place.p0, Kx = place.Kx;
     const int mv = g.M - m0 < BM ? g.M - m0 : BM;
     const bf16_t* zeros = (const bf16_t*)group_zeros;
     f4 acc[MI][NJ], accb[NJ];
@@ -672,7 +727,7 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) acc[i][j] = f4{0, 0, 0, 0};
     }
-    const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
+    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
     const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
 
     // Addresses of this thread's chunks (of the weight gradient's rows: what does not depend on k).  Rows and
@@ -681,7 +736,7 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
     int ka[UA], kb[UB];  // KC: k of the chunk in its stage; NC: the row's k
 #pragma unroll
     for (int u = 0; u < UA; ++u) {
-        const int s = u * 256 + tid, r = TA::row(s), c = TA::chunk(s) * 8;
+        const int s = u * THREADS + tid, r = TA::row(s), c = TA::chunk(s) * 8;
         ka[u] = DIR == GR_FWD ? c : r;
         const int rm = r < mv ? r : mv - 1, cm = c < mv ? c : mv - 8;
         pa[u] = (const bf16_t*)g.w + (DIR == GR_DW ? 0 : e * g.wnet) +
@@ -689,7 +744,7 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
     }
 #pragma unroll
     for (int u = 0; u < UB; ++u) {
-        const int s = u * 256 + tid, r = TB::row(s), c = TB::chunk(s) * 8;
+        const int s = u * THREADS + tid, r = TB::row(s), c = TB::chunk(s) * 8;
         kb[u] = DIR != GR_DW ? c : r;
         pb[u] = (const bf16_t*)g.p;
         if (DIR == GR_DW) pb[u] += n0 + (c < nv ? c : nv - 8);
@@ -721,7 +776,7 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
             if (DIR == GR_DW) q += (uint64_t)g.wdiv.of(na[u]) * (uint32_t)g.ldw;
             else pa[u] += step_a;
             if (!whole && k0 + ka[u] >= Kx) q = zeros;
-            copy_to_lds<16>(q, to + u * 4096);
+            copy_to_lds<16>(q, to + u * THREADS * 16);
         }
 #pragma unroll
         for (int u = 0; u < UB; ++u) {
@@ -729,7 +784,7 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
             if (DIR == GR_DW) q += (uint64_t)(uint32_t)nb[u] * (uint32_t)g.ldp;
             else pb[u] += 32;
             if (!whole && k0 + kb[u] >= Kx) q = zeros;
-            copy_to_lds<16>(q, to + TA::ELEMS * 2 + u * 4096);
+            copy_to_lds<16>(q, to + TA::ELEMS * 2 + u * THREADS * 16);
         }
     };
     auto fill = [&](int stage, int k0, int istage) {
@@ -752,42 +807,97 @@ __global__ __launch_bounds__(256, 2) void group_ring_kernel(GroupGemm g) {
             for (int t = 0; t < NST - 1; ++t) number(t, (IST + t) * 32);
         }
     }
-    for (int t = 0; t < steps; ++t) {
-        ring_wait<(NST - 2) * COPIES>();
-        const int next = at == 0 ? NST - 1 : at - 1;
-        fill(next, (t + NST - 1) * 32, nat);
+    constexpr int RA = DIR == GR_FWD ? 1 : 2, RB = DIR == GR_DW ? 2 : 1;  // reads of an operand
+    auto load_b = [&](bf8v (&fb)[NJ], int stage) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[j] = TB::frag(ring + stage * STAGE + TA::ELEMS, wn + 16 * j, lane);
+    };
+    auto load_a = [&](int stage, int i) { return TA::frag(ring + stage * STAGE, wm + 16 * i, lane); };
+    auto refill = [&](int t) {
+        fill(at == 0 ? NST - 1 : at - 1, (t + NST - 1) * 32, nat);
         if (DIR == GR_DW) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the numbers are read: their place is free)
             number(nat, (t + NST - 1 + IST) * 32);
             nat = nat == IST - 1 ? 0 : nat + 1;
         }
-        const bf16_t *la = ring + at * STAGE, *lb = la + TA::ELEMS;
-        bf8v fa[MI], fb[NJ];
+    };
+    auto add_bias = [&](const bf8v (&fb)[NJ]) {  // sums over k: a product with ones
+        if (!bias_rows) return;
+        const u4v ones = {0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80};
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) fb[j] = TB::frag(lb, wn + 16 * j, lane);
+        for (int j = 0; j < NJ; ++j)
+            accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, ones), fb[j], accb[j], 0, 0, 0);
+    };
+    if constexpr (AHEAD) {
+        // the operands of step t from registers (fb, fa: its first two blocks) and LDS, the next step's into fbn, fan
+        auto step = [&](int t, const bf8v (&fb)[NJ], const bf8v (&fa)[2], bf8v (&fbn)[NJ], bf8v (&fan)[2]) {
+            ring_wait<(NST - 3) * COPIES>();
+            refill(t);
+            const int next = at == NST - 1 ? 0 : at + 1;
+            bf8v f[MI];
+            f[0] = fa[0];
+            f[1] = fa[1];
 #pragma unroll
-        for (int i = 0; i < MI; ++i) fa[i] = TA::frag(la, wm + 16 * i, lane);
+            for (int i = 2; i < MI; ++i) f[i] = load_a(at, i);
+            load_b(fbn, next);
+            fan[0] = load_a(next, 0);
+            fan[1] = load_a(next, 1);
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+            for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        // reads two operands ahead of the products that take them
-        constexpr int RA = DIR == GR_FWD ? 1 : 2, RB = DIR == GR_DW ? 2 : 1;
-        __builtin_amdgcn_sched_group_barrier(0x100, RB * NJ + 2 * RA, 0);
+                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], fb[j], acc[i][j], 0, 0, 0);
+            // reads two operands ahead of the products that take them, the next step's with the last ones
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * RA, 0);
 #pragma unroll
-        for (int i = 0; i < MI - 2; ++i) {
+            for (int i = 0; i < MI - 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (RB * NJ + 2 * RA + 2) / 3, 0);
+            }
             __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+            add_bias(fb);
+            at = next;
+        };
+        bf8v fb[2][NJ], fa[2][2];
+        if (steps > 0) {
+            ring_wait<(NST - 2) * COPIES>();
+            load_b(fb[0], 0);
+            fa[0][0] = load_a(0, 0);
+            fa[0][1] = load_a(0, 1);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 2 * NJ, 0);
-        if (bias_rows) {  // sums over k: a product with ones
-            const uint32_t two = 0x3f803f80;
-            const u4v ones4 = {two, two, two, two};
+        int t = 0;
+        for (; t + 1 < steps; t += 2) {
+            step(t, fb[0], fa[0], fb[1], fa[1]);
+            step(t + 1, fb[1], fa[1], fb[0], fa[0]);
+        }
+        if (t < steps) step(t, fb[0], fa[0], fb[1], fa[1]);
+    } else {
+        for (int t = 0; t < steps; ++t) {
+            ring_wait<(NST - 2) * COPIES>();
+            refill(t);
+            bf8v fa[MI], fb[NJ];
+            load_b(fb, at);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, ones4), fb[j], accb[j], 0, 0, 0);
+            for (int i = 0; i < MI; ++i) fa[i] = load_a(at, i);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            // reads two operands ahead of the products that take them
+            __builtin_amdgcn_sched_group_barrier(0x100, RB * NJ + 2 * RA, 0);
+#pragma unroll
+            for (int i = 0; i < MI - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, NJ, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2 * NJ, 0);
+            add_bias(fb);
+            at = at == NST - 1 ? 0 : at + 1;
         }
-        at = at == NST - 1 ? 0 : at + 1;
     }
     ring_wait<0>();  // (no copy outlives its workgroup)
     group_store<DIR, bf16_t, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
@@ -857,9 +967,9 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + GS_OUT - 1) / GS_OUT;
     const int64_t id = blockIdx.x;
+    if (id >= (int64_t)*g.n_tiles * mt) return;
     const int2 t = g.tiles[id / mt];
     const int e = t.x, m0 = (int)(id % mt) * GS_OUT, p0 = t.y;
-    if (e < 0) return;
     const int end = e < g.K ? g.off[e + 1] : g.N;
     const int nv = end - p0 < 16 ? end - p0 : 16;
     f4 acc[GS_OUT / 16];
@@ -929,9 +1039,9 @@ __global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + BAND - 1) / BAND;
     const int64_t id = blockIdx.x;
+    if (id >= (int64_t)*g.n_tiles * mt) return;
     const int2 t = g.tiles[id / mt];
     const int e = t.x, m0 = (int)(id % mt) * BAND, p0 = t.y;
-    if (e < 0) return;
     const int end = e < g.K ? g.off[e + 1] : g.N;
     const int nv = end - p0 < 16 ? end - p0 : 16;
     f4 acc[C];

@@ -76,15 +76,13 @@ pnn_status check_act(int32_t act) {
     return PNN_OK;
 }
 
-GroupGemm group_base(const pnn_groups* g, bool few) {
+GroupGemm group_base(const pnn_groups* g) {
     const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
     const int32_t* w = (const int32_t*)g->plan_dev;
     GroupGemm a;
     memset(&a, 0, sizeof a);
     a.off = w;
     a.pairs = w + p.o_pairs;
-    a.tiles = (const int2*)(w + (few ? p.o_small : p.o_large));
-    a.n_tiles = few ? p.n_small : p.n_large;
     a.K = g->networks;
     a.N = (int)p.P;
     a.pdiv = a.wdiv = div_by(1);
@@ -93,8 +91,10 @@ GroupGemm group_base(const pnn_groups* g, bool few) {
     return a;
 }
 
-// Tiles of 16 pairs re-read the weights for each of them, tiles of 128 multiply what is not there.
-bool few_pairs(const pnn_groups* g) { return g->n * g->per_row <= 24 * (int64_t)g->networks; }
+pnn_status grid_fits(int64_t blocks) {
+    if (blocks > INT32_MAX) return fail(nullptr, PNN_ESHAPE, "%lld workgroups are more than a launch takes", (long long)blocks);
+    return PNN_OK;
+}
 
 // parts of a group's pairs in a weight gradient: with fewer workgroups than two per CU the groups
 // are split until there are as many, as long as a part keeps 512 pairs in the mean
@@ -105,52 +105,72 @@ int group_splits(int64_t P, int32_t K, int32_t inputs, int32_t outputs) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
 }
 
-pnn_status grid_fits(int64_t blocks) {
-    if (blocks > INT32_MAX) return fail(nullptr, PNN_ESHAPE, "%lld workgroups are more than a launch takes", (long long)blocks);
-    return PNN_OK;
-}
-
 // the ring kernels' copies: 16 bytes each, whole inside a row
 bool ring_ok(const void* p, int64_t ld, int64_t net, int width) {
     return aligned16(p) && ld % 8 == 0 && ld < (int64_t(1) << 31) && net % 8 == 0 && width % 8 == 0;
 }
 
-template <int DIR, typename TO>
-void launch_ring(const GroupGemm& a, int64_t others, hipStream_t s) {
-    constexpr int BM = 256, BN = 128, NST = 3;
-    const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? 4 * 2 * (NST - 1) * 256 : 0);
-    (void)hipFuncSetAttribute((const void*)group_ring_kernel<DIR, TO, BM, BN, NST>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    group_ring_kernel<DIR, TO, BM, BN, NST><<<(unsigned)((a.M + BM - 1) / BM * others), 256, lds, s>>>(a);
+template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
+pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
+    const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? WM * WN * 2 * (NST - 1) * 256 : 0);
+    TRY(grid_fits(blocks));
+    static std::atomic<uint64_t> set{0};  // devices on which this kernel may have that much LDS
+    int dev = 0;
+    (void)hipGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (!bit || !(set.load(std::memory_order_relaxed) & bit)) {
+        const hipError_t e = hipFuncSetAttribute((const void*)group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD>,
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return fail(nullptr, PNN_EHIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(e));
+        set.fetch_or(bit, std::memory_order_relaxed);
+    }
+    group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD><<<(unsigned)blocks, 64 * WM * WN, lds, s>>>(a);
+    return launched(DIR == GR_FWD ? "grouped forward" : DIR == GR_DX ? "grouped input gradient" : "grouped weight gradient");
+}
+
+enum { FEW = 0, TILE = 1, RING = 2, RING_HUGE = 3 };
+
+// Which kernel multiplies: tiles of 16 pairs re-read the weights for each of them, those of 128 and 256
+// multiply what is not there.
+int group_kind(const pnn_groups* g, bool ring) {
+    const int64_t mean = g->n * g->per_row / g->networks;
+    if (mean <= 24) return FEW;
+    if (!ring) return TILE;
+    return mean >= 512 ? RING_HUGE : RING;
 }
 
 template <int DIR, typename T, typename TO>
-pnn_status run_group_pairs(const GroupGemm& a, bool few, hipStream_t s) {
-    const int band = !few ? 128 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128;
-    const int64_t blocks = (a.M + band - 1) / band * a.n_tiles;
-    TRY(grid_fits(blocks));
-    if constexpr (sizeof(T) == 2)
-        if (!few && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx)) {
-            launch_ring<DIR, TO>(a, a.n_tiles, s);
-            return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
-        }
-    if (!few) group_tile_kernel<DIR, T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
-    else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
-    else group_few_dx_kernel<T, TO><<<(unsigned)blocks, 256, 0, s>>>(a);
+pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
+    const int kind = group_kind(g, sizeof(T) == 2 && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx));
+    const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
+    const int height = kind == FEW ? 0 : kind == RING_HUGE ? 2 : 1;
+    a.tiles = (const int2*)((const int32_t*)g->plan_dev + p.o_tiles[height]);
+    a.n_tiles = (const int32_t*)g->plan_dev + p.o_count + height;
+    auto blocks = [&](int band) { return (a.M + band - 1) / band * p.most[height]; };
+    if constexpr (sizeof(T) == 2) {
+        if (kind == RING_HUGE) return launch_ring<DIR, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
+        if (kind == RING) return launch_ring<DIR, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);
+    }
+    const int64_t all = blocks(kind == TILE ? 128 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
+    TRY(grid_fits(all));
+    if (kind == TILE) group_tile_kernel<DIR, T, TO><<<(unsigned)all, 256, 0, s>>>(a);
+    else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
+    else group_few_dx_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
     return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
 }
 
 template <int DIR>
-pnn_status run_group_pairs(const GroupGemm& a, int32_t type, int32_t out_type, bool few, hipStream_t s) {
+pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, int32_t type, int32_t out_type, hipStream_t s) {
     if (type == PNN_FP32)
-        return out_type == PNN_FP32 ? run_group_pairs<DIR, float, float>(a, few, s) : run_group_pairs<DIR, float, bf16_t>(a, few, s);
-    return out_type == PNN_FP32 ? run_group_pairs<DIR, bf16_t, float>(a, few, s) : run_group_pairs<DIR, bf16_t, bf16_t>(a, few, s);
+        return out_type == PNN_FP32 ? run_group_pairs<DIR, float, float>(a, g, s) : run_group_pairs<DIR, float, bf16_t>(a, g, s);
+    return out_type == PNN_FP32 ? run_group_pairs<DIR, bf16_t, float>(a, g, s) : run_group_pairs<DIR, bf16_t, bf16_t>(a, g, s);
 }
 
 // weight gradient (lr = 0), or the update y -= lr / pairs * gradient
 pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t outputs, int32_t type, const void* dy, int64_t dy_ld,
                              const void* x, int64_t x_ld, int xdiv, float* dw, int64_t dw_net, int64_t dw_ld, float* db,
                              int64_t db_net, float lr, bf16_t* shadow, void* ws, hipStream_t s) {
-    GroupGemm a = group_base(g, false);
+    GroupGemm a = group_base(g);
     const int S = group_splits((int64_t)g->n * g->per_row, g->networks, inputs, outputs);
     a.M = inputs; a.N = outputs;
     a.p = dy; a.ldp = dy_ld;
@@ -165,13 +185,20 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
         a.db = db; a.dbnet = db_net;
         a.lr = lr; a.shadow = shadow;
     }
-    const int64_t blocks = (int64_t)S * g->networks * ((inputs + 127) / 128) * ((outputs + 127) / 128);
-    TRY(grid_fits(blocks));
-    if (type == PNN_FP32) group_tile_kernel<GR_DW, float, float><<<(unsigned)blocks, 256, 0, s>>>(a);
-    else if (ring_ok(a.w, a.ldw, 0, a.M) && ring_ok(a.p, a.ldp, 0, a.N))
-        launch_ring<GR_DW, float>(a, (int64_t)S * g->networks * ((outputs + 127) / 128), s);
-    else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks, 256, 0, s>>>(a);
-    TRY(launched("grouped weight gradient"));
+    auto blocks = [&](int bm, int bn) {
+        return group_dw_blocks((int64_t)((inputs + bm - 1) / bm) * ((outputs + bn - 1) / bn), (int64_t)S * g->networks);
+    };
+    const int kind = group_kind(g, type != PNN_FP32 && ring_ok(x, x_ld, 0, inputs) && ring_ok(dy, dy_ld, 0, outputs));
+    if (kind == RING_HUGE) {
+        TRY((launch_ring<GR_DW, float, 256, 256, 2, 4, 4, true>(a, blocks(256, 256), s)));
+    } else if (kind == RING) {
+        TRY((launch_ring<GR_DW, float, 256, 128, 2, 2, 3, false>(a, blocks(256, 128), s)));
+    } else {
+        TRY(grid_fits(blocks(128, 128)));
+        if (type == PNN_FP32) group_tile_kernel<GR_DW, float, float><<<(unsigned)blocks(128, 128), 256, 0, s>>>(a);
+        else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks(128, 128), 256, 0, s>>>(a);
+        TRY(launched("grouped weight gradient"));
+    }
     if (S > 1) {
         GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, lr, shadow};
         const int64_t all = (int64_t)g->networks * outputs * (inputs + 1);
@@ -219,8 +246,8 @@ pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, in
     hipStream_t s = (hipStream_t)hip_stream;
     OnDeviceOf dev(s);
     int32_t* w = (int32_t*)plan_dev;
-    GroupArgs a = {ids_dev, w, w + p.o_pairs, w + p.o_hist, (int2*)(w + p.o_small), (int2*)(w + p.o_large),
-                   p.P, p.chunk, p.n_small, p.n_large, p.K, p.blocks};
+    GroupArgs a = {ids_dev, w, w + p.o_pairs, w + p.o_count, w + p.o_hist,
+                   {(int2*)(w + p.o_tiles[0]), (int2*)(w + p.o_tiles[1]), (int2*)(w + p.o_tiles[2])}, p.P, p.chunk, p.K, p.blocks};
     if (p.blocks > 1) {
         group_count_kernel<<<(unsigned)p.blocks, GR_THREADS, 0, s>>>(a);
         TRY(launched("counting the groups"));
@@ -239,15 +266,14 @@ pnn_status pnn_grouped_forward(const pnn_groups* groups, const pnn_group_layer* 
     TRY(check_rows("y_dev", y_dev, y_ld, layer->outputs, y_type));
     hipStream_t s = (hipStream_t)hip_stream;
     OnDeviceOf dev(s);
-    const bool few = few_pairs(groups);
-    GroupGemm a = group_base(groups, few);
+    GroupGemm a = group_base(groups);
     a.M = layer->outputs; a.Kx = layer->inputs;
     a.p = x_dev; a.ldp = x_ld; a.pdiv = div_by(groups->per_row);
     a.w = layer->w_dev; a.wnet = layer->w_net; a.ldw = layer->w_ld;
     a.b = layer->b_dev; a.bnet = layer->b_net;
     a.act = act;
     a.y = y_dev; a.ldy = y_ld;
-    return run_group_pairs<GR_FWD>(a, layer->type, y_type, few, s);
+    return run_group_pairs<GR_FWD>(a, groups, layer->type, y_type, s);
 }
 
 pnn_status pnn_grouped_workspace(const pnn_groups* groups, const pnn_group_layer* layer, int64_t* input_bytes,
@@ -273,18 +299,18 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     TRY(check_ws(ws_dev, ws_bytes, group_input_ws(groups, layer->inputs)));
     hipStream_t s = (hipStream_t)hip_stream;
     OnDeviceOf dev(s);
-    const bool few = few_pairs(groups), sum = groups->per_row > 1;
-    GroupGemm a = group_base(groups, few);
+    const bool sum = groups->per_row > 1;
+    GroupGemm a = group_base(groups);
     a.M = layer->inputs; a.Kx = layer->outputs;
     a.p = dy_dev; a.ldp = dy_ld;
     a.w = layer->w_dev; a.wnet = layer->w_net; a.ldw = layer->w_ld;
     if (!sum) {
         a.a = act >= 0 ? a_dev : nullptr; a.lda = a_ld; a.act = act;
         a.y = dx_dev; a.ldy = dx_ld;
-            return run_group_pairs<GR_DX>(a, layer->type, dx_type, few, s);
+            return run_group_pairs<GR_DX>(a, groups, layer->type, dx_type, s);
     }
     a.y = ws_dev; a.ldy = layer->inputs;
-    TRY(run_group_pairs<GR_DX>(a, layer->type, PNN_FP32, few, s));
+    TRY(run_group_pairs<GR_DX>(a, groups, layer->type, PNN_FP32, s));
     const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * layer->inputs + 255) / 256, 8192);
     const float* part = (const float*)ws_dev;
     const void* ad = act >= 0 ? a_dev : nullptr;

@@ -183,10 +183,10 @@ pnn_status pnn_train_routed(pnn_net* n, const float* x_dev, int64_t rows, const 
         DistillArgs a = distill_args(&d, stats, width);
         a.rows_per = per_row; a.ids = ids_dev; a.K = K;
         a.loss = loss_dev ? loss_dev : loss;
-        const bool two = a.wt != 0.0f && alpha > 0.0f && temperature != 1.0f;
-        TRY_NET(n, two ? (run_distill_loss<float, 2>(a, width, s)) : (run_distill_loss<float, 1>(a, width, s)));
+        const int mode = distill_mode(&d);
+        TRY_NET(n, run_distill_loss<float>(a, mode, width, s));
         a.dz = z; a.lddz = O;
-        TRY_NET(n, run_distill_grad<float>(a, width, s));
+        TRY_NET(n, run_distill_grad<float>(a, mode, width, s));
         if (n->bf16) {
             TRY_NET(n, grid_fits((P * O + 255) / 256));
             to_bf16_kernel<<<(unsigned)((P * O + 255) / 256), 256, 0, s>>>(z, (bf16_t*)err[0], P * O);

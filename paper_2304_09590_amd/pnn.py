@@ -7,6 +7,7 @@ is no fallback: if the compiled library is missing, importing the binding raises
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -321,72 +322,88 @@ class PNN:
             pass
 
 
-# ---- rows that name their network, without a handle (group_rows and the grouped products) ----
+# ---- calls without a handle: rows that name their network, distillation ----------------------
 
-def _call(fn, what: str, *args) -> None:
-    st = fn(*args)
+_torch = None
+
+
+def _t():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _call(what: str, *args) -> None:
+    st = getattr(lib(), what)(*args)
     if st != PNN_OK:
         raise PnnError(st, f"{what}: {lib().pnn_last_error(None).decode()}")
 
 
-class _On:
-    """The device of a call's tensors made current, with the call's stream current for allocations."""
-
-    def __init__(self, tensors, stream):
-        import torch
-        given = [t for t in tensors if t is not None]
-        for t in given:
-            if not t.is_cuda:
-                raise ValueError(f"expected CUDA tensors, got one on {t.device}")
-            if t.device != given[0].device:
-                raise ValueError(f"tensors on {given[0].device} and on {t.device}")
-        self.device = given[0].device
-        if stream is not None and not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream, device=self.device)
-        if stream is not None and stream.device != self.device:
-            raise ValueError(f"a stream of {stream.device} for tensors on {self.device}")
-        self._given = stream
-        self._contexts = []
-
-    def __enter__(self):
-        import torch
-        if torch.cuda.current_device() != self.device.index:
-            self._contexts.append(torch.cuda.device(self.device))
-        if self._given is not None:
-            self._contexts.append(torch.cuda.stream(self._given))
-        for c in self._contexts:
-            c.__enter__()
-        self.stream = torch.cuda.current_stream().cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        for c in reversed(self._contexts):
-            c.__exit__(*exc)
+def _on(stream, body, first, *others):
+    """body(stream handle) with the tensors' device current and, for allocations, the stream; the tensors have to
+    be on one GPU."""
+    torch = _t()
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError(f"expected CUDA tensors, got one on {first.device}")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {first.device} and on {t.device}")
+    if stream is None and torch._C._cuda_getDevice() == dev:
+        return body(torch._C._cuda_getCurrentRawStream(dev))
+    with torch.cuda.device(dev):
+        if stream is None:
+            return body(torch._C._cuda_getCurrentRawStream(dev))
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream, device=first.device)
+        if stream.device != first.device:
+            raise ValueError(f"a stream of {stream.device} for tensors on {first.device}")
+        with torch.cuda.stream(stream):
+            return body(stream.cuda_stream)
 
 
 def _type_of(t) -> int:
-    code = {"torch.float32": FP32, "torch.bfloat16": BF16_MIXED}.get(str(t.dtype))
-    if code is None:
-        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    return code
+    torch = _t()
+    if t.dtype is torch.float32:
+        return FP32
+    if t.dtype is torch.bfloat16:
+        return BF16_MIXED
+    raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
 
 
-def _rows(t, name: str, shape, dtype=None):
-    """(pointer, distance between rows) of a matrix whose rows' values are contiguous."""
-    if tuple(t.shape) != tuple(shape):
+def _rows(t, name: str, shape, dtype):
+    """(pointer, distance between rows) of a matrix (or a stack of matrices) whose rows' values are contiguous."""
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if dtype is not None and t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"the values of a row of {name} are not contiguous")
-    ld = t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
-    return t.data_ptr(), ld
+    return t.data_ptr(), (strides[-2] if shape[-2] > 1 else shape[-1])
 
 
 def _values(t, name: str, shape, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} is {tuple(t.shape)} of {t.dtype}, expected {tuple(shape)} of {dtype}, contiguous")
     return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_bytes(n: int, per_row: int, networks: int) -> int:
+    size = ctypes.c_int64()
+    _call("pnn_group_bytes", n, per_row, networks, ctypes.byref(size))
+    return size.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_workspace(n: int, per_row: int, networks: int, inputs: int, outputs: int, dtype: int) -> Tuple[int, int]:
+    one, two = ctypes.c_int64(), ctypes.c_int64()
+    groups, layer = PnnGroups(None, n, per_row, networks), PnnGroupLayer(inputs, outputs, dtype, None, 0, 0, None, 0)
+    _call("pnn_grouped_workspace", ctypes.byref(groups), ctypes.byref(layer), ctypes.byref(one), ctypes.byref(two))
+    return one.value, two.value
 
 
 class RowGroups:
@@ -410,141 +427,148 @@ class RowGroups:
 
 def group_rows(ids, networks: int, stream=None) -> RowGroups:
     """Group rows by network: ids int32 [n] or [n, per_row], an id outside [0, networks) drops the pair."""
-    import torch
-    if str(ids.dtype) != "torch.int32" or ids.dim() not in (1, 2) or not ids.is_contiguous():
-        raise ValueError(f"ids: expected contiguous int32 [n] or [n, per_row], got {tuple(ids.shape)} of {ids.dtype}")
-    n, per_row = ids.shape[0], (ids.shape[1] if ids.dim() == 2 else 1)
-    with _On([ids], stream) as on:
-        size = ctypes.c_int64()
-        _call(lib().pnn_group_bytes, "pnn_group_bytes", n, per_row, networks, ctypes.byref(size))
-        plan = torch.empty(size.value // 4, dtype=torch.int32, device=on.device)
-        _call(lib().pnn_group_rows, "pnn_group_rows", ids.data_ptr(), n, per_row, networks, plan.data_ptr(), size.value,
-              on.stream)
-    return RowGroups(plan, n, per_row, networks)
+    torch = _t()
+    shape = ids.shape
+    if ids.dtype is not torch.int32 or len(shape) not in (1, 2) or not ids.is_contiguous():
+        raise ValueError(f"ids: expected contiguous int32 [n] or [n, per_row], got {tuple(shape)} of {ids.dtype}")
+    n, per_row = shape[0], (shape[1] if len(shape) == 2 else 1)
+
+    def body(s):
+        size = _group_bytes(n, per_row, networks)
+        plan = torch.empty(size // 4, dtype=torch.int32, device=ids.device)
+        _call("pnn_group_rows", ids.data_ptr(), n, per_row, networks, plan.data_ptr(), size, s)
+        return plan
+
+    return RowGroups(_on(stream, body, ids), n, per_row, networks)
 
 
 def _weights(groups: RowGroups, w, b=None) -> PnnGroupLayer:
-    import torch
-    if w.dim() != 3 or w.shape[0] != groups.networks:
-        raise ValueError(f"w has shape {tuple(w.shape)}, expected ({groups.networks}, outputs, inputs)")
-    ptr, ld = _rows(w, "w", w.shape)
-    layer = PnnGroupLayer(w.shape[2], w.shape[1], _type_of(w), ptr, w.stride(0), ld, None, 0)
+    shape = w.shape
+    if len(shape) != 3 or shape[0] != groups.networks:
+        raise ValueError(f"w has shape {tuple(shape)}, expected ({groups.networks}, outputs, inputs)")
+    ptr, ld = _rows(w, "w", shape, w.dtype)
+    layer = PnnGroupLayer(shape[2], shape[1], _type_of(w), ptr, w.stride(0), ld, None, 0)
     if b is not None:
-        layer.b, layer.b_net = _rows(b, "b", w.shape[:2], torch.float32)
+        layer.b, layer.b_net = _rows(b, "b", shape[:2], _t().float32)
     return layer
 
 
 def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, out=None, out_dtype=None, stream=None):
     """y[p] = act(w[e] x[p // per_row] + b[e]) for every pair p of network e; dropped pairs give 0.
     x [n, inputs], w [networks, outputs, inputs] of x's type (float32 or bfloat16), b fp32."""
-    import torch
     layer = _weights(groups, w, b)
-    with _On([groups.plan, x, w, b, out], stream) as on:
+    shape = (groups.n * groups.per_row, layer.outputs)
+
+    def body(s):
+        y = out if out is not None else _t().empty(shape, dtype=out_dtype or x.dtype, device=x.device)
         px, ldx = _rows(x, "x", (groups.n, layer.inputs), w.dtype)
-        shape = (groups.n * groups.per_row, layer.outputs)
-        if out is None:
-            out = torch.empty(shape, dtype=out_dtype or x.dtype, device=on.device)
-        py, ldy = _rows(out, "out", shape, out_dtype)
-        _call(lib().pnn_grouped_forward, "pnn_grouped_forward", ctypes.byref(groups.struct), ctypes.byref(layer), px, ldx,
-              -1 if act is None else act, py, ldy, _type_of(out), on.stream)
-    return out
+        py, ldy = _rows(y, "out", shape, out_dtype or y.dtype)
+        _call("pnn_grouped_forward", ctypes.byref(groups.struct), ctypes.byref(layer), px, ldx, -1 if act is None else act,
+              py, ldy, _type_of(y), s)
+        return y
+
+    return _on(stream, body, x, groups.plan, w, b, out)
 
 
-def _workspace(groups, layer, on, which: int):
-    import torch
-    size = (ctypes.c_int64(), ctypes.c_int64())
-    _call(lib().pnn_grouped_workspace, "pnn_grouped_workspace", ctypes.byref(groups.struct), ctypes.byref(layer),
-          ctypes.byref(size[0]), ctypes.byref(size[1]))
-    if size[which].value == 0:
+def _workspace(groups: RowGroups, layer: PnnGroupLayer, device, which: int):
+    size = _group_workspace(groups.n, groups.per_row, groups.networks, layer.inputs, layer.outputs, layer.type)[which]
+    if size == 0:
         return None, None, 0
-    ws = torch.empty(size[which].value, dtype=torch.uint8, device=on.device)
-    return ws, ws.data_ptr(), size[which].value
+    ws = _t().empty(size, dtype=_t().uint8, device=device)
+    return ws, ws.data_ptr(), size
 
 
 def grouped_backward_input(groups: RowGroups, dy, w, a=None, act: Optional[int] = None, out=None, out_dtype=None,
                            stream=None):
     """dx[r] = (sum over row r's pairs of w[e]^T dy[pair]) * act'(a[r]) (the slope from stored activations)."""
-    import torch
     layer = _weights(groups, w)
-    with _On([groups.plan, dy, w, a, out], stream) as on:
+    shape = (groups.n, layer.inputs)
+    if (a is None) != (act is None):
+        raise ValueError("a and act go together")
+
+    def body(s):
+        dx = out if out is not None else _t().empty(shape, dtype=out_dtype or dy.dtype, device=dy.device)
         pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), w.dtype)
-        shape = (groups.n, layer.inputs)
-        if (a is None) != (act is None):
-            raise ValueError("a and act go together")
         pa, lda = _rows(a, "a", shape, w.dtype) if a is not None else (None, 0)
-        if out is None:
-            out = torch.empty(shape, dtype=out_dtype or dy.dtype, device=on.device)
-        po, ldo = _rows(out, "out", shape, out_dtype)
-        ws, pw, size = _workspace(groups, layer, on, 0)
-        _call(lib().pnn_grouped_backward_input, "pnn_grouped_backward_input", ctypes.byref(groups.struct),
-              ctypes.byref(layer), pd, ldd, pa, lda, -1 if act is None else act, po, ldo, _type_of(out), pw, size, on.stream)
-    return out
+        po, ldo = _rows(dx, "out", shape, out_dtype or dx.dtype)
+        ws, pw, size = _workspace(groups, layer, dy.device, 0)
+        _call("pnn_grouped_backward_input", ctypes.byref(groups.struct), ctypes.byref(layer), pd, ldd, pa, lda,
+              -1 if act is None else act, po, ldo, _type_of(dx), pw, size, s)
+        return dx
+
+    return _on(stream, body, dy, groups.plan, w, a, out)
 
 
 def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: bool = True, stream=None):
     """(dw, db): dw[e] = sum over network e's pairs of dy[p] x[p // per_row]^T and db[e] = sum of dy[p], fp32;
     zeros for a network without pairs; bias=False leaves db out (None)."""
-    import torch
+    torch = _t()
     if dy.dim() != 2 or x.dim() != 2:
         raise ValueError("dy and x are matrices")
     layer = PnnGroupLayer(x.shape[1], dy.shape[1], _type_of(x), None, 0, 0, None, 0)
-    with _On([groups.plan, dy, x, dw, db], stream) as on:
+    shape = (groups.networks, layer.outputs, layer.inputs)
+
+    def body(s):
+        w = dw if dw is not None else torch.empty(shape, dtype=torch.float32, device=x.device)
+        b = db if db is not None or not bias else torch.empty(shape[:2], dtype=torch.float32, device=x.device)
         pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), x.dtype)
-        px, ldx = _rows(x, "x", (groups.n, layer.inputs))
-        f32 = torch.float32
-        if dw is None:
-            dw = torch.empty((groups.networks, layer.outputs, layer.inputs), dtype=f32, device=on.device)
-        if db is None and bias:
-            db = torch.empty((groups.networks, layer.outputs), dtype=f32, device=on.device)
-        pw, ldw = _rows(dw, "dw", (groups.networks, layer.outputs, layer.inputs), f32)
-        pb, netb = _rows(db, "db", (groups.networks, layer.outputs), f32) if db is not None else (None, 0)
-        ws, ps, size = _workspace(groups, layer, on, 1)
-        _call(lib().pnn_grouped_backward_weights, "pnn_grouped_backward_weights", ctypes.byref(groups.struct),
-              ctypes.byref(layer), pd, ldd, px, ldx, pw, dw.stride(0), ldw, pb, netb, ps, size, on.stream)
-    return dw, db
+        px, ldx = _rows(x, "x", (groups.n, layer.inputs), x.dtype)
+        pw, ldw = _rows(w, "dw", shape, torch.float32)
+        pb, netb = _rows(b, "db", shape[:2], torch.float32) if b is not None else (None, 0)
+        ws, ps, size = _workspace(groups, layer, x.device, 1)
+        _call("pnn_grouped_backward_weights", ctypes.byref(groups.struct), ctypes.byref(layer), pd, ldd, px, ldx, pw,
+              w.stride(0), ldw, pb, netb, ps, size, s)
+        return w, b
+
+    return _on(stream, body, x, groups.plan, dy, dw, db)
 
 
-# ---- distillation from a teacher's top logits, without a handle ------------------------------
+@functools.lru_cache(maxsize=1024)
+def _distill_bytes(n: int, classes: int) -> int:
+    size = ctypes.c_int64()
+    _call("pnn_distill_bytes", n, classes, ctypes.byref(size))
+    return size.value
+
 
 def _distill(z, idx, t, y, temperature, alpha) -> PnnDistill:
-    import torch
+    torch = _t()
     if z.dim() != 2:
         raise ValueError(f"z has shape {tuple(z.shape)}, expected a matrix")
     n, top = z.shape[0], (idx.shape[-1] if idx is not None else 0)
-    pz, ldz = _rows(z, "z", z.shape)
-    a = PnnDistill(pz, ldz, _type_of(z), z.shape[1], n, None, None, top, None, temperature, alpha)
-    if idx is not None:
-        a.idx, a.t = _values(idx, "idx", (n, top), torch.int32), _values(t, "t", (n, top), z.dtype)
-    if y is not None:
-        a.y = _values(y, "y", (n,), torch.int32)
-    return a
+    pz, ldz = _rows(z, "z", z.shape, z.dtype)
+    return PnnDistill(pz, ldz, _type_of(z), z.shape[1], n, None if idx is None else _values(idx, "idx", (n, top), torch.int32),
+                      None if idx is None else _values(t, "t", (n, top), z.dtype), top,
+                      None if y is None else _values(y, "y", (n,), torch.int32), temperature, alpha)
 
 
 def distill_loss(z, idx, t, y=None, temperature: float = 1.0, alpha: float = 0.0, stream=None):
     """(loss [n] fp32, stats for distill_grad) of logits z [n, classes] against the teacher's entries: classes
     idx int32 [n, top], logits t [n, top] of z's type; labels y int32 [n] weigh alpha (see pnn_distill in pnn.h)."""
-    import torch
+    torch = _t()
     a = _distill(z, idx, t, y, temperature, alpha)
-    with _On([z, idx, t, y], stream) as on:
-        size = ctypes.c_int64()
-        _call(lib().pnn_distill_bytes, "pnn_distill_bytes", a.n, a.classes, ctypes.byref(size))
-        loss = torch.empty(a.n, dtype=torch.float32, device=on.device)
-        stats = torch.empty(size.value // 4, dtype=torch.float32, device=on.device)
-        _call(lib().pnn_distill_loss, "pnn_distill_loss", ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), size.value,
-              on.stream)
-    return loss, stats
+
+    def body(s):
+        size = _distill_bytes(a.n, a.classes)
+        loss = torch.empty(a.n, dtype=torch.float32, device=z.device)
+        stats = torch.empty(size // 4, dtype=torch.float32, device=z.device)
+        _call("pnn_distill_loss", ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), size, s)
+        return loss, stats
+
+    return _on(stream, body, z, idx, t, y)
 
 
 def distill_grad(z, idx, t, stats, g=None, y=None, temperature: float = 1.0, alpha: float = 0.0, out=None, stream=None):
     """The gradient of z from distill_loss's arguments and statistics; g fp32 [n] is the gradient of each row's
     loss (None: 1).  out may be z."""
-    import torch
+    torch = _t()
     a = _distill(z, idx, t, y, temperature, alpha)
-    with _On([z, idx, t, stats, g, y, out], stream) as on:
+
+    def body(s):
+        dz = out if out is not None else torch.empty(z.shape, dtype=z.dtype, device=z.device)
         pg = _values(g, "g", (a.n,), torch.float32) if g is not None else None
         ps = _values(stats, "stats", stats.shape, torch.float32)
-        if out is None:
-            out = torch.empty(z.shape, dtype=z.dtype, device=on.device)
-        po, ldo = _rows(out, "out", z.shape, z.dtype)
-        _call(lib().pnn_distill_grad, "pnn_distill_grad", ctypes.byref(a), pg, ps, 4 * stats.numel(), po, ldo, on.stream)
-    return out
+        po, ldo = _rows(dz, "out", z.shape, z.dtype)
+        _call("pnn_distill_grad", ctypes.byref(a), pg, ps, 4 * stats.numel(), po, ldo, s)
+        return dz
+
+    return _on(stream, body, z, idx, t, stats, g, y, out)
