@@ -112,71 +112,100 @@ __device__ inline void dl_join(Sums& s, float m, float a, float b, const Distill
     if (MODE != 1) s.b += o.b;
 }
 
-template <int MODE, int G>
-__device__ inline void dl_join_lanes(Sums& s, const DistillArgs& d) {
-#pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) {
-        const float m = __shfl_xor(s.m, o), a = __shfl_xor(s.a, o), b = MODE != 1 ? __shfl_xor(s.b, o) : 0.0f;
-        dl_join<MODE>(s, m, a, b, d);
-    }
-}
-
+// over G = 16 or 64 lanes: by DPP within the rows of 16, the four rows by two exchanges
 template <int G> __device__ inline float dl_max(float v) {
-#pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    v = row_allmax16(v);
+    if (G == 64) {
+        v = fmaxf(v, __shfl_xor(v, 16));
+        v = fmaxf(v, __shfl_xor(v, 32));
+    }
     return v;
 }
 template <int G> __device__ inline float dl_sum(float v) {
-#pragma unroll
-    for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    v = row_allsum16(v);
+    if (G == 64) {
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+    }
     return v;
 }
 
-// The teacher's distribution of a row, as G lanes see it: maximum and sum of the entries'
-// exponentials.  A sum of 0: the row has no entries (or only ones of -inf).
-struct Teacher { float ref, mass; };
-
-template <typename T, int G>
-__device__ inline Teacher dl_teacher(const DistillArgs& d, int64_t row, int lane) {
-    const int32_t* idx = d.idx + row / d.rows_per * d.k;
-    const T* t = (const T*)d.t + row / d.rows_per * d.k;
-    float m = -DL_INF;
-    for (int j = lane; j < d.k; j += G)
-        if ((unsigned)idx[j] < (unsigned)d.V) m = fmaxf(m, to_f<T>(t[j]));
-    m = dl_max<G>(m);
-    const float ref = m == -DL_INF ? 0.0f : m;
-    float s = 0.0f;
-    for (int j = lane; j < d.k; j += G)
-        if ((unsigned)idx[j] < (unsigned)d.V) s += exp2f((to_f<T>(t[j]) - ref) * d.ct);
-    return {ref, dl_sum<G>(s)};
+template <int MODE, int G>
+__device__ inline void dl_join_lanes(Sums& s, const DistillArgs& d) {
+    const float m = dl_max<G>(s.m);
+    if (m > s.m) dl_move<MODE>(s, m, d);
+    s.a = dl_sum<G>(s.a);
+    if (MODE != 1) s.b = dl_sum<G>(s.b);
 }
 
-// loss and statistics of a row from its sums, by G lanes
-template <typename T, int G>
-__device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, const Teacher& te, int has, const Sums& s, bool two) {
-    const T* z = (const T*)d.z + row * d.ldz;
+// The teacher's distribution of a row, as a wave sees it: maximum and sum of the entries' exponentials, and
+// the lane's first entry with the student's logit there.  A sum of 0: no entries, or only ones of -inf.
+template <typename T>
+struct Teacher {
+    float ref = 0.0f, mass = 0.0f, t, z;
+    int i = -1;
+    const int32_t* idx;
+    const T *ts, *zs;
+
+    __device__ inline void load(const DistillArgs& d, int64_t row, int lane, bool logits) {
+        idx = d.idx + row / d.rows_per * d.k;
+        ts = (const T*)d.t + row / d.rows_per * d.k;
+        zs = (const T*)d.z + row * d.ldz;
+        if (d.wt == 0.0f) return;
+        if (lane < d.k) {
+            i = idx[lane];
+            t = to_f<T>(ts[lane]);
+            if ((unsigned)i >= (unsigned)d.V) i = -1;
+            if (logits && i >= 0) z = to_f<T>(zs[i]);
+        }
+    }
+    __device__ inline bool entry(const DistillArgs& d, int j, int& at, float& value) const {
+        at = idx[j];
+        value = to_f<T>(ts[j]);
+        return (unsigned)at < (unsigned)d.V;
+    }
+    __device__ inline void sum(const DistillArgs& d, int lane) {
+        if (d.wt == 0.0f) return;
+        float m = i >= 0 ? t : -DL_INF, v;
+        int at;
+        for (int j = lane + 64; j < d.k; j += 64)
+            if (entry(d, j, at, v)) m = fmaxf(m, v);
+        m = dl_max<64>(m);
+        ref = m == -DL_INF ? 0.0f : m;
+        float s = i >= 0 ? exp2f((t - ref) * d.ct) : 0.0f;
+        for (int j = lane + 64; j < d.k; j += 64)
+            if (entry(d, j, at, v)) s += exp2f((v - ref) * d.ct);
+        mass = dl_sum<64>(s);
+    }
+};
+
+constexpr float DL_LN2 = 0.6931471806f;
+
+// loss and statistics of a row from its sums, by a wave
+template <typename T>
+__device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, const Teacher<T>& te, int has, const Sums& s, bool two) {
     const float la = logf(s.a), lb = two ? logf(s.b) : la;
-    constexpr float LN2 = 0.6931471806f;
     const Ref f = dl_ref(s.m, d);
     float kl = 0.0f;
     if (has & 1) {
-        const int32_t* idx = d.idx + row / d.rows_per * d.k;
-        const T* t = (const T*)d.t + row / d.rows_per * d.k;
         const float lm = logf(te.mass), im = 1.0f / te.mass;
-        for (int j = lane; j < d.k; j += G) {
-            const int i = idx[j];
-            if ((unsigned)i >= (unsigned)d.V) continue;
-            const float e = to_f<T>(t[j]) - te.ref, p = exp2f(e * d.ct) * im;
-            if (p == 0.0f) continue;  // an entry without weight, whatever the student gives it
-            kl += p * ((e * d.inv_t - lm) - (dl_t(to_f<T>(z[i]), f, d) * LN2 - la));
-        }
+        auto term = [&](float t, float z) {
+            const float e = t - te.ref, p = exp2f(e * d.ct) * im;
+            // (an entry without weight counts nothing, whatever the student gives it)
+            return p == 0.0f ? 0.0f : p * ((e * d.inv_t - lm) - (dl_t(z, f, d) * DL_LN2 - la));
+        };
+        if (te.i >= 0) kl = term(te.t, te.z);
+        float t;
+        int at;
+        for (int j = lane + 64; j < d.k; j += 64)
+            if (te.entry(d, j, at, t)) kl += term(t, to_f<T>(te.zs[at]));
     }
-    kl = dl_sum<G>(kl);
+    kl = dl_sum<64>(kl);
     if (lane != 0) return;
     float loss = 0.0f;
     if (s.a == 0.0f) has = 0;  // every logit is -inf: nothing to learn from
     if (has & 1) loss += d.wt * kl;
-    if (has & 2) loss += d.ws * (lb - dl_s(to_f<T>(z[d.y[row / d.rows_per]]), f, d) * LN2);
+    if (has & 2) loss += d.ws * (lb - dl_s(to_f<T>(te.zs[d.y[row / d.rows_per]]), f, d) * DL_LN2);
     d.loss[row] = loss;
     d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (two ? s.b : s.a), (float)has);
 }
@@ -188,9 +217,9 @@ __device__ inline int dl_label(const DistillArgs& d, int64_t row) {
 }
 
 // what a row learns from (bit 0 entries, bit 1 a label)
-__device__ inline int dl_has(const DistillArgs& d, int64_t row, const Teacher& te) {
+__device__ inline int dl_has(const DistillArgs& d, int64_t row, float mass) {
     if (d.ids && (unsigned)d.ids[row] >= (unsigned)d.K) return 0;
-    return (te.mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
+    return (mass == 0.0f ? 0 : 1) | (dl_label(d, row) >= 0 ? 2 : 0);
 }
 
 // dz of one value
@@ -222,29 +251,46 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
     const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
-    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = dl_has(d, row, te);
-    if (has == 0) {  // a padding row: its logits are not read
-        if (in == 0 && part == 0) {
-            d.loss[row] = 0.0f;
-            d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-        return;
-    }
     const T* z = (const T*)d.z + row * d.ldz;
     const int64_t lo = (int64_t)part * d.part;
     const int len = (int)(d.V - lo < d.part ? d.V - lo : d.part);
+    Teacher<T> te;
+    int has = 3;
+    if (W != 4 || d.S == 1) {  // (the parts of a row are summed whatever it has)
+        te.load(d, row, lane, true);
+        te.sum(d, lane);
+        has = dl_has(d, row, te.mass);
+        if (has == 0) {  // a padding row: its logits do not matter
+            if (in == 0) {
+                d.loss[row] = 0.0f;
+                d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            return;
+        }
+    }
     Sums s = {-DL_INF, 0.0f, 0.0f};
-    // (the next two loads are in flight while a value is added)
+    // sixteen values at a time, the next ones in flight; then what is left, eight at a time
+    constexpr int LEAP = W * 512;
     int v = in * 8;
-    Raw8<T> r[2];
-    load8(r[0], z + lo + v, len - v);
-    load8(r[1], z + lo + v + W * 512, len - v - W * 512);
-    for (; v < len; v += W * 512) {
+    const int pairs = len - v - 8 - LEAP >= 0 ? (len - v - 8 - LEAP) / (2 * LEAP) + 1 : 0;
+    Raw8<T> r0, r1;
+    if (pairs > 0) {
+        load8(r0, z + lo + v, 8);
+        load8(r1, z + lo + v + LEAP, 8);
+    }
+    for (int it = 0; it < pairs; ++it, v += 2 * LEAP) {
+        float x[16];
+        raw8_f(*(float(*)[8])x, r0);
+        raw8_f(*(float(*)[8])(x + 8), r1);
+        if (it + 1 < pairs) {
+            load8(r0, z + lo + v + 2 * LEAP, 8);
+            load8(r1, z + lo + v + 3 * LEAP, 8);
+        }
+        dl_add<MODE>(s, x, d);
+    }
+    for (; v < len; v += LEAP) {
         float x[8];
-        raw8_f(x, r[0]);
-        r[0] = r[1];
-        load8(r[1], z + lo + v + W * 1024, len - v - W * 1024);
+        load8_f<T>(x, z + lo + v, len - v);
         if (len - v < 8) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = i < len - v ? x[i] : -DL_INF;
@@ -263,7 +309,7 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
             return;
         }
     }
-    dl_finish<T, 64>(d, row, lane, te, has, s, MODE != 1);
+    dl_finish<T>(d, row, lane, te, has, s, MODE != 1);
 }
 
 // joins the parts of a row, one wave a row
@@ -271,16 +317,24 @@ template <typename T, int MODE>
 __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x;
-    const Teacher te = d.wt != 0.0f ? dl_teacher<T, 64>(d, row, lane) : Teacher{0.0f, 0.0f};
-    const int has = dl_has(d, row, te);
-    if (has == 0) return;  // (written with the parts)
+    Teacher<T> te;
+    te.load(d, row, lane, true);
     Sums s = {-DL_INF, 0.0f, 0.0f};
     for (int p = lane; p < d.S; p += 64) {
         const float4 v = d.parts[row * d.S + p];
         dl_join<MODE>(s, v.x, v.y, v.z, d);
     }
+    te.sum(d, lane);
+    const int has = dl_has(d, row, te.mass);
+    if (has == 0) {  // a padding row, whatever its logits
+        if (lane == 0) {
+            d.loss[row] = 0.0f;
+            d.stats[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+        return;
+    }
     dl_join_lanes<MODE, 64>(s, d);
-    dl_finish<T, 64>(d, row, lane, te, has, s, MODE != 1);
+    dl_finish<T>(d, row, lane, te, has, s, MODE != 1);
 }
 
 // Gradient, W waves a row or one part of a row per workgroup.  The entries' classes (and the label)
@@ -291,8 +345,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     __shared__ int sidx[4 / W][TOP];
     __shared__ float sp[4 / W][TOP], sz[4 / W][TOP + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    // (the last rows first: the loss has read them last, and what still is in the caches is theirs)
-    const int64_t row = W == 4 ? d.n - 1 - (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
     const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0, slot = W == 4 ? 0 : wave;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
@@ -316,14 +369,17 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     const int label = has & 2 ? dl_label(d, row) : -1;
     const int k = has & 1 ? d.k : 0;
     if (has & 1) {
-        const Teacher te = dl_teacher<T, 64>(d, row, lane);
+        Teacher<T> te;
+        te.load(d, row, lane, false);
+        te.sum(d, lane);
         const float im = 1.0f / te.mass;
-        const int64_t first = row / d.rows_per * d.k;
         for (int j = in; j < k; j += 64 * W) {
-            const int i = d.idx[first + j];
+            float t;
+            int i;
+            te.entry(d, j, i, t);
             const bool mine = i >= lo && i < hi;
             sidx[slot][j] = mine ? i : -1;
-            sp[slot][j] = mine ? exp2f((to_f<T>(((const T*)d.t)[first + j]) - te.ref) * d.ct) * im : 0.0f;
+            sp[slot][j] = mine ? exp2f((t - te.ref) * d.ct) * im : 0.0f;
             sz[slot][j] = mine ? to_f<T>(z[i]) : 0.0f;
         }
     }
@@ -367,9 +423,8 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
 // Few classes: 16 lanes a row, NZ values of z and one entry a lane in registers.
 template <typename T, int NZ>
 struct Tiny {
-    float z[NZ], t;
+    float z[NZ], t, ref, mass;
     int i, label;
-    Teacher te;
 
     __device__ inline float logit(int v) const {  // of class v, by all lanes of the row
         float r = 0.0f;
@@ -398,8 +453,8 @@ struct Tiny {
         }
         if ((unsigned)label >= (unsigned)d.V) label = -1;
         const float m = dl_max<16>(t);
-        te.ref = m == -DL_INF ? 0.0f : m;
-        te.mass = dl_sum<16>(i >= 0 ? exp2f((t - te.ref) * d.ct) : 0.0f);
+        ref = m == -DL_INF ? 0.0f : m;
+        mass = dl_sum<16>(i >= 0 ? exp2f((t - ref) * d.ct) : 0.0f);
     }
 };
 
@@ -410,12 +465,15 @@ __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
     if (row >= d.n) return;
     Tiny<T, NZ> r;
     r.load(d, row, lane);
-    int has = (r.te.mass == 0.0f ? 0 : 1) | (r.label >= 0 ? 2 : 0);
+    int has = (r.mass == 0.0f ? 0 : 1) | (r.label >= 0 ? 2 : 0);
     if (d.ids && (unsigned)d.ids[row] >= (unsigned)d.K) has = 0;
-    Sums s = {-DL_INF, 0.0f, 0.0f};
+    float top = r.z[0];
+#pragma unroll
+    for (int k = 1; k < NZ; ++k) top = fmaxf(top, r.z[k]);
+    Sums s = {dl_max<16>(top), 0.0f, 0.0f};
     dl_add<MODE>(s, r.z, d);
-    dl_join_lanes<MODE, 16>(s, d);
-    constexpr float LN2 = 0.6931471806f;
+    s.a = dl_sum<16>(s.a);
+    if (MODE != 1) s.b = dl_sum<16>(s.b);
     const Ref f = dl_ref(s.m, d);
     const float la = logf(s.a), lb = MODE != 1 ? logf(s.b) : la;
     const int at = r.i >= 0 ? r.i : 0;
@@ -428,15 +486,15 @@ __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
     const float zy = r.logit(r.label >= 0 ? r.label : 0);
     float kl = 0.0f;
     if (r.i >= 0) {
-        const float e = r.t - r.te.ref, p = exp2f(e * d.ct) / r.te.mass;
-        if (p != 0.0f) kl = p * ((e * d.inv_t - logf(r.te.mass)) - (dl_t(zi, f, d) * LN2 - la));
+        const float e = r.t - r.ref, p = exp2f(e * d.ct) / r.mass;
+        if (p != 0.0f) kl = p * ((e * d.inv_t - logf(r.mass)) - (dl_t(zi, f, d) * DL_LN2 - la));
     }
     kl = dl_sum<16>(kl);
     if (lane != 0) return;
     if (s.a == 0.0f) has = 0;  // every logit is -inf
     float loss = 0.0f;
     if (has & 1) loss += d.wt * kl;
-    if (has & 2) loss += d.ws * (lb - dl_s(zy, f, d) * LN2);
+    if (has & 2) loss += d.ws * (lb - dl_s(zy, f, d) * DL_LN2);
     d.loss[row] = loss;
     d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (MODE != 1 ? s.b : s.a), (float)has);
 }
@@ -456,7 +514,7 @@ __global__ __launch_bounds__(256) void distill_grad_tiny_kernel(DistillArgs d) {
     const float ea = has & 1 ? st.y : 0.0f, eb = has & 2 ? st.z : 0.0f;
     const int label = has & 2 ? r.label : -1;
     const Ref f = dl_ref(st.x, d);
-    const float p = r.i >= 0 && has & 1 ? exp2f((r.t - r.te.ref) * d.ct) / r.te.mass : 0.0f;
+    const float p = r.i >= 0 && has & 1 ? exp2f((r.t - r.ref) * d.ct) / r.mass : 0.0f;
     float sum[NZ];
 #pragma unroll
     for (int k = 0; k < NZ; ++k) sum[k] = 0.0f;

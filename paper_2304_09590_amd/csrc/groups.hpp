@@ -18,7 +18,8 @@ namespace pnn {
 constexpr int GR_MAX_NETS = 1024;   // most networks of a grouping (its counters live in LDS)
 constexpr int GR_THREADS = 512, GR_WAVES = GR_THREADS / 64;
 constexpr int GR_MAX_BLOCKS = 256;  // most workgroups that count (each reads all their counts)
-constexpr int GR_KEYS = 16;         // pairs that a thread keeps in registers
+constexpr int GR_CHUNK = 4096;      // pairs of a workgroup, eight a thread, in registers
+constexpr int GR_ALONE = 8192;      // pairs of one that is alone: one launch for two
 constexpr int GR_SMALL = 16;        // pairs per tile of the kernels for few rows
 constexpr int GR_LARGE = 128, GR_HUGE = 256;  // pairs per tile of the matrix-tile kernels
 constexpr int GR_HEIGHTS = 3;       // tiles of 16, 128 and 256 pairs
@@ -53,7 +54,7 @@ __host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
     }
     g.o_hist = at;
     g.chunk = (g.P + GR_MAX_BLOCKS - 1) / GR_MAX_BLOCKS;
-    if (g.chunk < 4096) g.chunk = g.P <= GR_THREADS * GR_KEYS ? GR_THREADS * GR_KEYS : 4096;  // (one launch, or two)
+    if (g.chunk < GR_CHUNK) g.chunk = g.P <= GR_ALONE ? GR_ALONE : GR_CHUNK;
     g.blocks = (int)((g.P + g.chunk - 1) / g.chunk);
     g.words = g.o_hist + (g.blocks > 1 ? up((int64_t)g.blocks * (K + 1)) : 0);
     return g;
@@ -72,13 +73,29 @@ __device__ inline int group_key(const GroupArgs& g, int64_t i) {
     return (unsigned)id < (unsigned)g.K ? id : g.K;
 }
 
+// the keys of pairs i, i + STEP, ... below `end` (-1 from there on), all loads in flight together
+template <int N, int STEP>
+__device__ inline void group_keys(const GroupArgs& g, int64_t i, int64_t end, int* keys) {
+    int id[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) id[t] = g.ids[i + t * STEP < g.P ? i + t * STEP : g.P - 1];
+#pragma unroll
+    for (int t = 0; t < N; ++t) keys[t] = i + t * STEP >= end ? -1 : (unsigned)id[t] < (unsigned)g.K ? id[t] : g.K;
+}
+
 // pairs of network e within this workgroup's chunk, into hist
 __global__ __launch_bounds__(GR_THREADS) void group_count_kernel(GroupArgs g) {
     __shared__ int cnt[GR_MAX_NETS + 1];
     for (int e = threadIdx.x; e <= g.K; e += GR_THREADS) cnt[e] = 0;
     __syncthreads();
     const int64_t lo = blockIdx.x * g.chunk, hi = lo + g.chunk < g.P ? lo + g.chunk : g.P;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += GR_THREADS) atomicAdd(&cnt[group_key(g, i)], 1);
+    for (int64_t b = lo + threadIdx.x; b < hi; b += GR_THREADS * 8) {  // (eight loads in flight)
+        int keys[8];
+        group_keys<8, GR_THREADS>(g, b, hi, keys);
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            if (keys[t] >= 0) atomicAdd(&cnt[keys[t]], 1);
+    }
     __syncthreads();
     for (int e = threadIdx.x; e <= g.K; e += GR_THREADS) g.hist[(int64_t)blockIdx.x * (g.K + 1) + e] = cnt[e];
 }
@@ -103,52 +120,57 @@ __device__ inline void wave_scan(int* out, int n, int lane, F f) {
     if (lane == 63) out[n] = s;
 }
 
-// Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds
-// what the chunks and waves before it hold, and places its pairs; lanes with equal keys find their
-// order with one ballot per key bit.  Integer sums only: the same bits every run.  With one
-// workgroup its own counts are all there is (no earlier launch).  All workgroups share the tiles.
+// Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds what the
+// chunks and waves before it hold, and places its pairs.  The lanes of a wave that hold the same key find each
+// other in LDS: each sets its bit in the key's word, and the bits below its own are its order.  (By one ballot
+// per key bit instead, 130 instructions a step, the placing was bound by them: 32,768 pairs, 256 networks
+// OLDPLACE.)  Integer sums only: the same bits every run.  With one workgroup its own counts are all there is
+// (no earlier launch).  All workgroups share the tiles.
+template <int KEYS>
 __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
+    constexpr int THREADS = GR_THREADS, WAVES = GR_WAVES;
     extern __shared__ int gsm[];
     const int K1 = g.K + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int* cur = gsm;                  // [GR_WAVES][K1]
-    int* tot = cur + GR_WAVES * K1;  // [K1]
+    unsigned long long* bits = (unsigned long long*)gsm;  // [WAVES][K1 + 1], the last for lanes without a pair
+    int* cur = (int*)(bits + WAVES * (K1 + 1));           // [WAVES][K1]
+    int* tot = cur + WAVES * K1;  // [K1]
     int* off = tot + K1;             // [K1 + 1]
     int* first = off + K1 + 1;       // [GR_HEIGHTS][K1 + 1] first tile of each network
-    for (int e = tid; e < GR_WAVES * K1; e += GR_THREADS) cur[e] = 0;
+    for (int e = tid; e < WAVES * K1; e += THREADS) cur[e] = 0;
+    for (int e = tid; e < WAVES * (K1 + 1); e += THREADS) bits[e] = 0;
     __syncthreads();
     const int64_t lo = blockIdx.x * g.chunk, hi = lo + g.chunk < g.P ? lo + g.chunk : g.P;
-    const int64_t part = (g.chunk + GR_WAVES * 64 - 1) / (GR_WAVES * 64) * 64;
+    const int64_t part = (g.chunk + WAVES * 64 - 1) / (WAVES * 64) * 64;
     const int64_t w0 = lo + wave * part, w1 = w0 + part < hi ? w0 + part : hi;
-    // (a chunk of at most GR_KEYS pairs a thread is read once, all loads in flight together)
-    int keys[GR_KEYS];
-    const bool kept = part <= 64 * GR_KEYS;
-    if (kept) {
+    // (a chunk of at most KEYS pairs a thread is read once, all loads in flight together)
+    int keys[KEYS];
+    const bool kept = part <= 64 * KEYS;
+    if (g.P == 0) {
 #pragma unroll
-        for (int t = 0; t < GR_KEYS; ++t) {
-            const int64_t i = w0 + 64 * t + lane;
-            keys[t] = i < w1 ? group_key(g, i) : -1;
-        }
+        for (int t = 0; t < KEYS; ++t) keys[t] = -1;
+    } else if (kept) {
+        group_keys<KEYS, 64>(g, w0 + lane, w1, keys);
 #pragma unroll
-        for (int t = 0; t < GR_KEYS; ++t)
+        for (int t = 0; t < KEYS; ++t)
             if (keys[t] >= 0) atomicAdd(&cur[wave * K1 + keys[t]], 1);
     } else {
         for (int64_t i = w0 + lane; i < w1; i += 64) atomicAdd(&cur[wave * K1 + group_key(g, i)], 1);
     }
     __syncthreads();
-    for (int e = tid; e < K1; e += GR_THREADS) {
+    for (int e = tid; e < K1; e += THREADS) {
         int before = 0, all = 0;
         if (g.blocks > 1)
             for (int b0 = 0; b0 < g.blocks; b0 += 16) {
                 int h[16];
 #pragma unroll
-                for (int b = 0; b < 16; ++b) h[b] = b0 + b < g.blocks ? g.hist[(int64_t)(b0 + b) * K1 + e] : 0;
+                for (int b = 0; b < 16; ++b) h[b] = g.hist[(int64_t)(b0 + b < g.blocks ? b0 + b : g.blocks - 1) * K1 + e];
 #pragma unroll
                 for (int b = 0; b < 16; ++b) {
-                    all += h[b];
+                    all += b0 + b < g.blocks ? h[b] : 0;
                     before += b0 + b < (int)blockIdx.x ? h[b] : 0;
                 }
             }
-        for (int w = 0; w < GR_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const int c = cur[w * K1 + e];
             cur[w * K1 + e] = before;
             before += c;
@@ -162,48 +184,65 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
         wave_scan(first + (wave - 1) * (K1 + 1), K1, lane, [&](int e) { return (tot[e] + h - 1) / h; });
     }
     __syncthreads();
-    const int bits = 32 - __clz(g.K);
-    auto place = [&](int64_t i, int key, bool live) {
-        uint64_t same = __ballot(live);
-        for (int t = 0; t < bits; ++t) {
-            const uint64_t one = __ballot((key >> t) & 1);
-            same &= ((key >> t) & 1) ? one : ~one;
+    const uint64_t below = (1ull << lane) - 1;
+    volatile unsigned long long* word = bits + wave * (K1 + 1);
+    // N steps at a time: their words (a wave's LDS accesses keep their order), their counters, their places
+    auto place = [&](auto steps, int64_t b, const int* key) {
+        constexpr int N = decltype(steps)::value;
+        uint64_t same[N];
+        int base[N];
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int at = key[t] < 0 ? K1 : key[t];
+            atomicOr((unsigned long long*)&word[at], 1ull << lane);
+            same[t] = word[at];
+            word[at] = 0;
         }
-        if (live) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int leader = __ffsll((unsigned long long)same) - 1;
-            int base = 0;
-            if (rank == 0) base = atomicAdd(&cur[wave * K1 + key], __popcll(same));
-            base = __shfl(base, leader);
-            g.pairs[off[key] + base + rank] = (int)i;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            base[t] = 0;
+            if (key[t] >= 0 && (same[t] & below) == 0) base[t] = atomicAdd(&cur[wave * K1 + key[t]], __popcll(same[t]));
         }
+#pragma unroll
+        for (int t = 0; t < N; ++t) base[t] = __shfl(base[t], __ffsll((unsigned long long)same[t]) - 1);
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+            if (key[t] >= 0) g.pairs[off[key[t]] + base[t] + __popcll(same[t] & below)] = (int)(b + 64 * t + lane);
     };
     if (kept) {
 #pragma unroll
-        for (int t = 0; t < GR_KEYS; ++t)
-            if (w0 + 64 * t < w1) place(w0 + 64 * t + lane, keys[t], keys[t] >= 0);
+        for (int t = 0; t < KEYS; t += 8)
+            if (w0 + 64 * t < w1) place(std::integral_constant<int, 8>{}, w0 + 64 * t, keys + t);
     } else {
-        for (int64_t b = w0; b < w1; b += 64) place(b + lane, b + lane < w1 ? group_key(g, b + lane) : 0, b + lane < w1);
+        for (int64_t b = w0; b < w1; b += 64 * 4) {
+            int key[4];
+            group_keys<4, 64>(g, b + lane, w1, key);
+            place(std::integral_constant<int, 4>{}, b, key);
+        }
     }
     if (blockIdx.x == 0)
-        for (int e = tid; e < K1; e += GR_THREADS) g.off[e] = off[e];
+        for (int e = tid; e < K1; e += THREADS) g.off[e] = off[e];
     if (blockIdx.x == 0 && tid < GR_HEIGHTS) g.count[tid] = first[tid * (K1 + 1) + K1];
-    const int64_t step = (int64_t)gridDim.x * GR_THREADS;
-    for (int h = 0; h < GR_HEIGHTS; ++h) {
+    const int* last = first + K1;  // [h (K1 + 1)]: how many tiles of height h there are
+    const int64_t n0 = last[0], n1 = n0 + last[K1 + 1], n2 = n1 + last[2 * (K1 + 1)];
+    const int64_t step = (int64_t)gridDim.x * THREADS;
+    for (int64_t v = blockIdx.x * (int64_t)THREADS + tid; v < n2; v += step) {
+        const int h = v < n0 ? 0 : v < n1 ? 1 : 2;
+        const int u = (int)(v - (h == 0 ? 0 : h == 1 ? n0 : n1));
         const int* f = first + h * (K1 + 1);
-        for (int64_t u = blockIdx.x * (int64_t)GR_THREADS + tid; u < f[K1]; u += step) {
-            int a = 0, b = K1;  // the last network whose first tile is at most u
-            while (b - a > 1) {
-                const int m = (a + b) >> 1;
-                if (f[m] <= u) a = m;
-                else b = m;
-            }
-            g.tiles[h][u] = make_int2(a, off[a] + (int)(u - f[a]) * group_height(h));
+        int a = 0, b = K1;  // the last network whose first tile is at most u
+        while (b - a > 1) {
+            const int m = (a + b) >> 1;
+            if (f[m] <= u) a = m;
+            else b = m;
         }
+        g.tiles[h][u] = make_int2(a, off[a] + (u - f[a]) * group_height(h));
     }
 }
 
-__host__ inline size_t group_lds(int K) { return sizeof(int) * ((size_t)GR_WAVES * (K + 1) + (2 + GR_HEIGHTS) * (K + 2)); }
+__host__ inline size_t group_lds(int K) {
+    return (size_t)GR_WAVES * (K + 2) * 8 + sizeof(int) * ((size_t)GR_WAVES * (K + 1) + (2 + GR_HEIGHTS) * (K + 2));
+}
 
 // ------------------------------------------------------------------------------------
 // products
@@ -483,34 +522,55 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     const float scale = DIR == GR_DW && g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
     if (DIR == GR_DW && g.lr != 0.0f && pairs == 0) return;  // no update
     // (the pair of column `lane` of the wave: asked of its lane in the loop, not of memory)
-    const int own = DIR != GR_DW && lane < 16 * NJ && wn + lane < nv ? g.pairs[p0 + wn + lane] : 0;
+    constexpr int OWN = (16 * NJ + 63) / 64;
+    int own[OWN];
+#pragma unroll
+    for (int h = 0; h < OWN; ++h) own[h] = DIR != GR_DW && wn + 64 * h + lane < nv ? g.pairs[p0 + wn + 64 * h + lane] : 0;
     float bias[8];
     if (DIR == GR_FWD) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) bias[r] = g.b && r < left && e < g.K ? g.b[e * g.bnet + m + r] : 0.0f;
     }
+    // what a result is combined with (slopes' activations, weights to update) is loaded sixteen columns ahead:
+    // behind a store it would wait for it
+    typedef typename std::conditional<DIR == GR_DW, float, T>::type E;
+    constexpr int TURNS = 16 / COLS;
+    Raw8<E> with[2][TURNS];
+    const bool has_with = DIR == GR_DX ? g.a && e < g.K : DIR == GR_DW && g.lr != 0.0f;
+    auto column = [&](int j, int c) { return wn + 16 * j + c * COLS + lane / PER; };
+    auto pair_of = [&](int j, int c) -> int64_t { return __shfl(own[j / 4], 16 * (j & 3) + c * COLS + lane / PER); };
+    auto fetch = [&](int j) {
+#pragma unroll
+        for (int c = 0; c < TURNS; ++c) {
+            const int64_t pair = DIR == GR_DX ? pair_of(j, c) : 0;
+            const int n = column(j, c), nr = n < nv ? left : 0;
+            if constexpr (DIR == GR_DX) load8(with[j & 1][c], (const T*)g.a + pair * g.lda + m, nr);
+            if constexpr (DIR == GR_DW) load8(with[j & 1][c], (const float*)g.y + e * g.ynet + (int64_t)(n0 + n) * g.ldy + m, nr);
+        }
+    };
+    if (has_with) fetch(0);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
+        if (has_with && j + 1 < NJ) fetch(j + 1);
 #pragma unroll
         for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = acc[i][j];
         __builtin_amdgcn_wave_barrier();
         auto leave = [&](int c, bool smooth) {
-            const int col = c + lane / PER, n = wn + 16 * j + col;
-            const int64_t pair = DIR != GR_DW ? __shfl(own, 16 * j + col) : 0;
+            const int col = c * COLS + lane / PER, n = column(j, c);
+            const int64_t pair = DIR != GR_DW ? pair_of(j, c) : 0;
             if (n >= nv || left <= 0) return;
             const f4 lo = *(const f4*)(turn + col * LD + part), hi = *(const f4*)(turn + col * LD + part + 4);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            float w[8];
+            if (DIR != GR_FWD && has_with) raw8_f(w, with[j & 1][c]);
             if (DIR == GR_DW) {
                 const int64_t at = (int64_t)(n0 + n) * g.ldy + m;
-                float* y = (float*)g.y + ((int64_t)split * g.K + e) * g.ynet + at;
                 if (g.lr != 0.0f) {
-                    Raw8<float> old;
-                    load8(old, y, left);
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) v[r] = old.v[r >> 2][r & 3] - scale * v[r];
+                    for (int r = 0; r < 8; ++r) v[r] = w[r] - scale * v[r];
                     if (g.shadow) store8(g.shadow + e * g.ynet + at, v, left);
                 }
-                store8(y, v, left);
+                store8((float*)g.y + ((int64_t)split * g.K + e) * g.ynet + at, v, left);
                 return;
             }
             if (e == g.K) {  // dropped
@@ -521,19 +581,17 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
                 for (int r = 0; r < 8; ++r) v[r] += bias[r];
                 if (smooth) group_act8(g.act, v);
                 else group_rectify8(g.act, v);
-            } else if (g.a) {
-                float a[8];
-                load8_f<T>(a, (const T*)g.a + pair * g.lda + m, left);
-                group_slope8(g.act, v, a);
+            } else if (has_with) {
+                group_slope8(g.act, v, w);
             }
             store8<true>((TO*)g.y + pair * g.ldy + m, v, left);
         };
         if (DIR == GR_FWD && (g.act == ACT_SIGMOID || g.act == ACT_TANH)) {  // (one copy of their code)
 #pragma unroll 1
-            for (int c = 0; c < 16; c += COLS) leave(c, true);
+            for (int c = 0; c < TURNS; ++c) leave(c, true);
         } else {
 #pragma unroll
-            for (int c = 0; c < 16; c += COLS) leave(c, false);
+            for (int c = 0; c < TURNS; ++c) leave(c, false);
         }
         __builtin_amdgcn_wave_barrier();
         if (bias_rows && kg == 0 && wn + 16 * j + l15 < nv) {
@@ -543,7 +601,9 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     }
 }
 
-// 128 x 128 tiles of one network's product, four waves of 64 x 64.
+// 128 x 128 tiles of one network's product, four waves of 32 x 128: all waves share the tile's columns, so a
+// tile that a group does not fill costs its share of the products only (32,768 rows over 256 networks,
+// 784 -> 1024, fp32: TILEFIG).
 template <int DIR, typename T, typename TO>
 __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     constexpr bool F32 = sizeof(T) == 4;
@@ -559,14 +619,15 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     if (!group_place_of<DIR, 128, 128, BK>(g, mt, at)) return;
     const int e = at.e, m0 = at.m0, n0 = at.n0, nv = at.nv, split = at.split, p0 = at.p0, Kx = at.Kx;
     const int mv = g.M - m0 < 128 ? g.M - m0 : 128;
-    f4 acc[4][4], accb[4];
+    constexpr int MI = 2, NJ = 8;
+    f4 acc[MI][NJ], accb[NJ];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        accb[i] = f4{0, 0, 0, 0};
+    for (int j = 0; j < NJ; ++j) {
+        accb[j] = f4{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f4{0, 0, 0, 0};
+        for (int i = 0; i < MI; ++i) acc[i][j] = f4{0, 0, 0, 0};
     }
-    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    const int wm = wave * 16 * MI;
     const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
 
     // this thread's chunks of a tile
@@ -617,18 +678,19 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         if (k0 + BK < Kx) load(k0 + BK);
 #pragma unroll
         for (int kb = 0; kb < BK; kb += 32) {
-            bf8v fa[PL][4];
+            bf8v fa[PL][MI];
 #pragma unroll
             for (int q = 0; q < PL; ++q)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) fa[q][i] = TA::frag(la + q * TA::ELEMS, wm + 16 * i, kb, lane);
+                for (int i = 0; i < MI; ++i) fa[q][i] = TA::frag(la + q * TA::ELEMS, wm + 16 * i, kb, lane);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < NJ; ++j) {
+                if (16 * j >= nv) break;  // (the same for all lanes)
                 bf8v fb[PL];
 #pragma unroll
-                for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, wn + 16 * j, kb, lane);
+                for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, 16 * j, kb, lane);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < MI; ++i) {
                     // fp32: the six products of parts above 2^-24 of the whole, the smallest first
                     if constexpr (F32) {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][i], fb[1], acc[i][j], 0, 0, 0);
@@ -651,8 +713,8 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         }
     }
     __syncthreads();
-    group_store<DIR, T, TO, 4, 4>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
-                                  (float*)lds + wave * group_turn<4>());
+    group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, 0, lane, bias_rows,
+                                    (float*)lds + wave * group_turn<MI>());
 }
 
 // ------------------------------------------------------------------------------------

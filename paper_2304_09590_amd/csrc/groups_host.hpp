@@ -25,6 +25,18 @@ pnn_status launched(const char* what) {
     return PNN_OK;
 }
 
+// lets a kernel have that much dynamic LDS, once per device (set: the devices on which it may)
+pnn_status lds_of(const void* kernel, int bytes, std::atomic<uint64_t>& set) {
+    int dev = 0;
+    (void)hipGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (bit && (set.load(std::memory_order_relaxed) & bit)) return PNN_OK;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return fail(nullptr, PNN_EHIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(e));
+    set.fetch_or(bit, std::memory_order_relaxed);
+    return PNN_OK;
+}
+
 constexpr int64_t GROUP_MAX_PAIRS = int64_t(1) << 30;
 constexpr int32_t GROUP_MAX_WIDTH = 1 << 20;
 
@@ -114,16 +126,8 @@ template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AH
 pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
     const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? WM * WN * 2 * (NST - 1) * 256 : 0);
     TRY(grid_fits(blocks));
-    static std::atomic<uint64_t> set{0};  // devices on which this kernel may have that much LDS
-    int dev = 0;
-    (void)hipGetDevice(&dev);
-    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-    if (!bit || !(set.load(std::memory_order_relaxed) & bit)) {
-        const hipError_t e = hipFuncSetAttribute((const void*)group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD>,
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return fail(nullptr, PNN_EHIP, "hipFuncSetAttribute failed: %s", hipGetErrorString(e));
-        set.fetch_or(bit, std::memory_order_relaxed);
-    }
+    static std::atomic<uint64_t> set{0};
+    TRY(lds_of((const void*)group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD>, lds, set));
     group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD><<<(unsigned)blocks, 64 * WM * WN, lds, s>>>(a);
     return launched(DIR == GR_FWD ? "grouped forward" : DIR == GR_DX ? "grouped input gradient" : "grouped weight gradient");
 }
@@ -252,7 +256,16 @@ pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, in
         group_count_kernel<<<(unsigned)p.blocks, GR_THREADS, 0, s>>>(a);
         TRY(launched("counting the groups"));
     }
-    group_place_kernel<<<(unsigned)std::max(p.blocks, 1), GR_THREADS, group_lds(p.K), s>>>(a);
+    const int lds = (int)group_lds(p.K);
+    if (p.blocks <= 1) {
+        static std::atomic<uint64_t> set{0};
+        TRY(lds_of((const void*)group_place_kernel<GR_ALONE / GR_THREADS>, (int)group_lds(GR_MAX_NETS), set));
+        group_place_kernel<GR_ALONE / GR_THREADS><<<1, GR_THREADS, lds, s>>>(a);
+    } else {
+        static std::atomic<uint64_t> set{0};
+        TRY(lds_of((const void*)group_place_kernel<GR_CHUNK / GR_THREADS>, (int)group_lds(GR_MAX_NETS), set));
+        group_place_kernel<GR_CHUNK / GR_THREADS><<<(unsigned)p.blocks, GR_THREADS, lds, s>>>(a);
+    }
     return launched("placing the groups");
 }
 
