@@ -20,12 +20,10 @@ constexpr int GR_THREADS = 512, GR_WAVES = GR_THREADS / 64;
 constexpr int GR_MAX_BLOCKS = 256;  // most workgroups that count (each reads all their counts)
 constexpr int GR_CHUNK = 4096;      // pairs of a workgroup, eight a thread, in registers
 constexpr int GR_ALONE = 8192;      // pairs of one that is alone: one launch for two
-constexpr int GR_SMALL = 16;        // pairs per tile of the kernels for few rows
-constexpr int GR_LARGE = 128, GR_HUGE = 256;  // pairs per tile of the matrix-tile kernels
-constexpr int GR_HEIGHTS = 3;       // tiles of 16, 128 and 256 pairs
+constexpr int GR_HEIGHTS = 4;       // pairs per tile: 16, and 64, 128 or 256 for the matrix-tile kernels
 
-// Layout of a plan (int32 words): off[K + 1] | pairs[P] | numbers of tiles | tiles of 16, of 128 and of 256
-// pairs | counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
+// Layout of a plan (int32 words): off[K + 1] | pairs[P] | numbers of tiles | tiles of 16, 64, 128 and
+// 256 pairs | counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
 // pairs.  The host knows only the most tiles there can be (extra workgroups end at once).
 struct GroupPlan {
     int64_t P;
@@ -36,7 +34,7 @@ struct GroupPlan {
     int64_t chunk;  // pairs per counting workgroup
 };
 
-__host__ __device__ inline int group_height(int h) { return h == 0 ? GR_SMALL : h == 1 ? GR_LARGE : GR_HUGE; }
+__host__ __device__ inline int group_height(int h) { return h == 0 ? 16 : 32 << h; }
 
 __host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
     GroupPlan g;
@@ -223,12 +221,17 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
     if (blockIdx.x == 0)
         for (int e = tid; e < K1; e += THREADS) g.off[e] = off[e];
     if (blockIdx.x == 0 && tid < GR_HEIGHTS) g.count[tid] = first[tid * (K1 + 1) + K1];
-    const int* last = first + K1;  // [h (K1 + 1)]: how many tiles of height h there are
-    const int64_t n0 = last[0], n1 = n0 + last[K1 + 1], n2 = n1 + last[2 * (K1 + 1)];
-    const int64_t step = (int64_t)gridDim.x * THREADS;
-    for (int64_t v = blockIdx.x * (int64_t)THREADS + tid; v < n2; v += step) {
-        const int h = v < n0 ? 0 : v < n1 ? 1 : 2;
-        const int u = (int)(v - (h == 0 ? 0 : h == 1 ? n0 : n1));
+    int64_t n[GR_HEIGHTS];  // tiles of this height and the ones before it
+    for (int h = 0; h < GR_HEIGHTS; ++h) n[h] = (h ? n[h - 1] : 0) + first[h * (K1 + 1) + K1];
+    const int64_t step = (int64_t)gridDim.x * GR_THREADS;
+    for (int64_t v = blockIdx.x * (int64_t)GR_THREADS + tid; v < n[GR_HEIGHTS - 1]; v += step) {
+        int h = 0, u = (int)v;
+#pragma unroll
+        for (int q = 1; q < GR_HEIGHTS; ++q)
+            if (v >= n[q - 1]) {
+                h = q;
+                u = (int)(v - n[q - 1]);
+            }
         const int* f = first + h * (K1 + 1);
         int a = 0, b = K1;  // the last network whose first tile is at most u
         while (b - a > 1) {
@@ -327,12 +330,10 @@ __device__ inline void load8(Raw8<float>& r, const float* p, int nv) {
         r.v[0] = *(const f4_a4*)p;
         r.v[1] = *(const f4_a4*)(p + 4);
     } else {
-        float q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        r.v[0] = r.v[1] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 7; ++j)
-            if (j < nv) q[j] = p[j];
-        r.v[0] = f4{q[0], q[1], q[2], q[3]};
-        r.v[1] = f4{q[4], q[5], q[6], q[7]};
+            if (j < nv) r.v[j >> 2][j & 3] = p[j];
     }
 }
 
@@ -441,32 +442,32 @@ __device__ inline bool group_place_of(const GroupGemm& g, int mt, GroupPlace& o)
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s4v lds_s4v;
 
-// An operand tile in LDS, 128 wide and BK deep, in bf16 (fp32 operands as three such planes).
+// An operand tile in LDS, W wide and BK deep, in bf16 (fp32 operands as three such planes).
 //  KC (memory runs along k): rows of BK values in 16-byte chunks; a row's chunks are permuted by
 //     XOR so that eight neighbouring rows' reads of one chunk fall on different banks.
-//  NC (memory runs across k): rows of 128 values, one per k, in 32-byte blocks, permuted by XOR so
+//  NC (memory runs across k): rows of W values, one per k, in 32-byte blocks, permuted by XOR so
 //     that the rows which one transposing read touches fall on different banks.
-template <bool KC, int BK>
+template <bool KC, int BK, int W>
 struct GTile {
-    static constexpr int ELEMS = 128 * BK, CPR = KC ? BK / 8 : 16;
+    static constexpr int ELEMS = W * BK, CPR = KC ? BK / 8 : W / 8, BLOCKS = W / 16;
     static __device__ inline int row(int s) { return s / CPR; }
     static __device__ inline int chunk(int s) { return s % CPR; }
     static __device__ inline int key(int r) {
         if (KC) return CPR == 8 ? r & 7 : (r >> 1) & 3;
-        return (r & 3) | ((r >> 1) & 4);
+        return ((r & 3) | ((r >> 1) & 4)) & (BLOCKS - 1);
     }
     static __device__ inline int offset(int r, int c) {
         if (KC) return r * BK + (c ^ key(r)) * 8;
-        return r * 128 + (((c >> 1) ^ key(r)) << 4) + (c & 1) * 8;
+        return r * W + (((c >> 1) ^ key(r)) << 4) + (c & 1) * 8;
     }
     // operand fragment of the 16 x 16 x 32 instruction: index t0 + (lane & 15), k kb + 8 (lane >> 4) ..
     static __device__ inline bf8v frag(const bf16_t* lds, int t0, int kb, int lane) {
         const int l15 = lane & 15, kg = lane >> 4;
         if (KC) return *(const bf8v*)(lds + offset(t0 + l15, kb / 8 + kg));
         const int r = kb + 8 * kg + (l15 >> 2);
-        const bf16_t* q = lds + r * 128 + (((t0 >> 4) ^ key(r)) << 4) + (l15 & 3) * 4;
+        const bf16_t* q = lds + r * W + (((t0 >> 4) ^ key(r)) << 4) + (l15 & 3) * 4;
         const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)q);
-        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(q + 4 * 128));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(q + 4 * W));
         const s4v both[2] = {lo, hi};
         return __builtin_bit_cast(bf8v, both);
     }
@@ -516,8 +517,9 @@ template <int MI> constexpr int group_turn() { return 16 * (16 * MI + 4); }  // 
 template <int DIR, typename T, typename TO, int MI, int NJ>
 __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], const f4 (&accb)[NJ], int e, int split, int p0, int m0,
                                    int n0, int nv, int wm, int wn, int lane, bool bias_rows, float* turn) {
-    constexpr int LD = 16 * MI + 4, PER = 2 * MI, COLS = 64 / PER;  // lanes of a column, columns at a time
-    const int l15 = lane & 15, kg = lane >> 4, part = lane % PER * 8, m = m0 + wm + part, left = g.M - m;
+    constexpr int LD = 16 * MI + 4, PER = 2 * MI, COLS = MI == 1 ? 16 : 64 / PER;  // lanes of a column, columns at a time
+    const int l15 = lane & 15, kg = lane >> 4, part = lane % PER * 8, m = m0 + wm + part;
+    const int left = lane < PER * COLS ? g.M - m : 0;
     const int pairs = DIR == GR_DW ? g.off[e + 1] - g.off[e] : 0;
     const float scale = DIR == GR_DW && g.lr != 0.0f && pairs > 0 ? g.lr / (float)pairs : 0.0f;
     if (DIR == GR_DW && g.lr != 0.0f && pairs == 0) return;  // no update
@@ -601,25 +603,27 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     }
 }
 
-// 128 x 128 tiles of one network's product, four waves of 32 x 128: all waves share the tile's columns, so a
-// tile that a group does not fill costs its share of the products only (32,768 rows over 256 networks,
-// 784 -> 1024, fp32: TILEFIG).
-template <int DIR, typename T, typename TO>
+// S x S tiles (128, or 64 where those are too few) of one network's product.  Over pairs, four waves of 32 x 128: all waves share the tile's
+// columns, so a tile that a group does not fill costs its share of the products only (32,768 rows over 256
+// networks, 784 -> 1024, fp32, 467 -> 416 us); a weight gradient's tiles are full, and 64 x 64 reads less of
+// LDS (32,768 rows, 64 networks, 2048 x 1024: 909 -> DWFIG us).
+template <int DIR, typename T, typename TO, int S>
 __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int BK = F32 ? 32 : 64, PL = F32 ? 3 : 1;
-    typedef GTile<DIR == GR_FWD, BK> TA;
-    typedef GTile<DIR != GR_DW, BK> TB;
+    typedef GTile<DIR == GR_FWD, BK, S> TA;
+    typedef GTile<DIR != GR_DW, BK, S> TB;
     constexpr int U = TA::ELEMS / 8 / 256;
     __shared__ __align__(16) bf16_t lds[2 * PL * TA::ELEMS];
     bf16_t *la = lds, *lb = lds + PL * TA::ELEMS;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int mt = (g.M + 127) / 128;
+    const int mt = (g.M + S - 1) / S;
     GroupPlace at;
-    if (!group_place_of<DIR, 128, 128, BK>(g, mt, at)) return;
+    if (!group_place_of<DIR, S, S, BK>(g, mt, at)) return;
     const int e = at.e, m0 = at.m0, n0 = at.n0, nv = at.nv, split = at.split, p0 = at.p0, Kx = at.Kx;
-    const int mv = g.M - m0 < 128 ? g.M - m0 : 128;
-    constexpr int MI = 2, NJ = 8;
+    const int mv = g.M - m0 < S ? g.M - m0 : S;
+    constexpr int WN = DIR == GR_DW ? 2 : 1;  // waves across n
+    constexpr int MI = S / 64 * WN, NJ = S / 16 / WN;
     f4 acc[MI][NJ], accb[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -627,7 +631,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) acc[i][j] = f4{0, 0, 0, 0};
     }
-    const int wm = wave * 16 * MI;
+    const int wm = wave / WN * 16 * MI, wn = wave % WN * 16 * NJ;
     const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
 
     // this thread's chunks of a tile
@@ -645,6 +649,14 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         }
     }
     Raw8<T> ra[U], rb[U];
+    int number[U];  // (weight gradient) the pairs of the step that is loaded next
+    auto numbers = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + TA::row(u * 256 + tid);
+            number[u] = g.pairs[p0 + (k < Kx ? k : Kx - 1)];
+        }
+    };
     auto load = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -659,12 +671,13 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
                 load8(rb[u], pb[u] + k0, pb[u] ? Kx - k0 - TB::chunk(s) * 8 : 0);
             } else {
                 const int r = TA::row(s), c = TA::chunk(s) * 8;
-                const int pair = k0 + r < Kx ? g.pairs[p0 + k0 + r] : 0;
-                load8(ra[u], (const T*)g.w + (int64_t)g.wdiv.of(pair) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
-                load8(rb[u], (const T*)g.p + (int64_t)pair * g.ldp + n0 + c, k0 + r < Kx ? nv - c : 0);
+                load8(ra[u], (const T*)g.w + (int64_t)g.wdiv.of(number[u]) * g.ldw + m0 + c, k0 + r < Kx ? mv - c : 0);
+                load8(rb[u], (const T*)g.p + (int64_t)number[u] * g.ldp + n0 + c, k0 + r < Kx ? nv - c : 0);
             }
         }
+        if (DIR == GR_DW) numbers(k0 + BK);
     };
+    if (DIR == GR_DW && Kx > 0) numbers(0);
     if (Kx > 0) load(0);
     for (int k0 = 0; k0 < Kx; k0 += BK) {
         __syncthreads();
@@ -685,10 +698,10 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
                 for (int i = 0; i < MI; ++i) fa[q][i] = TA::frag(la + q * TA::ELEMS, wm + 16 * i, kb, lane);
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
-                if (16 * j >= nv) break;  // (the same for all lanes)
+                if (wn + 16 * j >= nv) break;  // (the same for all lanes)
                 bf8v fb[PL];
 #pragma unroll
-                for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, 16 * j, kb, lane);
+                for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, wn + 16 * j, kb, lane);
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
                     // fp32: the six products of parts above 2^-24 of the whole, the smallest first
@@ -713,7 +726,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         }
     }
     __syncthreads();
-    group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, 0, lane, bias_rows,
+    group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
                                     (float*)lds + wave * group_turn<MI>());
 }
 
@@ -744,7 +757,7 @@ template <bool KC, int T>
 struct RTile {
     static constexpr int ELEMS = T * 32, CHUNKS = ELEMS / 8;
     static __device__ inline int row(int s) { return KC ? s >> 2 : s / (T / 8); }  // (NC: the k)
-    static __device__ inline int key(int r) { return KC ? (r >> 1) & 3 : (r & 3) | ((r >> 1) & 4); }
+    static __device__ inline int key(int r) { return KC ? (r >> 1) & 3 : ((r & 3) | ((r >> 1) & 4)) & (T / 16 - 1); }
     // the chunk of the row that belongs at place s
     static __device__ inline int chunk(int s) {
         const int r = row(s), c = KC ? s & 3 : s % (T / 8);
@@ -1000,18 +1013,26 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupJoin g) {
     }
 }
 
-// dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r])
+// dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r]), eight neighbouring values a thread
 template <typename T, typename TO>
 __global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part, int64_t n, int per_row, int M, const T* a,
                                                               int64_t lda, int act, TO* dx, int64_t ldx) {
-    const int64_t all = n * M;
+    const int chunks = (M + 7) / 8;
+    const int64_t all = n * chunks;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-        const int64_t r = i / M;
-        const int m = (int)(i - r * M);
-        float s = 0.0f;
-        for (int j = 0; j < per_row; ++j) s += part[(r * per_row + j) * M + m];
-        if (a) s *= act_deriv(act, to_f<T>(a[r * lda + m]));
-        dx[r * ldx + m] = from_f<TO>(s);
+        const int64_t r = i / chunks;
+        const int m = (int)(i - r * chunks) * 8, left = M - m;
+        float s[8], x[8];
+        if (a) load8_f<T>(x, a + r * lda + m, left);
+        load8_f<float>(s, part + r * per_row * M + m, left);
+        for (int j = 1; j < per_row; ++j) {
+            float v[8];
+            load8_f<float>(v, part + (r * per_row + j) * M + m, left);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q] += v[q];
+        }
+        if (a) group_slope8(act, s, x);
+        store8(dx + r * ldx + m, s, left);
     }
 }
 

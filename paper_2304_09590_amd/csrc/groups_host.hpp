@@ -108,13 +108,32 @@ pnn_status grid_fits(int64_t blocks) {
     return PNN_OK;
 }
 
-// parts of a group's pairs in a weight gradient: with fewer workgroups than two per CU the groups
-// are split until there are as many, as long as a part keeps 512 pairs in the mean
-int group_splits(int64_t P, int32_t K, int32_t inputs, int32_t outputs) {
-    const int64_t tiles = (int64_t)K * ((inputs + 127) / 128) * ((outputs + 127) / 128);
-    int64_t s = (512 + tiles - 1) / tiles;
-    s = std::min(s, P / K / 512);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
+// The kernels' tiles.  Large ones read operands less often; small ones are more, which hides the latency of
+// short products and unequal groups.
+enum { FEW, TILE64, TILE128, RING_SMALL, RING, RING_HUGE };
+constexpr int64_t GROUP_FILL = 512;  // workgroups that fill the device: two on each of 256 CUs
+
+// Parts that a group's pairs are cut into for a weight gradient, and the ring's tile: 256 x 256 where groups
+// are long and cutting them into parts of 512 pairs fills the device; else 256 x 128; else 128 x 64, groups cut
+// into parts of 256.
+void group_weights_plan(int64_t P, int32_t K, int32_t inputs, int32_t outputs, int* kind, int* splits) {
+    auto tiles = [&](int bm, int bn) { return (int64_t)K * ((inputs + bm - 1) / bm) * ((outputs + bn - 1) / bn); };
+    const int64_t mean = P / K;
+    auto cut = [&](int64_t t, int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>({(GROUP_FILL + t - 1) / t, mean / rows, 64})); };
+    int64_t t = tiles(256, 256), s = cut(t, 512);
+    if (mean >= 512 && t * s >= GROUP_FILL / 2) {
+        *kind = RING_HUGE;
+        *splits = (int)s;
+        return;
+    }
+    t = tiles(256, 128);
+    if (t >= GROUP_FILL) {
+        *kind = RING;
+        *splits = 1;
+        return;
+    }
+    *kind = RING_SMALL;
+    *splits = (int)cut(tiles(128, 64), 256);
 }
 
 // the ring kernels' copies: 16 bytes each, whole inside a row
@@ -132,32 +151,35 @@ pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
     return launched(DIR == GR_FWD ? "grouped forward" : DIR == GR_DX ? "grouped input gradient" : "grouped weight gradient");
 }
 
-enum { FEW = 0, TILE = 1, RING = 2, RING_HUGE = 3 };
-
-// Which kernel multiplies: tiles of 16 pairs re-read the weights for each of them, those of 128 and 256
-// multiply what is not there.
-int group_kind(const pnn_groups* g, bool ring) {
-    const int64_t mean = g->n * g->per_row / g->networks;
+// Which kernel multiplies pairs: tiles of 16 re-read the weights for each of them, those of 64 to 256 multiply
+// what is not there.
+int group_pairs_kind(const pnn_groups* g, int M, bool ring) {
+    const int64_t P = g->n * g->per_row, mean = P / g->networks;
     if (mean <= 24) return FEW;
-    if (!ring) return TILE;
-    return mean >= 512 ? RING_HUGE : RING;
+    // (half of a network's last tile is empty in the mean)
+    auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * (P / bn + g->networks / 2); };
+    if (!ring) return tiles(128, 128) >= GROUP_FILL ? TILE128 : TILE64;
+    if (mean >= 512 && tiles(256, 256) >= GROUP_FILL / 2) return RING_HUGE;
+    return tiles(256, 128) >= GROUP_FILL ? RING : RING_SMALL;
 }
 
 template <int DIR, typename T, typename TO>
 pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
-    const int kind = group_kind(g, sizeof(T) == 2 && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx));
+    const int kind = group_pairs_kind(g, a.M, sizeof(T) == 2 && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx));
     const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
-    const int height = kind == FEW ? 0 : kind == RING_HUGE ? 2 : 1;
+    const int height = kind == FEW ? 0 : kind == TILE64 || kind == RING_SMALL ? 1 : kind == RING_HUGE ? 3 : 2;
     a.tiles = (const int2*)((const int32_t*)g->plan_dev + p.o_tiles[height]);
     a.n_tiles = (const int32_t*)g->plan_dev + p.o_count + height;
     auto blocks = [&](int band) { return (a.M + band - 1) / band * p.most[height]; };
     if constexpr (sizeof(T) == 2) {
         if (kind == RING_HUGE) return launch_ring<DIR, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
         if (kind == RING) return launch_ring<DIR, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);
+        if (kind == RING_SMALL) return launch_ring<DIR, TO, 128, 64, 2, 2, 4, false>(a, blocks(128), s);
     }
-    const int64_t all = blocks(kind == TILE ? 128 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
+    const int64_t all = blocks(kind == TILE128 ? 128 : kind == TILE64 ? 64 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
     TRY(grid_fits(all));
-    if (kind == TILE) group_tile_kernel<DIR, T, TO><<<(unsigned)all, 256, 0, s>>>(a);
+    if (kind == TILE128) group_tile_kernel<DIR, T, TO, 128><<<(unsigned)all, 256, 0, s>>>(a);
+    else if (kind == TILE64) group_tile_kernel<DIR, T, TO, 64><<<(unsigned)all, 256, 0, s>>>(a);
     else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
     else group_few_dx_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
     return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
@@ -175,7 +197,8 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
                              const void* x, int64_t x_ld, int xdiv, float* dw, int64_t dw_net, int64_t dw_ld, float* db,
                              int64_t db_net, float lr, bf16_t* shadow, void* ws, hipStream_t s) {
     GroupGemm a = group_base(g);
-    const int S = group_splits((int64_t)g->n * g->per_row, g->networks, inputs, outputs);
+    int S, kind;
+    group_weights_plan((int64_t)g->n * g->per_row, g->networks, inputs, outputs, &kind, &S);
     a.M = inputs; a.N = outputs;
     a.p = dy; a.ldp = dy_ld;
     a.w = x; a.ldw = x_ld; a.wdiv = div_by(xdiv);
@@ -192,15 +215,21 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
     auto blocks = [&](int bm, int bn) {
         return group_dw_blocks((int64_t)((inputs + bm - 1) / bm) * ((outputs + bn - 1) / bn), (int64_t)S * g->networks);
     };
-    const int kind = group_kind(g, type != PNN_FP32 && ring_ok(x, x_ld, 0, inputs) && ring_ok(dy, dy_ld, 0, outputs));
-    if (kind == RING_HUGE) {
-        TRY((launch_ring<GR_DW, float, 256, 256, 2, 4, 4, true>(a, blocks(256, 256), s)));
-    } else if (kind == RING) {
-        TRY((launch_ring<GR_DW, float, 256, 128, 2, 2, 3, false>(a, blocks(256, 128), s)));
+    if (type != PNN_FP32 && ring_ok(x, x_ld, 0, inputs) && ring_ok(dy, dy_ld, 0, outputs)) {
+        if (kind == RING_HUGE) TRY((launch_ring<GR_DW, float, 256, 256, 2, 4, 4, true>(a, blocks(256, 256), s)));
+        else if (kind == RING) TRY((launch_ring<GR_DW, float, 256, 128, 2, 2, 3, false>(a, blocks(256, 128), s)));
+        else TRY((launch_ring<GR_DW, float, 128, 64, 2, 2, 4, false>(a, blocks(128, 64), s)));
     } else {
-        TRY(grid_fits(blocks(128, 128)));
-        if (type == PNN_FP32) group_tile_kernel<GR_DW, float, float><<<(unsigned)blocks(128, 128), 256, 0, s>>>(a);
-        else group_tile_kernel<GR_DW, bf16_t, float><<<(unsigned)blocks(128, 128), 256, 0, s>>>(a);
+        const bool small = blocks(128, 128) < GROUP_FILL;
+        const int64_t all = small ? blocks(64, 64) : blocks(128, 128);
+        TRY(grid_fits(all));
+        if (type == PNN_FP32) {
+            if (small) group_tile_kernel<GR_DW, float, float, 64><<<(unsigned)all, 256, 0, s>>>(a);
+            else group_tile_kernel<GR_DW, float, float, 128><<<(unsigned)all, 256, 0, s>>>(a);
+        } else {
+            if (small) group_tile_kernel<GR_DW, bf16_t, float, 64><<<(unsigned)all, 256, 0, s>>>(a);
+            else group_tile_kernel<GR_DW, bf16_t, float, 128><<<(unsigned)all, 256, 0, s>>>(a);
+        }
         TRY(launched("grouped weight gradient"));
     }
     if (S > 1) {
@@ -216,7 +245,8 @@ int64_t group_input_ws(const pnn_groups* g, int32_t inputs) {
     return g->per_row > 1 ? g->n * g->per_row * (int64_t)inputs * 4 : 0;
 }
 int64_t group_weights_ws(const pnn_groups* g, int32_t inputs, int32_t outputs) {
-    const int S = group_splits(g->n * g->per_row, g->networks, inputs, outputs);
+    int S, kind;
+    group_weights_plan(g->n * g->per_row, g->networks, inputs, outputs, &kind, &S);
     return S > 1 ? (int64_t)S * g->networks * outputs * ((int64_t)inputs + 1) * 4 : 0;
 }
 
@@ -251,7 +281,7 @@ pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, in
     OnDeviceOf dev(s);
     int32_t* w = (int32_t*)plan_dev;
     GroupArgs a = {ids_dev, w, w + p.o_pairs, w + p.o_count, w + p.o_hist,
-                   {(int2*)(w + p.o_tiles[0]), (int2*)(w + p.o_tiles[1]), (int2*)(w + p.o_tiles[2])}, p.P, p.chunk, p.K, p.blocks};
+                   {(int2*)(w + p.o_tiles[0]), (int2*)(w + p.o_tiles[1]), (int2*)(w + p.o_tiles[2]), (int2*)(w + p.o_tiles[3])}, p.P, p.chunk, p.K, p.blocks};
     if (p.blocks > 1) {
         group_count_kernel<<<(unsigned)p.blocks, GR_THREADS, 0, s>>>(a);
         TRY(launched("counting the groups"));
@@ -324,7 +354,7 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     }
     a.y = ws_dev; a.ldy = layer->inputs;
     TRY(run_group_pairs<GR_DX>(a, groups, layer->type, PNN_FP32, s));
-    const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * layer->inputs + 255) / 256, 8192);
+    const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * ((layer->inputs + 7) / 8) + 255) / 256, 8192);
     const float* part = (const float*)ws_dev;
     const void* ad = act >= 0 ? a_dev : nullptr;
 #define PNN_SUM_PAIRS(T, TO) \

@@ -234,7 +234,9 @@ SHAPES = [  # n, per_row, networks, inputs, outputs, kind, pad
     (50, 2, 7, 100, 131, "mixed", 1), (40, 1, 3, 8, 8, "none", 0), (24, 1, 1, 784, 16, "one", 0), (25, 1, 1, 784, 16, "one", 0),
     (300, 1, 5, 64, 128, "mixed", 0), (129, 3, 3, 129, 127, "mixed", 0), (1000, 1, 4, 200, 104, "few", 0),
     (257, 1, 1, 65, 257, "one", 2), (2000, 2, 3, 96, 40, "mixed", 8), (3000, 1, 2, 20, 12, "mixed", 0),
-    (700, 1, 2, 520, 264, "mixed", 0), (1500, 3, 4, 264, 776, "mixed", 0), (400, 1, 3, 512, 257, "mixed", 0)]
+    (700, 1, 2, 520, 264, "mixed", 0), (1500, 3, 4, 264, 776, "mixed", 0), (400, 1, 3, 512, 257, "mixed", 0),
+    (5000, 1, 2, 1024, 768, "mixed", 0), (9000, 1, 1, 72, 48, "one", 0), (4000, 1, 32, 1000, 1096, "mixed", 0),
+    (4000, 1, 32, 999, 1095, "mixed", 0)]
 
 
 @gpu
