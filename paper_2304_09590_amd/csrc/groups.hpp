@@ -648,7 +648,10 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             pb[u] = r < nv && Kx > 0 ? (const T*)g.p + (int64_t)(g.pdiv.of(g.pairs[p0 + r])) * g.ldp + TB::chunk(s) * 8 : nullptr;
         }
     }
-    Raw8<T> ra[U], rb[U];
+    // the next D steps' operands are in flight in registers (three where they are small: a step of 64 x 64 is
+    // shorter than a load)
+    constexpr int D = S == 64 ? 3 : 1;
+    Raw8<T> ra[D][U], rb[D][U];
     int number[U];  // (weight gradient) the pairs of the step that is loaded next
     auto numbers = [&](int k0) {
 #pragma unroll
@@ -657,7 +660,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             number[u] = g.pairs[p0 + (k < Kx ? k : Kx - 1)];
         }
     };
-    auto load = [&](int k0) {
+    auto load = [&](int k0, Raw8<T> (&ra)[U], Raw8<T> (&rb)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = u * 256 + tid;
@@ -678,17 +681,19 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         if (DIR == GR_DW) numbers(k0 + BK);
     };
     if (DIR == GR_DW && Kx > 0) numbers(0);
-    if (Kx > 0) load(0);
-    for (int k0 = 0; k0 < Kx; k0 += BK) {
-        __syncthreads();
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (d * BK < Kx) load(d * BK, ra[d], rb[d]);
+    auto step = [&](int k0, Raw8<T> (&ra)[U], Raw8<T> (&rb)[U]) {
+        lds_barrier();  // (waits for no load)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = u * 256 + tid;
             gt_store(la + TA::offset(TA::row(s), TA::chunk(s)), TA::ELEMS, ra[u]);
             gt_store(lb + TB::offset(TB::row(s), TB::chunk(s)), TB::ELEMS, rb[u]);
         }
-        __syncthreads();
-        if (k0 + BK < Kx) load(k0 + BK);
+        lds_barrier();
+        if (k0 + D * BK < Kx) load(k0 + D * BK, ra, rb);
 #pragma unroll
         for (int kb = 0; kb < BK; kb += 32) {
             bf8v fa[PL][MI];
@@ -702,28 +707,26 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
                 bf8v fb[PL];
 #pragma unroll
                 for (int q = 0; q < PL; ++q) fb[q] = TB::frag(lb + q * TB::ELEMS, wn + 16 * j, kb, lane);
+                // fp32: the six products of parts above 2^-24 of the whole, the smallest first
+                constexpr int PA[6] = {1, 2, 0, 1, 0, 0}, PB[6] = {1, 0, 2, 0, 1, 0};
 #pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    // fp32: the six products of parts above 2^-24 of the whole, the smallest first
-                    if constexpr (F32) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][i], fb[1], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[2][i], fb[0], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[2], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[1][i], fb[0], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[1], acc[i][j], 0, 0, 0);
-                    }
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[0][i], fb[0], acc[i][j], 0, 0, 0);
-                }
+                for (int p = F32 ? 0 : 5; p < 6; ++p)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[PA[p]][i], fb[PB[p]], acc[i][j], 0, 0, 0);
                 if (bias_rows) {  // sums over k: a product with ones
-                    const bf16_t one = 0x3f80;
-                    const uint32_t two = one | (uint32_t)one << 16;
-                    const u4v ones4 = {two, two, two, two};
-                    const bf8v ones = __builtin_bit_cast(bf8v, ones4);
+                    const u4v ones = {0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80};
 #pragma unroll
-                    for (int q = PL - 1; q >= 0; --q) accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fb[q], accb[j], 0, 0, 0);
+                    for (int q = PL - 1; q >= 0; --q)
+                        accb[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, ones), fb[q], accb[j], 0, 0, 0);
                 }
             }
         }
+    };
+    for (int k0 = 0; k0 < Kx; k0 += D * BK) {
+#pragma unroll
+        for (int d = 0; d < D; ++d)
+            if (k0 + d * BK < Kx) step(k0 + d * BK, ra[d], rb[d]);
     }
     __syncthreads();
     group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,

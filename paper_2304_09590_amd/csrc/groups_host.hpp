@@ -127,7 +127,7 @@ void group_weights_plan(int64_t P, int32_t K, int32_t inputs, int32_t outputs, i
         return;
     }
     t = tiles(256, 128);
-    if (t >= GROUP_FILL) {
+    if (t >= GROUP_FILL / 2) {
         *kind = RING;
         *splits = 1;
         return;
@@ -152,10 +152,12 @@ pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
 }
 
 // Which kernel multiplies pairs: tiles of 16 re-read the weights for each of them, those of 64 to 256 multiply
-// what is not there.
-int group_pairs_kind(const pnn_groups* g, int M, bool ring) {
+// what is not there.  Forward in us, tiles of 16 against 64 and more, at 1, 16, 24 and 64 pairs a network:
+// 64 networks 784 -> 512 in fp32 21, 25, 37, 66 against 29, 27, 31, 33; in bf16 14, 18, 24, 42 against 13, 13, 15,
+// 15; 32 networks 2048 -> 4096 in bf16 102, 138, 198, 378 against 111, 113, 114, 132.
+int group_pairs_kind(const pnn_groups* g, int M, bool bf16, bool ring) {
     const int64_t P = g->n * g->per_row, mean = P / g->networks;
-    if (mean <= 24) return FEW;
+    if (mean <= (bf16 ? 2 : 16)) return FEW;
     // (half of a network's last tile is empty in the mean)
     auto tiles = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * (P / bn + g->networks / 2); };
     if (!ring) return tiles(128, 128) >= GROUP_FILL ? TILE128 : TILE64;
@@ -165,7 +167,7 @@ int group_pairs_kind(const pnn_groups* g, int M, bool ring) {
 
 template <int DIR, typename T, typename TO>
 pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
-    const int kind = group_pairs_kind(g, a.M, sizeof(T) == 2 && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx));
+    const int kind = group_pairs_kind(g, a.M, sizeof(T) == 2, sizeof(T) == 2 && ring_ok(a.w, a.ldw, a.wnet, DIR == GR_FWD ? a.Kx : a.M) && ring_ok(a.p, a.ldp, 0, a.Kx));
     const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
     const int height = kind == FEW ? 0 : kind == TILE64 || kind == RING_SMALL ? 1 : kind == RING_HUGE ? 3 : 2;
     a.tiles = (const int2*)((const int32_t*)g->plan_dev + p.o_tiles[height]);
