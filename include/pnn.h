@@ -258,7 +258,9 @@ void pnn_destroy(pnn_net* net);
  * `type` is PNN_FP32 (fp32) or PNN_BF16_MIXED (bfloat16).  Products are summed in fp32; fp32
  * operands enter the matrix units in three bf16 parts (six products, as exact as fp32 products),
  * so they have to be finite and below 3.38e38: an infinite operand gives NaN in what it reaches,
- * as a NaN does.  Results must not overlap operands. */
+ * as a NaN does.  Results must not overlap operands, and a plan is used with the sizes it was made
+ * with.  What does not fit a launch (a result of more than 2^32 values of narrow rows, say) is refused
+ * with PNN_ESHAPE. */
 
 /* Row r's per_row ids are ids_dev[r per_row + j]: pair p = r per_row + j goes through network
  * ids_dev[p] in [0, networks); any other id drops the pair.  The same network may stand twice. */
@@ -359,7 +361,8 @@ pnn_status pnn_distill_grad(const pnn_distill* args, const float* g_dev, const v
  * A handle's child networks on rows that name them (at most 1,024 CNs: PNN_EINVAL otherwise).  Both
  * calls keep their grouping, activations and errors in one workspace of the handle that grows with the
  * pairs of a call, so calls of one handle on different streams have to be ordered by the caller; they
- * may be recorded into a graph as the other calls are (see the top).  x_dev
+ * may be recorded into a graph as the other calls are (see the top), but not while a merge's broadcast
+ * is still to be made (the fused last-layer plan: PNN_EHIP, nothing recorded).  x_dev
  * [rows][sizes[0]] fp32, ids_dev [rows][per_row] as in pnn_group_rows.  Products, activations and
  * roundings are those of pnn_infer and pnn_train_epoch up to the order of the fp32 sums. */
 

@@ -21,6 +21,7 @@ constexpr int DL_TINY_TOP = 16, DL_TINY = 128;  // most entries and classes of a
 struct DistillArgs {
     const void* z;
     int64_t ldz, n;
+    int64_t row0;             // first row of the launch
     int V, k;
     const int32_t* idx;
     const void* t;
@@ -247,7 +248,7 @@ template <typename T, int MODE, int W>
 __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
     __shared__ Sums across[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    const int64_t row = d.row0 + (W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave);
     const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
 // joins the parts of a row, one wave a row
 template <typename T, int MODE>
 __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
-    const int64_t row = blockIdx.x;
+    const int64_t row = d.row0 + blockIdx.x;
     const int lane = threadIdx.x;
     Teacher<T> te;
     te.load(d, row, lane, true);
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     __shared__ int sidx[4 / W][TOP];
     __shared__ float sp[4 / W][TOP], sz[4 / W][TOP + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave;
+    const int64_t row = d.row0 + (W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave);
     const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0, slot = W == 4 ? 0 : wave;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
@@ -461,7 +462,7 @@ struct Tiny {
 template <typename T, int MODE, int NZ>
 __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
     const int lane = threadIdx.x & 15;
-    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int64_t row = d.row0 + (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (row >= d.n) return;
     Tiny<T, NZ> r;
     r.load(d, row, lane);
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(256) void distill_loss_tiny_kernel(DistillArgs d) {
 template <typename T, int NZ>
 __global__ __launch_bounds__(256) void distill_grad_tiny_kernel(DistillArgs d) {
     const int lane = threadIdx.x & 15;
-    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int64_t row = d.row0 + (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (row >= d.n) return;
     T* dz = (T*)d.dz + row * d.lddz;
     const float4 st = d.stats[row];

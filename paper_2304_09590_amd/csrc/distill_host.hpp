@@ -77,38 +77,46 @@ int distill_mode(const pnn_distill* a) {
     return a->temperature == 2.0f ? 3 : 2;
 }
 
-template <typename T, int MODE>
-pnn_status launch_distill_loss(const DistillArgs& d, int width, hipStream_t s) {
-    if (width == DL_LANES) {
-        const unsigned blocks = (unsigned)((d.n + 15) / 16);
-        if (d.V <= 16) distill_loss_tiny_kernel<T, MODE, 1><<<blocks, 256, 0, s>>>(d);
-        else distill_loss_tiny_kernel<T, MODE, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
-    } else if (width == DL_WAVE) {
-        distill_loss_kernel<T, MODE, 1><<<(unsigned)((d.n + 3) / 4), 256, 0, s>>>(d);
-    } else {
-        TRY(grid_fits(d.n * d.S));
-        distill_loss_kernel<T, MODE, 4><<<(unsigned)(d.n * d.S), 256, 0, s>>>(d);
-        if (d.S > 1) {
-            TRY(launched("distillation loss"));
-            distill_join_kernel<T, MODE><<<(unsigned)d.n, 64, 0, s>>>(d);
-        }
+// f(d, workgroups) for as many rows at a time as a launch holds workgroups of 256 threads
+template <typename F>
+pnn_status distill_launches(DistillArgs d, int width, const char* what, F f) {
+    const int64_t most = MAX_THREADS / 256, per = width == DL_LANES ? 16 : width == DL_WAVE ? 4 : 1;  // rows of a workgroup
+    const int64_t rows = width == DL_BLOCK ? std::max<int64_t>(1, most / d.S) : most * per;
+    for (d.row0 = 0; d.row0 < d.n; d.row0 += rows) {
+        const int64_t m = std::min(rows, d.n - d.row0);
+        f(d, (unsigned)(width == DL_BLOCK ? m * d.S : (m + per - 1) / per), (unsigned)m);
+        TRY(launched(what));
     }
-    return launched("distillation loss");
+    return PNN_OK;
 }
 
 template <typename T, int MODE>
-pnn_status launch_distill_grad(const DistillArgs& d, int width, hipStream_t s) {
-    if (width == DL_LANES) {
-        const unsigned blocks = (unsigned)((d.n + 15) / 16);
-        if (d.V <= 16) distill_grad_tiny_kernel<T, 1><<<blocks, 256, 0, s>>>(d);
-        else distill_grad_tiny_kernel<T, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
-    } else if (width == DL_WAVE) {
-        distill_grad_kernel<T, MODE, 1><<<(unsigned)((d.n + 3) / 4), 256, 0, s>>>(d);
-    } else {
-        TRY(grid_fits(d.n * d.S));
-        distill_grad_kernel<T, MODE, 4><<<(unsigned)(d.n * d.S), 256, 0, s>>>(d);
-    }
-    return launched("distillation gradient");
+pnn_status launch_distill_loss(const DistillArgs& a, int width, hipStream_t s) {
+    return distill_launches(a, width, "distillation loss", [&](const DistillArgs& d, unsigned blocks, unsigned rows) {
+        if (width == DL_LANES) {
+            if (d.V <= 16) distill_loss_tiny_kernel<T, MODE, 1><<<blocks, 256, 0, s>>>(d);
+            else distill_loss_tiny_kernel<T, MODE, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
+        } else if (width == DL_WAVE) {
+            distill_loss_kernel<T, MODE, 1><<<blocks, 256, 0, s>>>(d);
+        } else {
+            distill_loss_kernel<T, MODE, 4><<<blocks, 256, 0, s>>>(d);
+            if (d.S > 1) distill_join_kernel<T, MODE><<<rows, 64, 0, s>>>(d);
+        }
+    });
+}
+
+template <typename T, int MODE>
+pnn_status launch_distill_grad(const DistillArgs& a, int width, hipStream_t s) {
+    return distill_launches(a, width, "distillation gradient", [&](const DistillArgs& d, unsigned blocks, unsigned) {
+        if (width == DL_LANES) {
+            if (d.V <= 16) distill_grad_tiny_kernel<T, 1><<<blocks, 256, 0, s>>>(d);
+            else distill_grad_tiny_kernel<T, DL_TINY / 16><<<blocks, 256, 0, s>>>(d);
+        } else if (width == DL_WAVE) {
+            distill_grad_kernel<T, MODE, 1><<<blocks, 256, 0, s>>>(d);
+        } else {
+            distill_grad_kernel<T, MODE, 4><<<blocks, 256, 0, s>>>(d);
+        }
+    });
 }
 
 template <typename T>

@@ -1198,6 +1198,15 @@ __global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
     }
 }
 
+__global__ __launch_bounds__(256) void rows_to_bf16_kernel(const float* src, bf16_t* dst, int64_t n) {
+    for (int64_t i = (blockIdx.x * 256ll + threadIdx.x) * 8; i < n; i += gridDim.x * 2048ll) {
+        float v[8];
+        const int left = n - i < 8 ? (int)(n - i) : 8;
+        load8_f<float>(v, src + i, left);
+        store8(dst + i, v, left);
+    }
+}
+
 // A row's answer: the outputs x^L of its pairs, weighted (without weights each counts the same), and
 // the class of the largest (lowest index on ties).  A row without a network: outputs 0, class -1.
 __global__ __launch_bounds__(256) void routed_answer_kernel(const float* z, const int32_t* ids, const float* weights, int64_t n,

@@ -10,11 +10,12 @@ struct OnDeviceOf {
     explicit OnDeviceOf(hipStream_t s) {
         hipDevice_t dev = -1;
         int cur = -1;
-        if (!s || hipStreamGetDevice(s, &dev) != hipSuccess || hipGetDevice(&cur) != hipSuccess || dev == cur) {
-            if (s) (void)hipGetLastError();
+        if (!s) return;
+        if (hipStreamGetDevice(s, &dev) != hipSuccess || hipGetDevice(&cur) != hipSuccess) {
+            (void)hipGetLastError();  // (the launch itself will tell)
             return;
         }
-        if (hipSetDevice(dev) == hipSuccess) before = cur;
+        if (dev != cur && hipSetDevice(dev) == hipSuccess) before = cur;
     }
     ~OnDeviceOf() { if (before >= 0) (void)hipSetDevice(before); }
 };
@@ -103,8 +104,11 @@ GroupGemm group_base(const pnn_groups* g) {
     return a;
 }
 
-pnn_status grid_fits(int64_t blocks) {
-    if (blocks > INT32_MAX) return fail(nullptr, PNN_ESHAPE, "%lld workgroups are more than a launch takes", (long long)blocks);
+// a launch holds less than 2^32 threads
+constexpr int64_t MAX_THREADS = (int64_t(1) << 32) - 1;
+pnn_status grid_fits(int64_t blocks, int threads) {
+    if (blocks > MAX_THREADS / threads)
+        return fail(nullptr, PNN_ESHAPE, "%lld workgroups are more than a launch takes", (long long)blocks);
     return PNN_OK;
 }
 
@@ -144,7 +148,7 @@ bool ring_ok(const void* p, int64_t ld, int64_t net, int width) {
 template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
 pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
     const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? WM * WN * 2 * (NST - 1) * 256 : 0);
-    TRY(grid_fits(blocks));
+    TRY(grid_fits(blocks, 64 * WM * WN));
     static std::atomic<uint64_t> set{0};
     TRY(lds_of((const void*)group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD>, lds, set));
     group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD><<<(unsigned)blocks, 64 * WM * WN, lds, s>>>(a);
@@ -179,7 +183,7 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
         if (kind == RING_SMALL) return launch_ring<DIR, TO, 128, 64, 2, 2, 4, false>(a, blocks(128), s);
     }
     const int64_t all = blocks(kind == TILE128 ? 128 : kind == TILE64 ? 64 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
-    TRY(grid_fits(all));
+    TRY(grid_fits(all, 256));
     if (kind == TILE128) group_tile_kernel<DIR, T, TO, 128><<<(unsigned)all, 256, 0, s>>>(a);
     else if (kind == TILE64) group_tile_kernel<DIR, T, TO, 64><<<(unsigned)all, 256, 0, s>>>(a);
     else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
@@ -224,7 +228,7 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
     } else {
         const bool small = blocks(128, 128) < GROUP_FILL;
         const int64_t all = small ? blocks(64, 64) : blocks(128, 128);
-        TRY(grid_fits(all));
+        TRY(grid_fits(all, 256));
         if (type == PNN_FP32) {
             if (small) group_tile_kernel<GR_DW, float, float, 64><<<(unsigned)all, 256, 0, s>>>(a);
             else group_tile_kernel<GR_DW, float, float, 128><<<(unsigned)all, 256, 0, s>>>(a);

@@ -33,6 +33,9 @@ pnn_status routed_usable(pnn_net* n, const float* x_dev, const int32_t* ids_dev,
     if (!x_dev || !ids_dev) return fail(n, PNN_EINVAL, "x_dev / ids_dev is NULL");
     if (!aligned16(x_dev)) return fail(n, PNN_EINVAL, "x_dev is not 16-byte aligned");
     TRY(check_abort(n, true, s));
+    // (recorded, the copy of the merged network would be made at every replay, and not before the first)
+    if (n->bcast_pending && capturing(s))
+        return fail(n, PNN_EHIP, "a merge has left its broadcast to the next call: make one outside the recording first");
     return settle(n, s);
 }
 
@@ -54,14 +57,16 @@ pnn_group_layer routed_layer(const pnn_net* n, int l) {
     return g;
 }
 
+void rows_to_bf16(const float* src, bf16_t* dst, int64_t values, hipStream_t s) {
+    rows_to_bf16_kernel<<<(unsigned)std::min<int64_t>((values + 2047) / 2048, 65536), 256, 0, s>>>(src, dst, values);
+}
+
 // the rows as the first layer's products take them
 pnn_status routed_rows(pnn_net* n, const float* x, bf16_t* xb, int64_t rows, const void** xin, hipStream_t s) {
     *xin = x;
     if (!n->bf16) return PNN_OK;
-    const int64_t all = rows * n->sizes[0];
-    TRY_NET(n, grid_fits((all + 255) / 256));
     Launch lc(n, s, "routed_rows");
-    to_bf16_kernel<<<(unsigned)((all + 255) / 256), 256, 0, s>>>(x, xb, all);
+    rows_to_bf16(x, xb, rows * n->sizes[0], s);
     *xin = xb;
     return lc.done();
 }
@@ -188,8 +193,7 @@ pnn_status pnn_train_routed(pnn_net* n, const float* x_dev, int64_t rows, const 
         a.dz = z; a.lddz = O;
         TRY_NET(n, run_distill_grad<float>(a, mode, width, s));
         if (n->bf16) {
-            TRY_NET(n, grid_fits((P * O + 255) / 256));
-            to_bf16_kernel<<<(unsigned)((P * O + 255) / 256), 256, 0, s>>>(z, (bf16_t*)err[0], P * O);
+            rows_to_bf16(z, (bf16_t*)err[0], P * O, s);
             delta = err[0];
         }
         TRY(lc.done());

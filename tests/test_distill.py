@@ -290,3 +290,36 @@ def test_another_stream_and_a_graph(n, v, k):
         torch.cuda.synchronize()
         for a, b in zip(kept, step()):
             assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,v", [(30, 10), (30, 700), (5, 9000)])
+def test_labels_alone(n, v, dtype):
+    """alpha = 1 needs no teacher: the cross-entropy and its output error."""
+    z, idx, t, y, g = case(n, v, 2, dtype, seed=13)
+    loss, stats = pnn.distill_loss(z, None, None, y=y, alpha=1.0)
+    dz = pnn.distill_grad(z, None, None, stats, g, y=y, alpha=1.0)
+    want, tol, dwant, dtol = reference(z, idx, t, y, 1.0, 1.0, g)
+    if dtype == BF16:
+        dtol = dtol + (dwant.abs() + dtol) * torch.finfo(BF16).eps / 2
+    assert ((loss.double().cpu() - want).abs() <= tol).all() and ((dz.double().cpu() - dwant).abs() <= dtol).all()
+    loss, stats = pnn.distill_loss(z, None, None)  # neither a teacher nor labels
+    assert (loss == 0).all() and (pnn.distill_grad(z, None, None, stats) == 0).all()
+
+
+@gpu
+def test_more_rows_than_one_launch_holds():
+    n = (1 << 28) + 37  # 16 rows a workgroup of 256 threads, 2^32 threads
+    z = torch.zeros(n, 2, device="cuda")
+    z[:, 1] = 1
+    y = torch.zeros(n, dtype=torch.int32, device="cuda")
+    y[-1] = 1
+    loss, stats = pnn.distill_loss(z, None, None, y=y, alpha=1.0)
+    up = math.log1p(math.exp(1.0))
+    assert abs(float(loss[0]) - up) <= 4e-7 and abs(float(loss[-2]) - up) <= 4e-7 and abs(float(loss[-1]) - (up - 1)) <= 4e-7
+    assert float(loss.min()) == float(loss[-1]) and float(loss.max()) == float(loss[0])
+    dz = pnn.distill_grad(z, None, None, stats, y=y, alpha=1.0, out=z)
+    s = 1 / (1 + math.exp(1.0))
+    assert abs(float(dz[0, 0]) - (s - 1)) <= 4e-7 and abs(float(dz[-1, 0]) - s) <= 4e-7
+    assert (dz[:-1] == dz[0]).all()

@@ -107,6 +107,15 @@ def test_no_rows_need_no_device():
     assert backward_input(g=groups_of(n=0, plan=None), dy=None, dx=None) == pnn.PNN_OK
 
 
+def test_the_header_is_plain_c(tmp_path):
+    import os
+    import subprocess
+    header = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "pnn.h")
+    c = tmp_path / "use.c"
+    c.write_text(f'#include "{header}"\nint main(void) {{ return sizeof(pnn_groups) + sizeof(pnn_group_layer) + sizeof(pnn_distill) == 0; }}\n')
+    subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-fsyntax-only", str(c)])
+
+
 def test_the_binding_refuses_what_it_cannot_pass():
     with pytest.raises(ValueError):
         pnn.group_rows(torch.zeros(4, dtype=torch.int64), 2)
@@ -387,3 +396,66 @@ def test_another_stream_and_a_graph(n):
         torch.cuda.synchronize()
         for a, b in zip(kept, step()):
             assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("n", [40, 900])
+def test_shared_weights_and_a_network_named_twice(n):
+    """Networks that share their weights (a stride of 0 between them), and rows that name one network in all pairs."""
+    c = Case(n, 3, 4, 40, 24, F32)
+    ids = torch.randint(0, 4, (n, 1), dtype=torch.int32, device="cuda").expand(n, 3).contiguous()
+    g = pnn.group_rows(ids, 4)
+    w = c.w[:1].expand(4, 24, 40)
+    y = pnn.grouped_forward(g, c.x, w)
+    want = c.x.double() @ c.w[0].double().T
+    size = c.x.double().abs() @ c.w[0].double().abs().T
+    close(y, want.repeat_interleave(3, 0), size.repeat_interleave(3, 0), 40)
+    dx = pnn.grouped_backward_input(g, y, w)
+    d = y.double().view(n, 3, 24).sum(1)
+    close(dx, d @ c.w[0].double(), y.double().abs().view(n, 3, 24).sum(1) @ c.w[0].double().abs(), 72)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_thousand_networks(dtype):
+    c = Case(3000, 1, 1024, 24, 16, dtype)
+    want, size = c.forward(None, 1.0)
+    close(pnn.grouped_forward(c.groups, c.x, c.w, c.b), want, size, 24)
+    dw, db = pnn.grouped_backward_weights(c.groups, c.dy, c.x)
+    want, size, bwant, bsize = c.backward_weights()
+    close(dw, want, size, 3000)
+    close(db, bwant, bsize, 3000)
+
+
+@gpu
+def test_two_threads_on_two_streams():
+    """Calls without a handle at the same time, from two host threads, each on its own stream."""
+    import threading
+    cases = [Case(700, 2, 5, 72, 88, BF16, seed=s) for s in (1, 2)]
+
+    def step(c, stream=None):
+        g = pnn.group_rows(c.ids.cuda(), 5, stream=stream)
+        y = pnn.grouped_forward(g, c.x, c.w, c.b, act=pnn.TANH, stream=stream)
+        return (y, pnn.grouped_backward_input(g, y, c.w, stream=stream), *pnn.grouped_backward_weights(g, y, c.x, stream=stream))
+
+    want = [step(c) for c in cases]
+    torch.cuda.synchronize()
+    got, failed = [None, None], []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            for _ in range(30):
+                got[i] = step(cases[i], stream)
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w))

@@ -319,3 +319,31 @@ def test_refusals():
     net.infer_routed(x, ids, infer_pred)  # the handles still work
     soft.train_routed(x, ids, idx, t, y, 2.0, 0.5)
     torch.cuda.synchronize()
+
+
+@gpu
+def test_a_deferred_broadcast_is_not_recorded():
+    """The copy that a merge leaves to the next call is made by an eager call, not by every replay of a graph."""
+    net = network((784, 256, 10), (pnn.SIGMOID, pnn.SOFTMAX), 4, batch=128, lr=0.1)
+    assert net.plan == "mini-batch fused last layer"
+    x, ids, idx, t, y = (v.cuda() for v in batch(40, 1, net, 5))
+    pred = torch.empty(40, dtype=torch.int32, device="cuda")
+    net.infer_routed(x, ids, pred)
+    net.merge(broadcast=True)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(pnn.PnnError) as e:
+        with torch.cuda.graph(graph):
+            net.infer_routed(x, ids, pred)
+    assert e.value.status == pnn.PNN_EHIP and "broadcast" in str(e.value)
+    out = torch.empty(40, 10, device="cuda")
+    net.infer_routed(x, ids, pred, out=out)  # makes it
+    assert all(np.array_equal(net.get_params(k), net.get_params(-1)) for k in range(4))
+    graph = torch.cuda.CUDAGraph()
+    kept = torch.empty_like(out)
+    with torch.cuda.graph(graph):
+        net.infer_routed(x, ids, pred, out=kept)
+    for _ in range(3):
+        kept.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(kept, out)
