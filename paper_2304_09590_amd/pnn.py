@@ -364,13 +364,21 @@ def _on(stream, body, first, *others):
             return body(stream.cuda_stream)
 
 
+_TYPES = {}
+
+
 def _type_of(t) -> int:
-    torch = _t()
-    if t.dtype is torch.float32:
-        return FP32
-    if t.dtype is torch.bfloat16:
-        return BF16_MIXED
-    raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    if not _TYPES:
+        _TYPES.update({_t().float32: FP32, _t().bfloat16: BF16_MIXED})
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _empty(like, shape, dtype=None):
+    """New memory beside a tensor (new_empty, which costs less than a device and a type to parse)."""
+    return like.new_empty(shape) if dtype is None or dtype is like.dtype else like.new_empty(shape, dtype=dtype)
 
 
 def _rows(t, name: str, shape, dtype):
@@ -380,9 +388,10 @@ def _rows(t, name: str, shape, dtype):
     if t.dtype is not dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
     strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
+    width = shape[-1]
+    if strides[-1] != 1 and width > 1:
         raise ValueError(f"the values of a row of {name} are not contiguous")
-    return t.data_ptr(), (strides[-2] if shape[-2] > 1 else shape[-1])
+    return t.data_ptr(), (strides[-2] if shape[-2] > 1 else width)
 
 
 def _values(t, name: str, shape, dtype):
@@ -435,7 +444,7 @@ def group_rows(ids, networks: int, stream=None) -> RowGroups:
 
     def body(s):
         size = _group_bytes(n, per_row, networks)
-        plan = torch.empty(size // 4, dtype=torch.int32, device=ids.device)
+        plan = _empty(ids, size // 4)
         _call("pnn_group_rows", ids.data_ptr(), n, per_row, networks, plan.data_ptr(), size, s)
         return plan
 
@@ -446,11 +455,11 @@ def _weights(groups: RowGroups, w, b=None) -> PnnGroupLayer:
     shape = w.shape
     if len(shape) != 3 or shape[0] != groups.networks:
         raise ValueError(f"w has shape {tuple(shape)}, expected ({groups.networks}, outputs, inputs)")
-    ptr, ld = _rows(w, "w", shape, w.dtype)
-    layer = PnnGroupLayer(shape[2], shape[1], _type_of(w), ptr, w.stride(0), ld, None, 0)
-    if b is not None:
-        layer.b, layer.b_net = _rows(b, "b", shape[:2], _t().float32)
-    return layer
+    net, ld, one = w.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError("the values of a row of w are not contiguous")
+    pb, b_net = _rows(b, "b", shape[:2], _t().float32) if b is not None else (None, 0)
+    return PnnGroupLayer(shape[2], shape[1], _type_of(w), w.data_ptr(), net, ld if shape[1] > 1 else shape[2], pb, b_net)
 
 
 def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, out=None, out_dtype=None, stream=None):
@@ -460,7 +469,7 @@ def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, 
     shape = (groups.n * groups.per_row, layer.outputs)
 
     def body(s):
-        y = out if out is not None else _t().empty(shape, dtype=out_dtype or x.dtype, device=x.device)
+        y = out if out is not None else _empty(x, shape, out_dtype)
         px, ldx = _rows(x, "x", (groups.n, layer.inputs), w.dtype)
         py, ldy = _rows(y, "out", shape, out_dtype or y.dtype)
         _call("pnn_grouped_forward", ctypes.byref(groups.struct), ctypes.byref(layer), px, ldx, -1 if act is None else act,
@@ -470,11 +479,11 @@ def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, 
     return _on(stream, body, x, groups.plan, w, b, out)
 
 
-def _workspace(groups: RowGroups, layer: PnnGroupLayer, device, which: int):
+def _workspace(groups: RowGroups, layer: PnnGroupLayer, like, which: int):
     size = _group_workspace(groups.n, groups.per_row, groups.networks, layer.inputs, layer.outputs, layer.type)[which]
     if size == 0:
         return None, None, 0
-    ws = _t().empty(size, dtype=_t().uint8, device=device)
+    ws = _empty(like, size, _t().uint8)
     return ws, ws.data_ptr(), size
 
 
@@ -487,11 +496,11 @@ def grouped_backward_input(groups: RowGroups, dy, w, a=None, act: Optional[int] 
         raise ValueError("a and act go together")
 
     def body(s):
-        dx = out if out is not None else _t().empty(shape, dtype=out_dtype or dy.dtype, device=dy.device)
+        dx = out if out is not None else _empty(dy, shape, out_dtype)
         pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), w.dtype)
         pa, lda = _rows(a, "a", shape, w.dtype) if a is not None else (None, 0)
         po, ldo = _rows(dx, "out", shape, out_dtype or dx.dtype)
-        ws, pw, size = _workspace(groups, layer, dy.device, 0)
+        ws, pw, size = _workspace(groups, layer, dy, 0)
         _call("pnn_grouped_backward_input", ctypes.byref(groups.struct), ctypes.byref(layer), pd, ldd, pa, lda,
               -1 if act is None else act, po, ldo, _type_of(dx), pw, size, s)
         return dx
@@ -509,13 +518,13 @@ def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: b
     shape = (groups.networks, layer.outputs, layer.inputs)
 
     def body(s):
-        w = dw if dw is not None else torch.empty(shape, dtype=torch.float32, device=x.device)
-        b = db if db is not None or not bias else torch.empty(shape[:2], dtype=torch.float32, device=x.device)
+        w = dw if dw is not None else _empty(x, shape, torch.float32)
+        b = db if db is not None or not bias else _empty(x, shape[:2], torch.float32)
         pd, ldd = _rows(dy, "dy", (groups.n * groups.per_row, layer.outputs), x.dtype)
         px, ldx = _rows(x, "x", (groups.n, layer.inputs), x.dtype)
         pw, ldw = _rows(w, "dw", shape, torch.float32)
         pb, netb = _rows(b, "db", shape[:2], torch.float32) if b is not None else (None, 0)
-        ws, ps, size = _workspace(groups, layer, x.device, 1)
+        ws, ps, size = _workspace(groups, layer, x, 1)
         _call("pnn_grouped_backward_weights", ctypes.byref(groups.struct), ctypes.byref(layer), pd, ldd, px, ldx, pw,
               w.stride(0), ldw, pb, netb, ps, size, s)
         return w, b
@@ -549,8 +558,8 @@ def distill_loss(z, idx, t, y=None, temperature: float = 1.0, alpha: float = 0.0
 
     def body(s):
         size = _distill_bytes(a.n, a.classes)
-        loss = torch.empty(a.n, dtype=torch.float32, device=z.device)
-        stats = torch.empty(size // 4, dtype=torch.float32, device=z.device)
+        loss = _empty(z, a.n, torch.float32)
+        stats = _empty(z, size // 4, torch.float32)
         _call("pnn_distill_loss", ctypes.byref(a), loss.data_ptr(), stats.data_ptr(), size, s)
         return loss, stats
 
@@ -564,7 +573,7 @@ def distill_grad(z, idx, t, stats, g=None, y=None, temperature: float = 1.0, alp
     a = _distill(z, idx, t, y, temperature, alpha)
 
     def body(s):
-        dz = out if out is not None else torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        dz = out if out is not None else _empty(z, z.shape)
         pg = _values(g, "g", (a.n,), torch.float32) if g is not None else None
         ps = _values(stats, "stats", stats.shape, torch.float32)
         po, ldo = _rows(dz, "out", z.shape, z.dtype)
