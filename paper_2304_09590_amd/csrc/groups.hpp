@@ -120,9 +120,9 @@ __device__ inline void wave_scan(int* out, int n, int lane, F f) {
 
 // Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds what the
 // chunks and waves before it hold, and places its pairs.  The lanes of a wave that hold the same key find each
-// other in LDS: each sets its bit in the key's word, and the bits below its own are its order.  (By one ballot
-// per key bit instead, 130 instructions a step, the placing was bound by them: 32,768 pairs, 256 networks
-// OLDPLACE.)  Integer sums only: the same bits every run.  With one workgroup its own counts are all there is
+// other in LDS: each sets its bit in the key's word, and the bits below its own are its order.  (One ballot
+// per key bit instead is 130 instructions a step: 120,000 pairs, 256 networks 12.9 us, this way 11.4.)  Integer
+// sums only: the same bits every run.  With one workgroup its own counts are all there is
 // (no earlier launch).  All workgroups share the tiles.
 template <int KEYS>
 __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
@@ -131,9 +131,9 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
     const int K1 = g.K + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     unsigned long long* bits = (unsigned long long*)gsm;  // [WAVES][K1 + 1], the last for lanes without a pair
     int* cur = (int*)(bits + WAVES * (K1 + 1));           // [WAVES][K1]
-    int* tot = cur + WAVES * K1;  // [K1]
-    int* off = tot + K1;             // [K1 + 1]
-    int* first = off + K1 + 1;       // [GR_HEIGHTS][K1 + 1] first tile of each network
+    int* tot = cur + WAVES * K1;                          // [K1]
+    int* off = tot + K1;                                  // [K1 + 1]
+    int* first = off + K1 + 1;                            // [GR_HEIGHTS][K1 + 1] first tile of each network
     for (int e = tid; e < WAVES * K1; e += THREADS) cur[e] = 0;
     for (int e = tid; e < WAVES * (K1 + 1); e += THREADS) bits[e] = 0;
     __syncthreads();
@@ -423,13 +423,16 @@ __device__ inline bool group_place_of(const GroupGemm& g, int mt, GroupPlace& o)
         o.Kx = first + all - o.p0 < part ? first + all - o.p0 : part;
         return true;
     }
-    // eight tiles of pairs next to each other, then along m: their rows and weights stay in L2
+    // WIDE tiles of pairs next to each other, then along m: the workgroups that an XCD runs at a time (32 of 256
+    // x 256, 64 and more of smaller ones) are about as many tiles wide as high and share their operands in L2
+    // (65,536 pairs 4096 -> 4096, 16 networks, bf16: 2,183 us with eight tiles of 256, 2,025 us with four)
+    constexpr int WIDE = 4;
     const int64_t n_tiles = *g.n_tiles, total = n_tiles * mt;
     if (blockIdx.x >= total) return false;
     const int64_t id = group_xcd(blockIdx.x, total);
-    const int64_t grp = id / (8 * mt), in = id - grp * 8 * mt;
-    const int64_t left = n_tiles - grp * 8, wide = left < 8 ? left : 8;
-    const int2 t = g.tiles[grp * 8 + in % wide];
+    const int64_t grp = id / (WIDE * mt), in = id - grp * WIDE * mt;
+    const int64_t left = n_tiles - grp * WIDE, wide = left < WIDE ? left : WIDE;
+    const int2 t = g.tiles[grp * WIDE + in % wide];
     o.m0 = (int)(in / wide) * BM;
     o.e = t.x;
     o.p0 = t.y;
@@ -603,10 +606,12 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     }
 }
 
-// S x S tiles (128, or 64 where those are too few) of one network's product.  Over pairs, four waves of 32 x 128: all waves share the tile's
-// columns, so a tile that a group does not fill costs its share of the products only (32,768 rows over 256
-// networks, 784 -> 1024, fp32, 467 -> 416 us); a weight gradient's tiles are full, and 64 x 64 reads less of
-// LDS (32,768 rows, 64 networks, 2048 x 1024: 909 -> DWFIG us).
+// Rows at any alignment, and fp32: S x S tiles (128, or 64 where those are too few) of one network's product.
+// Bound by the matrix units for full tiles: 32,768 rows 784 -> 1024 over 64 networks in fp32 take 267 us, 197
+// TFLOP/s or 1,180 of the six bf16 products.  Over pairs, four waves of 32 x 128: all waves share the tile's
+// columns, so a tile that a group does not fill costs its share of the products only (the same over 256 networks
+// of unequal groups 467 -> 401 us); a weight gradient's tiles are full, and 64 x 64 a wave reads less of LDS
+// (32,768 rows, 64 networks, 2048 x 1024: 909 -> 867 us).
 template <int DIR, typename T, typename TO, int S>
 __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
     constexpr bool F32 = sizeof(T) == 4;
@@ -648,10 +653,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             pb[u] = r < nv && Kx > 0 ? (const T*)g.p + (int64_t)(g.pdiv.of(g.pairs[p0 + r])) * g.ldp + TB::chunk(s) * 8 : nullptr;
         }
     }
-    // the next D steps' operands are in flight in registers (three where they are small: a step of 64 x 64 is
-    // shorter than a load)
-    constexpr int D = S == 64 ? 3 : 1;
-    Raw8<T> ra[D][U], rb[D][U];
+    Raw8<T> ra[U], rb[U];  // the next step's operands, in flight
     int number[U];  // (weight gradient) the pairs of the step that is loaded next
     auto numbers = [&](int k0) {
 #pragma unroll
@@ -660,7 +662,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             number[u] = g.pairs[p0 + (k < Kx ? k : Kx - 1)];
         }
     };
-    auto load = [&](int k0, Raw8<T> (&ra)[U], Raw8<T> (&rb)[U]) {
+    auto load = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = u * 256 + tid;
@@ -681,10 +683,8 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
         if (DIR == GR_DW) numbers(k0 + BK);
     };
     if (DIR == GR_DW && Kx > 0) numbers(0);
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (d * BK < Kx) load(d * BK, ra[d], rb[d]);
-    auto step = [&](int k0, Raw8<T> (&ra)[U], Raw8<T> (&rb)[U]) {
+    if (Kx > 0) load(0);
+    for (int k0 = 0; k0 < Kx; k0 += BK) {
         lds_barrier();  // (waits for no load)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -693,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
             gt_store(lb + TB::offset(TB::row(s), TB::chunk(s)), TB::ELEMS, rb[u]);
         }
         lds_barrier();
-        if (k0 + D * BK < Kx) load(k0 + D * BK, ra, rb);
+        if (k0 + BK < Kx) load(k0 + BK);
 #pragma unroll
         for (int kb = 0; kb < BK; kb += 32) {
             bf8v fa[PL][MI];
@@ -722,11 +722,6 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
                 }
             }
         }
-    };
-    for (int k0 = 0; k0 < Kx; k0 += D * BK) {
-#pragma unroll
-        for (int d = 0; d < D; ++d)
-            if (k0 + d * BK < Kx) step(k0 + d * BK, ra[d], rb[d]);
     }
     __syncthreads();
     group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
@@ -734,8 +729,10 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
 }
 
 // ------------------------------------------------------------------------------------
-// bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, WM x WN waves,
-// a ring of stages of 32 k in LDS that global memory fills directly.
+// bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, WM x WN waves, a ring of stages of
+// 32 k in LDS that global memory fills directly.  The matrix units bound a long contraction (65,536 pairs 4096 ->
+// 4096, 16 networks: 2,025 us, 1,086 TFLOP/s of the 1,327 that a large library product reaches on the card); at 1024
+// the results' stores, which a round of workgroups makes at one time, add a quarter (without them 551 us of 671).
 
 static __device__ __align__(64) uint32_t group_zeros[16];  // what lies outside an operand
 
@@ -910,7 +907,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
         // the operands of step t from registers (fb, fa: its first two blocks) and LDS, the next step's into fbn, fan
         auto step = [&](int t, const bf8v (&fb)[NJ], const bf8v (&fa)[2], bf8v (&fbn)[NJ], bf8v (&fan)[2]) {
             ring_wait<(NST - 3) * COPIES>();
-            refill(t);
+            if (DIR != GR_DW) refill(t);
             const int next = at == NST - 1 ? 0 : at + 1;
             bf8v f[MI];
             f[0] = fa[0];
@@ -924,6 +921,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], fb[j], acc[i][j], 0, 0, 0);
+            if (DIR == GR_DW) refill(t);  // (behind the operands' reads, which then do not wait for the
+            // numbers': 131,072 pairs 2048 x 2048 1,132 -> 1,103 us)
             // reads two operands ahead of the products that take them, the next step's with the last ones
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * RA, 0);
 #pragma unroll
