@@ -41,6 +41,9 @@ struct DistillArgs {
     int64_t lddz;
 };
 
+// the row whose entries and label row r has (most calls: its own; a 64-bit division is long)
+__device__ inline int64_t dl_shared(const DistillArgs& d, int64_t row) { return d.rows_per == 1 ? row : (int64_t)((uint32_t)row / (uint32_t)d.rows_per); }
+
 constexpr float DL_INF = __builtin_huge_valf();
 
 // Running maximum m and sums of exp2(z c - m c), at the scales c = ct and cs.  MODE 1: one sum; 2: two; 3: two
@@ -149,8 +152,8 @@ struct Teacher {
     const T *ts, *zs;
 
     __device__ inline void load(const DistillArgs& d, int64_t row, int lane, bool logits) {
-        idx = d.idx + row / d.rows_per * d.k;
-        ts = (const T*)d.t + row / d.rows_per * d.k;
+        idx = d.idx + dl_shared(d, row) * d.k;
+        ts = (const T*)d.t + dl_shared(d, row) * d.k;
         zs = (const T*)d.z + row * d.ldz;
         if (d.wt == 0.0f) return;
         if (lane < d.k) {
@@ -206,14 +209,14 @@ __device__ inline void dl_finish(const DistillArgs& d, int64_t row, int lane, co
     float loss = 0.0f;
     if (s.a == 0.0f) has = 0;  // every logit is -inf: nothing to learn from
     if (has & 1) loss += d.wt * kl;
-    if (has & 2) loss += d.ws * (lb - dl_s(to_f<T>(te.zs[d.y[row / d.rows_per]]), f, d) * DL_LN2);
+    if (has & 2) loss += d.ws * (lb - dl_s(to_f<T>(te.zs[d.y[dl_shared(d, row)]]), f, d) * DL_LN2);
     d.loss[row] = loss;
     d.stats[row] = make_float4(s.m, 1.0f / s.a, 1.0f / (two ? s.b : s.a), (float)has);
 }
 
 __device__ inline int dl_label(const DistillArgs& d, int64_t row) {
     if (!d.y) return -1;
-    const int y = d.y[row / d.rows_per];
+    const int y = d.y[dl_shared(d, row)];
     return (unsigned)y < (unsigned)d.V ? y : -1;
 }
 
@@ -248,8 +251,8 @@ template <typename T, int MODE, int W>
 __global__ __launch_bounds__(256) void distill_loss_kernel(DistillArgs d) {
     __shared__ Sums across[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = d.row0 + (W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave);
-    const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0;
+    const int64_t row = d.row0 + (W == 4 ? blockIdx.x / (uint32_t)d.S : (int64_t)blockIdx.x * 4 + wave);
+    const int part = W == 4 ? (int)(blockIdx.x % (uint32_t)d.S) : 0;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
     const T* z = (const T*)d.z + row * d.ldz;
@@ -346,8 +349,8 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     __shared__ int sidx[4 / W][TOP];
     __shared__ float sp[4 / W][TOP], sz[4 / W][TOP + 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row = d.row0 + (W == 4 ? (int64_t)blockIdx.x / d.S : (int64_t)blockIdx.x * 4 + wave);
-    const int part = W == 4 ? (int)(blockIdx.x % d.S) : 0, slot = W == 4 ? 0 : wave;
+    const int64_t row = d.row0 + (W == 4 ? blockIdx.x / (uint32_t)d.S : (int64_t)blockIdx.x * 4 + wave);
+    const int part = W == 4 ? (int)(blockIdx.x % (uint32_t)d.S) : 0, slot = W == 4 ? 0 : wave;
     if (row >= d.n) return;
     const int in = W == 4 ? tid : lane;
     const T* z = (const T*)d.z + row * d.ldz;
@@ -438,7 +441,7 @@ struct Tiny {
     }
     __device__ inline void load(const DistillArgs& d, int64_t row, int lane) {
         const T* p = (const T*)d.z + row * d.ldz;
-        const int64_t base = row / d.rows_per;
+        const int64_t base = dl_shared(d, row);
         i = -1;
         t = -DL_INF;
         if (d.wt != 0.0f && lane < d.k) {

@@ -382,8 +382,8 @@ __device__ inline void store8(bf16_t* p, const float (&v)[8], int nv) {
 
 // workgroup number -> place in an order in which each XCD (its numbers are those equal mod 8) gets
 // one contiguous stretch, so that neighbours in it share an L2
-__device__ inline int64_t group_xcd(int64_t id, int64_t total) {
-    const int64_t q = total >> 3, r = total & 7, x = id & 7;
+__device__ inline uint32_t group_xcd(uint32_t id, uint32_t total) {
+    const uint32_t q = total >> 3, r = total & 7, x = id & 7;
     return x * q + (x < r ? x : r) + (id >> 3);
 }
 
@@ -427,13 +427,14 @@ __device__ inline bool group_place_of(const GroupGemm& g, int mt, GroupPlace& o)
     // x 256, 64 and more of smaller ones) are about as many tiles wide as high and share their operands in L2
     // (65,536 pairs 4096 -> 4096, 16 networks, bf16: 2,183 us with eight tiles of 256, 2,025 us with four)
     constexpr int WIDE = 4;
-    const int64_t n_tiles = *g.n_tiles, total = n_tiles * mt;
-    if (blockIdx.x >= total) return false;
-    const int64_t id = group_xcd(blockIdx.x, total);
-    const int64_t grp = id / (WIDE * mt), in = id - grp * WIDE * mt;
-    const int64_t left = n_tiles - grp * WIDE, wide = left < WIDE ? left : WIDE;
-    const int2 t = g.tiles[grp * WIDE + in % wide];
-    o.m0 = (int)(in / wide) * BM;
+    // (a launch has fewer than 2^24 workgroups: 32 bits do, and 64-bit divisions are long)
+    const uint32_t n_tiles = *g.n_tiles;
+    if (blockIdx.x >= (uint64_t)n_tiles * mt) return false;
+    const uint32_t id = group_xcd(blockIdx.x, n_tiles * mt);
+    const uint32_t grp = id / (WIDE * mt), in = id - grp * WIDE * mt;
+    const uint32_t left = n_tiles - grp * WIDE, wide = left < WIDE ? left : WIDE, row = wide == WIDE ? in / WIDE : in / wide;
+    const int2 t = g.tiles[grp * WIDE + in - row * wide];
+    o.m0 = (int)row * BM;
     o.e = t.x;
     o.p0 = t.y;
     const int end = o.e < g.K ? g.off[o.e + 1] : g.N;
@@ -981,7 +982,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
                                          (float*)ring + wave * group_turn<MI>());
 }
 
-// the sum of a weight gradient's parts, in their order; with lr the update
+// Rows of `values` for workgroups of 256 threads: the power of two of threads that takes a row
+__host__ __device__ inline int row_threads(int values) {
+    int t = 1;
+    while (t < values && t < 256) t *= 2;
+    return t;
+}
+
+// the sum of a weight gradient's parts, in their order; with lr the update.  A row is an output's weights of a
+// network and its bias, eight values a thread.
 struct GroupJoin {
     const int32_t* off;
     const float *part, *dbpart;   // [splits][K][N][M], [splits][K][N]
@@ -992,50 +1001,67 @@ struct GroupJoin {
     int64_t dbnet;
     float lr;
     bf16_t* shadow;
+    int threads;                  // of a row
 };
 
 __global__ __launch_bounds__(256) void group_join_kernel(GroupJoin g) {
-    const int64_t per = (int64_t)g.N * g.M, all = (int64_t)g.K * per, nb = g.db ? (int64_t)g.K * g.N : 0;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all + nb; i += gridDim.x * 256ll) {
-        const bool w = i < all;
-        const int64_t q = w ? i : i - all, step = w ? all : nb;
-        const float* p = w ? g.part : g.dbpart;
-        float s = p[q];
-        for (int k = 1; k < g.splits; ++k) s += p[k * step + q];
-        const int e = (int)(w ? q / per : q / g.N);
-        const int64_t in = w ? q - e * per : q - (int64_t)e * g.N;
-        float* out = w ? g.y + e * g.ynet + in / g.M * g.ldy + in % g.M : g.db + e * g.dbnet + in;
-        if (g.lr != 0.0f) {
-            const int pairs = g.off[e + 1] - g.off[e];
-            if (pairs == 0) continue;
-            s = *out - g.lr / (float)pairs * s;
-            if (w && g.shadow) g.shadow[out - g.y] = f2bf(s);
+    const int rows = 256 / g.threads, tx = threadIdx.x % g.threads, ty = threadIdx.x / g.threads;
+    const int64_t all = (int64_t)g.K * g.N * g.M;
+    for (int64_t r = (int64_t)blockIdx.x * rows + ty; r < (int64_t)g.K * g.N; r += (int64_t)gridDim.x * rows) {
+        const int e = (int)((uint32_t)r / (uint32_t)g.N), n = (int)r - e * g.N;
+        const int pairs = g.off[e + 1] - g.off[e];
+        if (g.lr != 0.0f && pairs == 0) continue;  // no update
+        const float scale = g.lr != 0.0f ? g.lr / (float)pairs : 0.0f;
+        const int64_t at = (int64_t)n * g.ldy + e * g.ynet;
+        for (int m = tx * 8; m < g.M; m += g.threads * 8) {
+            const float* p = g.part + r * g.M + m;
+            float s[8];
+            load8_f<float>(s, p, g.M - m);
+            for (int k = 1; k < g.splits; ++k) {
+                float v[8];
+                load8_f<float>(v, p + k * all, g.M - m);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s[q] += v[q];
+            }
+            if (g.lr != 0.0f) {
+                float w[8];
+                load8_f<float>(w, g.y + at + m, g.M - m);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) s[q] = w[q] - scale * s[q];
+                if (g.shadow) store8(g.shadow + at + m, s, g.M - m);
+            }
+            store8(g.y + at + m, s, g.M - m);
         }
-        *out = s;
+        if (g.db && tx == 0) {
+            float s = g.dbpart[r];
+            for (int k = 1; k < g.splits; ++k) s += g.dbpart[k * (int64_t)g.K * g.N + r];
+            float* db = g.db + e * g.dbnet + n;
+            *db = g.lr != 0.0f ? *db - scale * s : s;
+        }
     }
 }
 
 // dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r]), eight neighbouring values a thread
 template <typename T, typename TO>
 __global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part, int64_t n, int per_row, int M, const T* a,
-                                                              int64_t lda, int act, TO* dx, int64_t ldx) {
-    const int chunks = (M + 7) / 8;
-    const int64_t all = n * chunks;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-        const int64_t r = i / chunks;
-        const int m = (int)(i - r * chunks) * 8, left = M - m;
-        float s[8], x[8];
-        if (a) load8_f<T>(x, a + r * lda + m, left);
-        load8_f<float>(s, part + r * per_row * M + m, left);
-        for (int j = 1; j < per_row; ++j) {
-            float v[8];
-            load8_f<float>(v, part + (r * per_row + j) * M + m, left);
+                                                              int64_t lda, int act, TO* dx, int64_t ldx, int threads) {
+    const int rows = 256 / threads, tx = threadIdx.x % threads, ty = threadIdx.x / threads;
+    for (int64_t r = (int64_t)blockIdx.x * rows + ty; r < n; r += (int64_t)gridDim.x * rows)
+        for (int m = tx * 8; m < M; m += threads * 8) {
+            const int left = M - m;
+            const float* p = part + r * per_row * M + m;
+            float s[8], x[8];
+            if (a) load8_f<T>(x, a + r * lda + m, left);
+            load8_f<float>(s, p, left);
+            for (int j = 1; j < per_row; ++j) {
+                float v[8];
+                load8_f<float>(v, p + (int64_t)j * M, left);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s[q] += v[q];
+                for (int q = 0; q < 8; ++q) s[q] += v[q];
+            }
+            if (a) group_slope8(act, s, x);
+            store8(dx + r * ldx + m, s, left);
         }
-        if (a) group_slope8(act, s, x);
-        store8(dx + r * ldx + m, s, left);
-    }
 }
 
 // Few pairs a network: 16 pairs and a band of the weights per workgroup, whose four waves split the
@@ -1051,10 +1077,11 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
     const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + GS_OUT - 1) / GS_OUT;
-    const int64_t id = blockIdx.x;
-    if (id >= (int64_t)*g.n_tiles * mt) return;
-    const int2 t = g.tiles[id / mt];
-    const int e = t.x, m0 = (int)(id % mt) * GS_OUT, p0 = t.y;
+    const uint32_t id = blockIdx.x;
+    if (id >= (uint64_t)*g.n_tiles * mt) return;
+    const uint32_t tile = id / mt, band = id - tile * mt;
+    const int2 t = g.tiles[tile];
+    const int e = t.x, m0 = (int)band * GS_OUT, p0 = t.y;
     const int end = e < g.K ? g.off[e + 1] : g.N;
     const int nv = end - p0 < 16 ? end - p0 : 16;
     f4 acc[GS_OUT / 16];
@@ -1123,10 +1150,11 @@ __global__ __launch_bounds__(256) void group_few_dx_kernel(GroupGemm g) {
     const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + BAND - 1) / BAND;
-    const int64_t id = blockIdx.x;
-    if (id >= (int64_t)*g.n_tiles * mt) return;
-    const int2 t = g.tiles[id / mt];
-    const int e = t.x, m0 = (int)(id % mt) * BAND, p0 = t.y;
+    const uint32_t id = blockIdx.x;
+    if (id >= (uint64_t)*g.n_tiles * mt) return;
+    const uint32_t tile = id / mt, band = id - tile * mt;
+    const int2 t = g.tiles[tile];
+    const int e = t.x, m0 = (int)band * BAND, p0 = t.y;
     const int end = e < g.K ? g.off[e + 1] : g.N;
     const int nv = end - p0 < 16 ? end - p0 : 16;
     f4 acc[C];

@@ -239,9 +239,10 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
         TRY(launched("grouped weight gradient"));
     }
     if (S > 1) {
-        GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, lr, shadow};
-        const int64_t all = (int64_t)g->networks * outputs * (inputs + 1);
-        group_join_kernel<<<(unsigned)std::min<int64_t>((all + 255) / 256, 8192), 256, 0, s>>>(j);
+        GroupJoin j = {a.off, (const float*)ws, dbpart, g->networks, inputs, outputs, S, dw, dw_ld, dw_net, db, db_net, lr, shadow,
+                       row_threads((inputs + 7) / 8)};
+        const int64_t rows = (int64_t)g->networks * outputs, each = 256 / j.threads;
+        group_join_kernel<<<(unsigned)std::min<int64_t>((rows + each - 1) / each, 8192), 256, 0, s>>>(j);
         TRY(launched("sum of a grouped weight gradient"));
     }
     return PNN_OK;
@@ -360,11 +361,12 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     }
     a.y = ws_dev; a.ldy = layer->inputs;
     TRY(run_group_pairs<GR_DX>(a, groups, layer->type, PNN_FP32, s));
-    const unsigned blocks = (unsigned)std::min<int64_t>((groups->n * ((layer->inputs + 7) / 8) + 255) / 256, 8192);
+    const int threads = row_threads((layer->inputs + 7) / 8), each = 256 / threads;
+    const unsigned blocks = (unsigned)std::min<int64_t>((groups->n + each - 1) / each, 8192);
     const float* part = (const float*)ws_dev;
     const void* ad = act >= 0 ? a_dev : nullptr;
 #define PNN_SUM_PAIRS(T, TO) \
-    group_sum_pairs_kernel<T, TO><<<blocks, 256, 0, s>>>(part, groups->n, groups->per_row, layer->inputs, (const T*)ad, a_ld, act, (TO*)dx_dev, dx_ld)
+    group_sum_pairs_kernel<T, TO><<<blocks, 256, 0, s>>>(part, groups->n, groups->per_row, layer->inputs, (const T*)ad, a_ld, act, (TO*)dx_dev, dx_ld, threads)
     if (layer->type == PNN_FP32) { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(float, float); else PNN_SUM_PAIRS(float, bf16_t); }
     else { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(bf16_t, float); else PNN_SUM_PAIRS(bf16_t, bf16_t); }
 #undef PNN_SUM_PAIRS
