@@ -39,6 +39,7 @@ struct DistillArgs {
     const float* g;
     void* dz;
     int64_t lddz;
+    bool stream = false;      // dz passes the caches by
 };
 
 // the row whose entries and label row r has (most calls: its own; a 64-bit division is long)
@@ -402,7 +403,8 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
         r[0] = r[1];
         load8(r[1], z + v + W * 1024, hi - v - W * 1024);
         dl_grad8<MODE>(d, x, f, ka, kb);
-        store8(dz + v, x, hi - v);
+        if (d.stream) store8<true>(dz + v, x, hi - v);
+        else store8(dz + v, x, hi - v);
     }
     meet();  // (waits for the stores: those below come after them)
     for (int j = in; j < k; j += 64 * W) {

@@ -165,6 +165,11 @@ pnn_status pnn_distill_grad(const pnn_distill* a, const float* g_dev, const void
     const int width = distill_width(a->n, a->classes, a->top);
     DistillArgs d = distill_args(a, const_cast<void*>(stats_dev), width);
     d.g = g_dev; d.dz = dz_dev; d.lddz = dz_ld;
+    // The gradient is streamed where the logits, read again by row, and it exceed the 256 MB memory-side cache together.
+    // Loss and gradient in us, cached -> streamed, and with a reader of the gradient: 32,000 classes in bf16, 131 MB
+    // 79 -> 79, 129 -> 125; 147 MB 94 -> 93, 166 -> 146; 262 MB 186 -> 161, 273 -> 269; 16,000 classes in fp32, 98 MB
+    // 57 -> 66, 87 -> 95; 131 MB 77 -> 84, 131 -> 131; 147 MB 86 -> 92, 164 -> 146; 262 MB 183 -> 159, 271 -> 264.
+    d.stream = a->n * a->classes * (int64_t)type_size(a->type) > (int64_t(128) << 20);
     const int mode = distill_mode(a);
     return a->type == PNN_FP32 ? run_distill_grad<float>(d, mode, width, s) : run_distill_grad<bf16_t>(d, mode, width, s);
 }

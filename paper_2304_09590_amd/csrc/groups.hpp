@@ -286,6 +286,7 @@ struct GroupGemm {
     int64_t lda;
     void* y;                   // result; fp32 gradients of a weight gradient
     int64_t ldy, ynet;
+    bool stream = false;       // the result's rows pass the caches by
     float* db;                 // (weight gradient) bias gradient, nullable
     int64_t dbnet;
     int splits;                // (weight gradient) parts of a group, summed by group_join_kernel
@@ -352,15 +353,18 @@ __device__ inline void load8_f(float (&v)[8], const T* p, int nv) {
     raw8_f(v, r);
 }
 
-// the first nv of eight values
-// (STREAM: whole rows of a large result, which pass the caches by: the writes of a round of workgroups,
-// 33 MB at once, evict what the next round reads; forward 65,536 pairs 1024 -> 4096, 16 networks, bf16
-// 669 -> 597 us, input gradient 32,768 pairs 2048 x 2048 274 -> 238 us; fp32 results lose by it)
+// the first nv of eight values; streamed past the caches where a result is too large to be found there again
 template <bool STREAM = false>
 __device__ inline void store8(float* p, const float (&v)[8], int nv) {
     if (nv >= 8) {
-        *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
-        *(f4_a4*)(p + 4) = f4{v[4], v[5], v[6], v[7]};
+        const f4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+        if (STREAM) {
+            __builtin_nontemporal_store(lo, (f4_a4*)p);
+            __builtin_nontemporal_store(hi, (f4_a4*)(p + 4));
+        } else {
+            *(f4_a4*)p = lo;
+            *(f4_a4*)(p + 4) = hi;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -594,7 +598,9 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
             } else if (has_with) {
                 group_slope8(g.act, v, w);
             }
-            store8<true>((TO*)g.y + pair * g.ldy + m, v, left);
+            TO* y = (TO*)g.y + pair * g.ldy + m;
+            if (g.stream) store8<true>(y, v, left);
+            else store8(y, v, left);
         };
         if (DIR == GR_FWD && (g.act == ACT_SIGMOID || g.act == ACT_TANH)) {  // (one copy of their code)
 #pragma unroll 1

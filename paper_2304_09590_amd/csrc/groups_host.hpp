@@ -177,6 +177,11 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     a.tiles = (const int2*)((const int32_t*)g->plan_dev + p.o_tiles[height]);
     a.n_tiles = (const int32_t*)g->plan_dev + p.o_count + height;
     auto blocks = [&](int band) { return (a.M + band - 1) / band * p.most[height]; };
+    // Large bf16 results are streamed: written past the caches they evict nothing of what the next workgroups read.
+    // Forward in us, cached -> streamed, and with the next layer, which reads the result: 2048 x 2048, 134 MB 314 ->
+    // 263, 641 -> 603; 67 MB 157 -> 154, 357 -> 370; 1024 x 1024, 134 MB 171 -> 148, 356 -> 328; 17 MB 38 -> 38,
+    // 75 -> 78.
+    a.stream = sizeof(TO) == 2 && p.P * a.M * (int64_t)sizeof(TO) >= (int64_t(96) << 20);
     if constexpr (sizeof(T) == 2) {
         if (kind == RING_HUGE) return launch_ring<DIR, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
         if (kind == RING) return launch_ring<DIR, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);

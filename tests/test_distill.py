@@ -323,3 +323,26 @@ def test_more_rows_than_one_launch_holds():
     s = 1 / (1 + math.exp(1.0))
     assert abs(float(dz[0, 0]) - (s - 1)) <= 4e-7 and abs(float(dz[-1, 0]) - s) <= 4e-7
     assert (dz[:-1] == dz[0]).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,n,v", [(F32, 4200, 8191), (BF16, 8400, 8190)])
+def test_a_gradient_larger_than_the_caches(dtype, n, v):
+    """Rows off 16 bytes with a ragged end; the entries' and the label's places are written after the rest of their row."""
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    z = (torch.randn(n, v, generator=gen, device="cuda") * 3).to(dtype)
+    idx = torch.randint(0, v, (n, 40), generator=gen, device="cuda", dtype=torch.int32)
+    t = torch.randn(n, 40, generator=gen, device="cuda").to(dtype)
+    y = torch.randint(0, v, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    g = torch.randn(n, generator=gen, device="cuda")
+    assert 2 * z.numel() * z.element_size() > 256 << 20
+    dz = torch.full_like(z, 7)
+    loss, stats = pnn.distill_loss(z, idx, t, y=y, temperature=2.0, alpha=0.25)
+    pnn.distill_grad(z, idx, t, stats, g, y=y, temperature=2.0, alpha=0.25, out=dz)
+    at = torch.cat([torch.arange(8), torch.arange(n // 2, n // 2 + 8), torch.arange(n - 8, n)]).cuda()
+    want, tol, dwant, dtol = reference(z[at], idx[at], t[at], y[at], 2.0, 0.25, g[at])
+    if dtype == BF16:
+        dtol = dtol + (dwant.abs() + dtol) * torch.finfo(BF16).eps / 2
+    assert ((loss[at].double().cpu() - want).abs() <= tol).all() and ((dz[at].double().cpu() - dwant).abs() <= dtol).all()
+    again = pnn.distill_grad(z, idx, t, stats, g, y=y, temperature=2.0, alpha=0.25, out=z)
+    assert again is z and torch.equal(z, dz)  # in place

@@ -459,3 +459,20 @@ def test_two_threads_on_two_streams():
     assert not failed
     for g, w in zip(got, want):
         assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+
+@gpu
+@pytest.mark.parametrize("outputs,pad", [(2056, 0), (2051, 1)])
+def test_results_larger_than_the_caches(outputs, pad):
+    """Ragged groups, dropped rows and rows off 16 bytes, both directions."""
+    n, networks, inputs = 25000, 5, 72
+    c = Case(n, 1, networks, inputs, outputs, BF16, pad=pad, seed=29)
+    assert n * outputs * 2 >= 96 << 20
+    flat = torch.full((n, outputs + 3), 7, dtype=BF16, device="cuda")
+    got = pnn.grouped_forward(c.groups, c.x, c.w, c.b, act=pnn.RELU, out=flat[:, :outputs])
+    want, size = c.forward(pnn.RELU, 1.0)
+    close(got, want, size, inputs, pnn.RELU)
+    assert (got[~c.kept] == 0).all() and (flat[:, outputs:] == 7).all()
+    back = Case(n, 1, networks, outputs, inputs, BF16, pad=pad, seed=31)
+    want, size = back.backward_input()
+    close(pnn.grouped_backward_input(back.groups, back.dy, back.w), want, size, inputs)
