@@ -362,7 +362,7 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     if (!sum) {
         a.a = act >= 0 ? a_dev : nullptr; a.lda = a_ld; a.act = act;
         a.y = dx_dev; a.ldy = dx_ld;
-            return run_group_pairs<GR_DX>(a, groups, layer->type, dx_type, s);
+        return run_group_pairs<GR_DX>(a, groups, layer->type, dx_type, s);
     }
     a.y = ws_dev; a.ldy = layer->inputs;
     TRY(run_group_pairs<GR_DX>(a, groups, layer->type, PNN_FP32, s));
