@@ -51,20 +51,25 @@ constexpr float DL_INF = __builtin_huge_valf();
 
 // Running maximum m and sums of exp2(z c - m c), at the scales c = ct and cs.  MODE 1: one sum; 2: two; 3: two
 // whose second scale is twice the first (T = 2), so that its terms are the first's squares.  m c is rounded once
-// and the same wherever it is used (Ref), so its rounding shifts all terms alike and cancels.
+// and the same wherever it is used (Ref), so its rounding shifts all terms alike and cancels, as long as the shift
+// is small: below 2^20 it is at most 2^-5.  From there on (`huge`) differences are taken before they are scaled,
+// and nothing is shifted: the shift grows with m c, and at 2^31 the exponentials would leave fp32's range.
 struct Sums { float m, a, b; };
+constexpr float DL_FAR = 1048576.0f;
 struct Ref {
     float t, s;
-    bool huge;  // m c leaves fp32's range: differences are taken before they are scaled
+    bool huge;
 };
 
 __device__ inline Ref dl_ref(float m, const DistillArgs& d) {
     const float r = m == -DL_INF ? 0.0f : m;  // (no value yet, or only ones of -inf: their terms are 0)
     Ref f = {r * d.ct, r * d.cs, false};
-    f.huge = !(__builtin_fabsf(f.t) < 1e38f && __builtin_fabsf(f.s) < 1e38f);
+    f.huge = !(__builtin_fabsf(f.t) < DL_FAR && __builtin_fabsf(f.s) < DL_FAR);
     if (f.huge) f.t = f.s = r;
     return f;
 }
+// what the terms' exponents at maximum m and scale c exceed (z - m) c by (exact: the rounding of m c)
+__device__ inline float dl_shift(float m, float c, float ref, bool huge) { return huge ? 0.0f : __builtin_fmaf(m, c, -ref); }
 // exponents (to base 2) of a logit
 __device__ inline float dl_t(float z, const Ref& f, const DistillArgs& d) {
     return f.huge ? (z - f.t) * d.ct : __builtin_fmaf(z, d.ct, -f.t);
@@ -78,8 +83,11 @@ template <int MODE>
 __device__ inline void dl_move(Sums& s, float m, const DistillArgs& d) {
     const Ref f = dl_ref(m, d), old = dl_ref(s.m, d);
     const bool none = s.m == -DL_INF;  // (the sums are 0, or NaN, and stay so)
-    const float by = f.huge || old.huge ? (s.m - m) * d.ct : old.t - f.t;
-    const float bs = f.huge || old.huge ? (s.m - m) * d.cs : old.s - f.s;
+    float by = old.t - f.t, bs = old.s - f.s;
+    if (f.huge || old.huge) {  // (a maximum on either side of the switch: the shifts do not cancel)
+        by = (s.m - m) * d.ct + (dl_shift(m, d.ct, f.t, f.huge) - dl_shift(s.m, d.ct, old.t, old.huge));
+        bs = (s.m - m) * d.cs + (dl_shift(m, d.cs, f.s, f.huge) - dl_shift(s.m, d.cs, old.s, old.huge));
+    }
     s.a *= none ? 0.0f : __builtin_amdgcn_exp2f(by);
     if (MODE != 1) s.b *= none ? 0.0f : __builtin_amdgcn_exp2f(bs);
     s.m = m;
