@@ -23,12 +23,14 @@ constexpr int GR_ALONE = 8192;      // pairs of one that is alone: one launch fo
 constexpr int GR_HEIGHTS = 4;       // pairs per tile: 16, and 64, 128 or 256 for the matrix-tile kernels
 
 // Layout of a plan (int32 words): off[K + 1] | pairs[P] | numbers of tiles | tiles of 16, 64, 128 and
-// 256 pairs | counts of the workgroups.  A tile is (network, first position); network K stands for the dropped
-// pairs.  The host knows only the most tiles there can be (extra workgroups end at once).
+// 256 pairs | counts of the workgroups | with several pairs a row, a byte for each pair: 1 unless it is dropped.  A tile
+// is (network, first position); network K stands for the dropped pairs.  The host knows only the most tiles there can
+// be (extra workgroups end at once).  What lies before the bytes depends on the number of pairs alone, so a plan also
+// serves the same pairs as rows of one pair each.
 struct GroupPlan {
     int64_t P;
     int K;
-    int64_t o_pairs, o_count, o_tiles[GR_HEIGHTS], o_hist, words;
+    int64_t o_pairs, o_count, o_tiles[GR_HEIGHTS], o_hist, o_kept, words;
     int64_t most[GR_HEIGHTS];
     int blocks;
     int64_t chunk;  // pairs per counting workgroup
@@ -54,7 +56,8 @@ __host__ inline GroupPlan group_plan(int64_t n, int per_row, int K) {
     g.chunk = (g.P + GR_MAX_BLOCKS - 1) / GR_MAX_BLOCKS;
     if (g.chunk < GR_CHUNK) g.chunk = g.P <= GR_ALONE ? GR_ALONE : GR_CHUNK;
     g.blocks = (int)((g.P + g.chunk - 1) / g.chunk);
-    g.words = g.o_hist + (g.blocks > 1 ? up((int64_t)g.blocks * (K + 1)) : 0);
+    g.o_kept = g.o_hist + (g.blocks > 1 ? up((int64_t)g.blocks * (K + 1)) : 0);
+    g.words = g.o_kept + (per_row > 1 ? up((g.P + 3) / 4) : 0);
     return g;
 }
 
@@ -62,6 +65,7 @@ struct GroupArgs {
     const int32_t* ids;
     int32_t *off, *pairs, *count, *hist;
     int2* tiles[GR_HEIGHTS];
+    uint8_t* kept;  // (nullable) of each pair: 1 unless it is dropped
     int64_t P, chunk;
     int K, blocks;
 };
@@ -205,7 +209,10 @@ __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
         for (int t = 0; t < N; ++t) base[t] = __shfl(base[t], __ffsll((unsigned long long)same[t]) - 1);
 #pragma unroll
         for (int t = 0; t < N; ++t)
-            if (key[t] >= 0) g.pairs[off[key[t]] + base[t] + __popcll(same[t] & below)] = (int)(b + 64 * t + lane);
+            if (key[t] >= 0) {
+                g.pairs[off[key[t]] + base[t] + __popcll(same[t] & below)] = (int)(b + 64 * t + lane);
+                if (g.kept) g.kept[b + 64 * t + lane] = key[t] < g.K;
+            }
     };
     if (kept) {
 #pragma unroll
@@ -1051,13 +1058,17 @@ __global__ __launch_bounds__(256) void group_join_kernel(GroupJoin g) {
     }
 }
 
-// dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r]), eight neighbouring values a thread.
+// dx[r] = (sum over j of the pairs' shares, ascending) (.) phi'(a[r]), eight neighbouring values a thread.  A row
+// without a pair that is kept gets 0 and not 0 times its slope, which a NaN in a[r] would show in.
 // Bound by the shares' bytes: two of each of 16,384 rows of 2048 in fp32 to bf16, 336 MB in 58 us.
 template <typename T, typename TO>
-__global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part, int64_t n, int per_row, int M, const T* a,
-                                                              int64_t lda, int act, TO* dx, int64_t ldx, int threads) {
+__global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part, int64_t n, int per_row, int M, const uint8_t* kept,
+                                                              const T* a, int64_t lda, int act, TO* dx, int64_t ldx, int threads) {
     const int rows = 256 / threads, tx = threadIdx.x % threads, ty = threadIdx.x / threads;
-    for (int64_t r = (int64_t)blockIdx.x * rows + ty; r < n; r += (int64_t)gridDim.x * rows)
+    for (int64_t r = (int64_t)blockIdx.x * rows + ty; r < n; r += (int64_t)gridDim.x * rows) {
+        int some = 0;
+        if (a)
+            for (int j = 0; j < per_row; ++j) some |= kept[r * per_row + j];
         for (int m = tx * 8; m < M; m += threads * 8) {
             const int left = M - m;
             const float* p = part + r * per_row * M + m;
@@ -1070,9 +1081,10 @@ __global__ __launch_bounds__(256) void group_sum_pairs_kernel(const float* part,
 #pragma unroll
                 for (int q = 0; q < 8; ++q) s[q] += v[q];
             }
-            if (a) group_slope8(act, s, x);
+            if (some) group_slope8(act, s, x);
             store8(dx + r * ldx + m, s, left);
         }
+    }
 }
 
 // Few pairs a network: 16 pairs and a band of the weights per workgroup, whose four waves split the

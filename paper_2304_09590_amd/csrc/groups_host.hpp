@@ -293,7 +293,8 @@ pnn_status pnn_group_rows(const int32_t* ids_dev, int64_t n, int32_t per_row, in
     OnDeviceOf dev(s);
     int32_t* w = (int32_t*)plan_dev;
     GroupArgs a = {ids_dev, w, w + p.o_pairs, w + p.o_count, w + p.o_hist,
-                   {(int2*)(w + p.o_tiles[0]), (int2*)(w + p.o_tiles[1]), (int2*)(w + p.o_tiles[2]), (int2*)(w + p.o_tiles[3])}, p.P, p.chunk, p.K, p.blocks};
+                   {(int2*)(w + p.o_tiles[0]), (int2*)(w + p.o_tiles[1]), (int2*)(w + p.o_tiles[2]), (int2*)(w + p.o_tiles[3])},
+                   per_row > 1 ? (uint8_t*)(w + p.o_kept) : nullptr, p.P, p.chunk, p.K, p.blocks};
     if (p.blocks > 1) {
         group_count_kernel<<<(unsigned)p.blocks, GR_THREADS, 0, s>>>(a);
         TRY(launched("counting the groups"));
@@ -369,9 +370,10 @@ pnn_status pnn_grouped_backward_input(const pnn_groups* groups, const pnn_group_
     const int threads = row_threads((layer->inputs + 7) / 8), each = 256 / threads;
     const unsigned blocks = (unsigned)std::min<int64_t>((groups->n + each - 1) / each, 8192);
     const float* part = (const float*)ws_dev;
+    const uint8_t* kept = (const uint8_t*)((const int32_t*)groups->plan_dev + group_plan(groups->n, groups->per_row, groups->networks).o_kept);
     const void* ad = act >= 0 ? a_dev : nullptr;
 #define PNN_SUM_PAIRS(T, TO) \
-    group_sum_pairs_kernel<T, TO><<<blocks, 256, 0, s>>>(part, groups->n, groups->per_row, layer->inputs, (const T*)ad, a_ld, act, (TO*)dx_dev, dx_ld, threads)
+    group_sum_pairs_kernel<T, TO><<<blocks, 256, 0, s>>>(part, groups->n, groups->per_row, layer->inputs, kept, (const T*)ad, a_ld, act, (TO*)dx_dev, dx_ld, threads)
     if (layer->type == PNN_FP32) { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(float, float); else PNN_SUM_PAIRS(float, bf16_t); }
     else { if (dx_type == PNN_FP32) PNN_SUM_PAIRS(bf16_t, float); else PNN_SUM_PAIRS(bf16_t, bf16_t); }
 #undef PNN_SUM_PAIRS
