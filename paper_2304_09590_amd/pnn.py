@@ -3,6 +3,10 @@
 Argument marshalling only: every step of training, merging and inference runs in the
 library's HIP kernels.  Device tensors come from PyTorch (memory and streams only).  There
 is no fallback: if the compiled library is missing, importing the binding raises.
+
+Every call that takes tensors takes `stream`: None for the current one; a torch.cuda.Stream, on which the
+tensors are then recorded, so that their memory is not given to others before the call's work has ended;
+or a raw handle, whose caller keeps the tensors until then.  New results belong to that stream.
 """
 from __future__ import annotations
 
@@ -170,11 +174,31 @@ def shard(n: int, k_total: int, k: int) -> Tuple[int, int]:
     return s.value, ln.value
 
 
-def _stream_handle(stream) -> Optional[int]:
-    if stream is None:
+_torch = None
+
+
+def _t():
+    global _torch
+    if _torch is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        _torch = torch
+    return _torch
+
+
+def _stream_handle(stream, *tensors) -> Optional[int]:
+    """The stream's handle; the tensors are recorded on a torch.cuda.Stream."""
+    if stream is None:
+        return _t().cuda.current_stream().cuda_stream
+    _record(stream, tensors)
     return getattr(stream, "cuda_stream", stream)
+
+
+def _record(stream, tensors) -> None:
+    """Memory of tensors that work on a torch.cuda.Stream uses is not given to others before that work has ended."""
+    if isinstance(stream, _t().cuda.Stream):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
 
 
 def _dev_ptr(t, dtype_name: str):
@@ -211,13 +235,13 @@ class PNN:
 
     def train_epoch(self, x, y, stream=None) -> None:
         self._check(self._lib.pnn_train_epoch(self.h, _dev_ptr(x, "torch.float32"), _dev_ptr(y, "torch.int32"),
-                                              x.shape[0], _stream_handle(stream)), "pnn_train_epoch")
+                                              x.shape[0], _stream_handle(stream, x, y)), "pnn_train_epoch")
 
     def train_epoch_order(self, x, y, order, stream=None) -> None:
         """One epoch over x[order], y[order] (order: int32 device tensor of N row indices)."""
         self._check(self._lib.pnn_train_epoch_order(self.h, _dev_ptr(x, "torch.float32"), _dev_ptr(y, "torch.int32"),
                                                     x.shape[0], _dev_ptr(order, "torch.int32"),
-                                                    _stream_handle(stream)), "pnn_train_epoch_order")
+                                                    _stream_handle(stream, x, y, order)), "pnn_train_epoch_order")
 
     def merge(self, broadcast: bool = False, stream=None) -> None:
         self._check(self._lib.pnn_merge(self.h, 1 if broadcast else 0, _stream_handle(stream)), "pnn_merge")
@@ -227,7 +251,7 @@ class PNN:
         self._check(self._lib.pnn_infer(self.h, which, _dev_ptr(x, "torch.float32"), x.shape[0],
                                         _dev_ptr(pred, "torch.int32"), _dev_ptr(out, "torch.float32"),
                                         ctypes.byref(c) if count else None, _dev_ptr(y, "torch.int32"),
-                                        _stream_handle(stream)), "pnn_infer")
+                                        _stream_handle(stream, x, pred, out, y)), "pnn_infer")
         return c.value if count else None
 
     def merge_weighted(self, weights, broadcast: bool = False, stream=None) -> None:
@@ -242,7 +266,7 @@ class PNN:
         c = ctypes.c_int64(-1)
         cost = ctypes.c_double(float("nan"))
         self._check(self._lib.pnn_eval(self.h, which, _dev_ptr(x, "torch.float32"), _dev_ptr(y, "torch.int32"),
-                                       x.shape[0], ctypes.byref(c), ctypes.byref(cost), _stream_handle(stream)),
+                                       x.shape[0], ctypes.byref(c), ctypes.byref(cost), _stream_handle(stream, x, y)),
                     "pnn_eval")
         return c.value, cost.value
 
@@ -253,7 +277,7 @@ class PNN:
         cost = ctypes.c_double(float("nan"))
         self._check(self._lib.pnn_eval_noalloc(self.h, which, _dev_ptr(x, "torch.float32"),
                                                _dev_ptr(y, "torch.int32"), x.shape[0], ctypes.byref(c),
-                                               ctypes.byref(cost), _stream_handle(stream)), "pnn_eval_noalloc")
+                                               ctypes.byref(cost), _stream_handle(stream, x, y)), "pnn_eval_noalloc")
         return c.value, cost.value
 
     def get_params(self, which: int = -1) -> np.ndarray:
@@ -275,7 +299,8 @@ class PNN:
                      (out, (rows, self.cfg.sizes[self.cfg.n_layers])))
         self._check(self._lib.pnn_infer_routed(self.h, _dev_ptr(x, "torch.float32"), rows, _dev_ptr(ids, "torch.int32"), per_row,
                                                _dev_ptr(weights, "torch.float32"), _dev_ptr(pred, "torch.int32"),
-                                               _dev_ptr(out, "torch.float32"), _stream_handle(stream)), "pnn_infer_routed")
+                                               _dev_ptr(out, "torch.float32"), _stream_handle(stream, x, ids, weights, pred, out)),
+                    "pnn_infer_routed")
 
     def train_routed(self, x, ids, idx=None, t=None, y=None, temperature: float = 1.0, alpha: float = 0.0, loss=None,
                      stream=None) -> None:
@@ -286,7 +311,7 @@ class PNN:
         self._check(self._lib.pnn_train_routed(self.h, _dev_ptr(x, "torch.float32"), rows, _dev_ptr(ids, "torch.int32"), per_row,
                                                _dev_ptr(idx, "torch.int32"), _dev_ptr(t, "torch.float32"), top,
                                                _dev_ptr(y, "torch.int32"), temperature, alpha, _dev_ptr(loss, "torch.float32"),
-                                               _stream_handle(stream)), "pnn_train_routed")
+                                               _stream_handle(stream, x, ids, idx, t, y, loss)), "pnn_train_routed")
 
     @staticmethod
     def _shapes(*given) -> None:
@@ -324,26 +349,15 @@ class PNN:
 
 # ---- calls without a handle: rows that name their network, distillation ----------------------
 
-_torch = None
-
-
-def _t():
-    global _torch
-    if _torch is None:
-        import torch
-        _torch = torch
-    return _torch
-
-
 def _call(what: str, *args) -> None:
     st = getattr(lib(), what)(*args)
     if st != PNN_OK:
         raise PnnError(st, f"{what}: {lib().pnn_last_error(None).decode()}")
 
 
-def _on(stream, body, first, *others):
+def _on(stream, body, first, *others, groups=None):
     """body(stream handle) with the tensors' device current and, for allocations, the stream; the tensors have to
-    be on one GPU."""
+    be on one GPU.  The tensors, and a plan that another stream's memory holds, are recorded on the stream."""
     torch = _t()
     dev = first.get_device()
     if dev < 0:
@@ -351,15 +365,24 @@ def _on(stream, body, first, *others):
     for t in others:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors on {first.device} and on {t.device}")
-    if stream is None and torch._C._cuda_getDevice() == dev:
-        return body(torch._C._cuda_getCurrentRawStream(dev))
+    if groups is not None and groups.plan.get_device() != dev:
+        raise ValueError(f"tensors on {first.device} and a plan on {groups.plan.device}")
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(dev)
+        if groups is not None and groups.stream != s:
+            _record(torch.cuda.current_stream(dev), (groups.plan,))
+        if torch._C._cuda_getDevice() == dev:
+            return body(s)
     with torch.cuda.device(dev):
         if stream is None:
-            return body(torch._C._cuda_getCurrentRawStream(dev))
-        if not isinstance(stream, torch.cuda.Stream):
+            return body(s)
+        raw = not isinstance(stream, torch.cuda.Stream)
+        if raw:
             stream = torch.cuda.ExternalStream(stream, device=first.device)
         if stream.device != first.device:
             raise ValueError(f"a stream of {stream.device} for tensors on {first.device}")
+        if not raw:
+            _record(stream, (first, *others, groups.plan if groups is not None else None))
         with torch.cuda.stream(stream):
             return body(stream.cuda_stream)
 
@@ -418,8 +441,9 @@ def _group_workspace(n: int, per_row: int, networks: int, inputs: int, outputs: 
 class RowGroups:
     """Rows grouped by the networks that they name (pnn_group_rows)."""
 
-    def __init__(self, plan, n: int, per_row: int, networks: int):
+    def __init__(self, plan, n: int, per_row: int, networks: int, stream: Optional[int] = None):
         self.plan, self.n, self.per_row, self.networks = plan, n, per_row, networks
+        self.stream = stream  # the handle of the stream that the plan's memory belongs to, if known
         self.struct = PnnGroups(plan.data_ptr(), n, per_row, networks)
 
     @property
@@ -446,9 +470,10 @@ def group_rows(ids, networks: int, stream=None) -> RowGroups:
         size = _group_bytes(n, per_row, networks)
         plan = _empty(ids, size // 4)
         _call("pnn_group_rows", ids.data_ptr(), n, per_row, networks, plan.data_ptr(), size, s)
-        return plan
+        return plan, s
 
-    return RowGroups(_on(stream, body, ids), n, per_row, networks)
+    plan, s = _on(stream, body, ids)
+    return RowGroups(plan, n, per_row, networks, s)
 
 
 def _weights(groups: RowGroups, w, b=None) -> PnnGroupLayer:
@@ -476,7 +501,7 @@ def grouped_forward(groups: RowGroups, x, w, b=None, act: Optional[int] = None, 
               py, ldy, _type_of(y), s)
         return y
 
-    return _on(stream, body, x, groups.plan, w, b, out)
+    return _on(stream, body, x, w, b, out, groups=groups)
 
 
 def _workspace(groups: RowGroups, layer: PnnGroupLayer, like, which: int):
@@ -505,7 +530,7 @@ def grouped_backward_input(groups: RowGroups, dy, w, a=None, act: Optional[int] 
               -1 if act is None else act, po, ldo, _type_of(dx), pw, size, s)
         return dx
 
-    return _on(stream, body, dy, groups.plan, w, a, out)
+    return _on(stream, body, dy, w, a, out, groups=groups)
 
 
 def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: bool = True, stream=None):
@@ -529,7 +554,7 @@ def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: b
               w.stride(0), ldw, pb, netb, ps, size, s)
         return w, b
 
-    return _on(stream, body, x, groups.plan, dy, dw, db)
+    return _on(stream, body, x, dy, dw, db, groups=groups)
 
 
 @functools.lru_cache(maxsize=1024)
