@@ -255,10 +255,13 @@ void pnn_destroy(pnn_net* net);
  * hip_stream and on its device (the null stream: on the current device).  A row's values are
  * contiguous; `_ld` is the distance between rows and `_net` between networks, in values.  Rows need
  * be aligned to their type only (16-byte alignment and widths that are multiples of 8 are faster).
- * `type` is PNN_FP32 (fp32) or PNN_BF16_MIXED (bfloat16).  Products are summed in fp32; fp32
- * operands enter the matrix units in three bf16 parts (six products, as exact as fp32 products),
- * so they have to be finite and below 3.38e38: an infinite operand gives NaN in what it reaches,
- * as a NaN does.  Results must not overlap operands, and a plan is used with the sizes it was made
+ * `type` is PNN_FP32 (fp32) or PNN_BF16_MIXED (bfloat16).  Products are summed in fp32.  fp32
+ * operands enter the matrix units in three bf16 parts (six products, as exact as fp32 products), or
+ * as they are in a forward product or an input gradient of at most 16 pairs a network in the mean.
+ * So they have to be finite and below 3.38e38: an infinite operand makes what it reaches NaN where
+ * it is taken in parts, and what fp32 arithmetic gives (infinite or NaN) where it is not; which of
+ * the two depends on the number of pairs.  Parts end at 2^-133, so that operands below 2^-110 lose
+ * their last bits.  Results must not overlap operands, and a plan is used with the sizes it was made
  * with.  What does not fit a launch (a result of more than 2^32 values of narrow rows, say) is refused
  * with PNN_ESHAPE. */
 
@@ -329,7 +332,8 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
  * -inf has no weight.  A label outside [0, classes) is none.  A row without entries and without a
  * label, and one whose logits are all -inf, has loss 0 and gradient 0; its logits may hold
  * anything in the first case.  z, t and dz are of `type`; sums and statistics are fp32, and the
- * maximum is subtracted first, so logits near the type's limits do not overflow.  The order of the
+ * maximum is subtracted first, so logits near the type's limits do not overflow (a class further below
+ * the maximum than fp32's range counts as one of -inf).  The order of the
  * sums depends on the sizes alone.  No handle, as for the grouped products above. */
 typedef struct {
     const void* z_dev;      /* [n][classes] */
