@@ -568,6 +568,8 @@ def _distill(z, idx, t, y, temperature, alpha) -> PnnDistill:
     torch = _t()
     if z.dim() != 2:
         raise ValueError(f"z has shape {tuple(z.shape)}, expected a matrix")
+    if (idx is None) != (t is None):
+        raise ValueError("idx and t go together")
     n, top = z.shape[0], (idx.shape[-1] if idx is not None else 0)
     pz, ldz = _rows(z, "z", z.shape, z.dtype)
     return PnnDistill(pz, ldz, _type_of(z), z.shape[1], n, None if idx is None else _values(idx, "idx", (n, top), torch.int32),
