@@ -394,8 +394,8 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
     TRY(check_rows("dw_dev", dw_dev, dw_ld, layer->inputs, PNN_FP32));
     if (((uintptr_t)db_dev & 3) != 0) return fail(nullptr, PNN_EINVAL, "db_dev is not aligned to its type");
     // (one network's rows after another's, or all networks' share of a row before the next row)
-    const int64_t M = layer->inputs, after = (layer->outputs - 1) * dw_ld + M;
-    if (groups->networks > 1 && dw_net < after && (dw_net < M || dw_ld - M < (groups->networks - 1) * dw_net))
+    const __int128 M = layer->inputs, after = (layer->outputs - 1) * (__int128)dw_ld + M;  // (strides of any size)
+    if (groups->networks > 1 && dw_net < after && (dw_net < M || dw_ld - M < (groups->networks - 1) * (__int128)dw_net))
         return fail(nullptr, PNN_EINVAL, "the networks of dw_dev overlap");
     if (db_dev && db_net < layer->outputs && groups->networks > 1) return fail(nullptr, PNN_EINVAL, "the networks of db_dev overlap");
     TRY(check_ws(ws_dev, ws_bytes, group_weights_ws(groups, layer->inputs, layer->outputs)));

@@ -17,6 +17,12 @@ def test_networks_that_overlap_are_refused(dw_net, dw_ld, overlap):
     assert ("overlap" in pnn.lib().pnn_last_error(None).decode()) == overlap
 
 
+@pytest.mark.parametrize("dw_net,dw_ld,overlap", [(40, 1 << 62, False), (1 << 61, 1 << 62, True), ((1 << 63) - 1, 1 << 62, True),
+                                                  (1 << 62, 1 << 60, True), ((1 << 62) + 8, 1 << 60, False)])
+def test_strides_near_the_end_of_64_bits(dw_net, dw_ld, overlap):
+    test_networks_that_overlap_are_refused(dw_net, dw_ld, overlap)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,networks,inputs,outputs,pad", [(300, 5, 64, 128, 0), (5000, 2, 24, 40, 0), (3000, 3, 33, 17, 1), (4000, 3, 520, 264, 0)])
