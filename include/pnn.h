@@ -333,8 +333,10 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
  * label, and one whose logits are all -inf, has loss 0 and gradient 0; its logits may hold
  * anything in the first case.  z, t and dz are of `type`; sums and statistics are fp32, and the
  * maximum is subtracted first, so logits near the type's limits do not overflow (a class further below
- * the maximum than fp32's range counts as one of -inf).  The order of the
- * sums depends on the sizes alone.  No handle, as for the grouped products above. */
+ * the maximum than fp32's range counts as one of -inf).  Logarithms and quotients are rounded before T
+ * scales them, so a loss is off by about 2^-22 (1 - alpha) T^2 and dz_v by 2^-22 g (1 - alpha) T q_v, which
+ * at temperatures of thousands is as much as is left of them.  The order of the sums depends on the sizes
+ * alone.  No handle, as for the grouped products above. */
 typedef struct {
     const void* z_dev;      /* [n][classes] */
     int64_t z_ld;

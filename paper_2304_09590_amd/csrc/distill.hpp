@@ -353,7 +353,9 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs d) {
 }
 
 // Gradient, W waves a row or one part of a row per workgroup.  The entries' classes (and the label)
-// are written again after the stream has passed, from logits read before it: so dz may be z.
+// are written again after the stream has passed, from logits read before it: so dz may be z.  Each entry is
+// compared with all others of its row for repeated classes, which is quadratic in the entries: 4,096 rows of
+// 32,000 classes in bf16 with 64, 128, 256, 512 and 1,024 entries 113, 122, 151, 267 and 703 us.
 template <typename T, int MODE, int W>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs d) {
     constexpr int TOP = W == 4 ? DL_MAX_TOP : DL_WAVE_TOP;

@@ -125,8 +125,9 @@ __device__ inline void wave_scan(int* out, int n, int lane, F f) {
 // Stable placement.  Every workgroup counts its chunk by wave (a wave owns a contiguous part), adds what the
 // chunks and waves before it hold, and places its pairs.  The lanes of a wave that hold the same key find each
 // other in LDS: each sets its bit in the key's word, and the bits below its own are its order.  (One ballot
-// per key bit instead is 130 instructions a step: 120,000 pairs, 256 networks 12.9 us, this way 11.4.)  Integer
-// sums only: the same bits every run.  With one workgroup its own counts are all there is
+// per key bit instead is 130 instructions a step: 120,000 pairs, 256 networks 12.9 us, this way 11.4.)  Bound by
+// latencies one after another: of 12.6 us for both launches over the same pairs the other workgroups' counts take
+// 3.5, the placing 3.6 and the tile lists 0.7.  Integer sums only: the same bits every run.  With one workgroup its own counts are all there is
 // (no earlier launch).  All workgroups share the tiles.
 template <int KEYS>
 __global__ __launch_bounds__(GR_THREADS) void group_place_kernel(GroupArgs g) {
@@ -748,9 +749,11 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
 
 // ------------------------------------------------------------------------------------
 // bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, WM x WN waves, a ring of stages of
-// 32 k in LDS that global memory fills directly.  The matrix units bound a long contraction (65,536 pairs 4096 ->
-// 4096, 16 networks: 2,025 us, 1,086 TFLOP/s of the 1,327 that a large library product reaches on the card); at 1024
-// the results' stores, which a round of workgroups makes at one time, add a quarter (without them 551 us of 671).
+// 32 k in LDS that global memory fills directly.  A long contraction (65,536 pairs 4096 -> 4096, 16 networks) takes
+// 2,025 to 2,060 us, 1,067 to 1,086 TFLOP/s of the 1,327 that a large library product reaches on the card: the matrix
+// cores are busy in 0.54 of the cycles, at a clock that the load holds near 1.9 GHz (0.60 at 1.4 GHz in the first passes
+// after an idle spell).  At a contraction of 1024 they are busy in 0.48: the results' stores, which a round of workgroups
+// makes at one time, add a quarter (without them 551 us of 671 for 32,768 rows to two each of 32 networks).
 
 static __device__ __align__(64) uint32_t group_zeros[16];  // what lies outside an operand
 

@@ -119,7 +119,16 @@ constexpr int64_t GROUP_FILL = 512;  // workgroups that fill the device: two on 
 
 // Parts that a group's pairs are cut into for a weight gradient, and the ring's tile: 256 x 256 where groups
 // are long and cutting them into parts of 512 pairs fills the device; else 256 x 128; else 128 x 64, groups cut
-// into parts of 256.
+// into parts of 256.  In us for tiles of 256 x 256, 256 x 128, 128 x 64 on whole groups: 2048 x 2048, 16 networks, 32,768
+// pairs 298, 313, 508, 8,192 pairs 116, 111, 165; 784 x 512, 64 networks, 4,096 pairs 36, 33, 37; 512 x 512, 8
+// networks, 2,000 pairs 16, 13, 9.  784 x 256, 60,000 pairs: one network whole 1,377, 1,146, 634, in 64 parts 88, 102,
+// 116; four networks whole 358, 295, 164, in 29, 29 and 58 parts 84, 92, 158.  Parts are written and read again,
+// which costs more than it gains where whole groups nearly fill the device: 1024 x 1024, 16 networks, 16,384 pairs in
+// the rule's two parts 93, whole 47; 784 x 512, 16 networks, 60,000 pairs in its four parts 114, whole 101; 512 x 512,
+// 8 networks, 8,000 pairs in its two (128 x 64) 25, whole 17.  Through registers (fp32), tiles of 64 and of 128 on whole
+// groups: 501 x 203, 24 networks, 1,501 pairs 10, 15; 784 x 1024, 256 networks, 32,768 pairs 601, 540.
+// The parts follow the mean: a group that holds most pairs is cut no finer than an even one would be.  784 x
+// 1024, 256 networks, 32,768 pairs: even 336, half of them in one network 512, all in one 745 (fp32 530, 1,408, 2,619).
 void group_weights_plan(int64_t P, int32_t K, int32_t inputs, int32_t outputs, int* kind, int* splits) {
     auto tiles = [&](int bm, int bn) { return (int64_t)K * ((inputs + bm - 1) / bm) * ((outputs + bn - 1) / bn); };
     const int64_t mean = P / K;
@@ -156,9 +165,19 @@ pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
 }
 
 // Which kernel multiplies pairs: tiles of 16 re-read the weights for each of them, those of 64 to 256 multiply
-// what is not there.  Forward in us, tiles of 16 against 64 and more, at 1, 16, 24 and 64 pairs a network:
-// 64 networks 784 -> 512 in fp32 21, 25, 37, 66 against 29, 27, 31, 33; in bf16 14, 18, 24, 42 against 13, 13, 15,
-// 15; 32 networks 2048 -> 4096 in bf16 102, 138, 198, 378 against 111, 113, 114, 132.
+// what is not there.  Kernels in us, tiles of 16 against the larger ones that the rule would take.  fp32 at 1, 8, 16, 20
+// pairs a network: 64 networks 784 -> 512 15, 23, 27, 34 against 26, 28, 29, 30, its input gradient 18, 29, 36, 44
+// against 24, 27, 29, 29; 32 networks 1001 -> 999 19, 30, 35, 41 against 34, 37, 37, 37, its input gradient 25, 33, 43, 54
+// against 37, 37, 40, 40.  bf16 at 1, 2, 4, 8: 784 -> 512 8, 11, 13, 14 against 9, 10, 11, 12, its input gradient 13,
+// 13, 14, 15 against 10, 11, 12, 12; 32 networks 2048 -> 4096 64, 95, 106, 121 against 74, 105, 118, 108, its input
+// gradient 68, 88, 93, 97 against 69, 93, 98, 101; 1001 -> 999 17, 22, 23, 26 against 19, 19, 19, 19, its input gradient 40,
+// 41, 42, 42 against 31, 31, 31, 28.  One limit a type serves both directions: it costs a bf16 input gradient of
+// narrow or unaligned layers a quarter at one and two pairs, and a wide forward product a tenth at three and four.
+// Tiles of 64 against 128: fp32 8 networks 512 -> 512 8,000 pairs 34, 45, 16,000 pairs 61, 61; 256 networks 784 -> 1024
+// 32,768 pairs 453, 397; bf16 of one value more each way 27, 26; 46, 38; 317, 253.  The ring's 128 x 64, 256 x 128, 256 x
+// 256: 8 networks 1024 -> 1024 8,000 pairs 35, 35, 31, 16,000 pairs 59, 55, 60; 64 networks 784 -> 512 32,000 pairs 62, 51,
+// 57; 16 networks 2048 -> 2048 8,192 pairs 124, 96, 106, 32,768 pairs 447, 293, 277; 4 networks 2048 -> 2048 8,000 pairs
+// 112, 73, 61.  (256 x 256 is taken too early for short contractions: 8 networks 512 -> 512, 32,000 pairs 34, 27, 40.)
 int group_pairs_kind(const pnn_groups* g, int M, bool bf16, bool ring) {
     const int64_t P = g->n * g->per_row, mean = P / g->networks;
     if (mean <= (bf16 ? 2 : 16)) return FEW;
