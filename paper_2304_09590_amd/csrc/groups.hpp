@@ -751,9 +751,10 @@ __global__ __launch_bounds__(256, 2) void group_tile_kernel(GroupGemm g) {
 // bf16 products whose rows start at multiples of 16 bytes: tiles of BM x BN, WM x WN waves, a ring of stages of
 // 32 k in LDS that global memory fills directly.  A long contraction (65,536 pairs 4096 -> 4096, 16 networks) takes
 // 2,025 to 2,060 us, 1,067 to 1,086 TFLOP/s of the 1,327 that a large library product reaches on the card: the matrix
-// cores are busy in 0.54 of the cycles, at a clock that the load holds near 1.9 GHz (0.60 at 1.4 GHz in the first passes
-// after an idle spell).  At a contraction of 1024 they are busy in 0.48: the results' stores, which a round of workgroups
-// makes at one time, add a quarter (without them 551 us of 671 for 32,768 rows to two each of 32 networks).
+// cores are busy in 0.50 to 0.54 of the cycles, at a clock of 2.1 to 1.9 GHz under this load (0.60 at 1.4 GHz in the
+// first passes after an idle spell).  At a contraction of 1024 they are busy in 0.48 (16 even networks, one a row: 524 to
+// 560 us) and in 0.35 (32,768 rows to two each of 32 networks: 660): the results' stores, which a round of workgroups
+// makes at one time, add a quarter (without them 551 us of 671).
 
 static __device__ __align__(64) uint32_t group_zeros[16];  // what lies outside an operand
 
