@@ -322,6 +322,66 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
                                         void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rows that choose their networks.  A router scores every network for a row; the row goes through
+ * the ones that it likes best, and their results are weighed into one.  No handle and nothing kept, as
+ * for the grouped products above, whose ids these are.
+ *
+ * Row r has scores s [networks] of `type` and, with p = softmax(s), goes through the networks of its
+ * per_row largest scores: ids, in descending order (lowest index on ties), and gates p at these, or
+ * with `normalize` p divided by its sum over them.  A score of -inf is never chosen: a row with fewer
+ * others has ids of -1 and gates of 0 at its end, and one of -inf alone takes no part.  A row with a
+ * NaN or an infinite score has ids of -1 and gates, gradients and a balance loss of NaN.
+ * With counts_e the pairs of network e, C their sum and n' the rows that take part, the balance loss is
+ *   loss = networks sum_e (counts_e / C) (sum_r p_re) / n'
+ * (1 where rows are spread evenly, 0 without rows).  Statistics and sums are fp32 (counts int32), and their order
+ * depends on the sizes alone. */
+typedef struct {
+    const void* s_dev; /* [n][networks] */
+    int64_t s_ld;
+    int32_t type;
+    int32_t networks;  /* 1..1024 */
+    int64_t n;         /* < 2^31, n per_row <= 2^30 */
+    int32_t per_row;   /* 1..64, <= networks */
+    int32_t normalize;
+} pnn_router;
+
+/* Workspace of a pnn_route that counts. */
+pnn_status pnn_route_bytes(int64_t n, int32_t networks, int64_t* bytes);
+
+/* ids_dev int32 [n][per_row], gates_dev fp32 [n][per_row]; counts_dev int32 [networks + 1] (the pairs of
+ * each network, then n') and loss_dev fp32 [1], or neither (and then no workspace). */
+pnn_status pnn_route(const pnn_router* args, int32_t* ids_dev, float* gates_dev, int32_t* counts_dev, float* loss_dev,
+                     void* ws_dev, int64_t ws_bytes, void* hip_stream);
+
+/* ds_dev [n][networks] of `type`: the gradient of the scores from dgates_dev fp32 [n][per_row] (nullable)
+ * at the chosen ids (what stands at an id outside the networks is not read) and from dloss_dev fp32 [1]
+ * (nullable), the balance loss's (counts_dev; the counts themselves have no gradient).  ds_dev may be
+ * s_dev (with the same distance between rows). */
+pnn_status pnn_route_grad(const pnn_router* args, const int32_t* ids_dev, const int32_t* counts_dev, const float* dgates_dev,
+                          const float* dloss_dev, void* ds_dev, int64_t ds_ld, void* hip_stream);
+
+/* Results of pairs, weighed into rows: out[r] = sum_j w[r per_row + j] y[r per_row + j], j ascending, over
+ * the pairs whose id lies in [0, networks); 0 without one.  Sums are fp32. */
+typedef struct {
+    const void* y_dev; /* [n per_row][width] of `type` */
+    int64_t y_ld;
+    int32_t type;
+    int32_t width;     /* 1..2^20 */
+    int64_t n;
+    int32_t per_row, networks;
+    const int32_t* ids_dev; /* [n][per_row] */
+    const float* w_dev;     /* [n][per_row] */
+} pnn_combine;
+
+/* out_dev [n][width] of out_type. */
+pnn_status pnn_combine_rows(const pnn_combine* args, void* out_dev, int64_t out_ld, int32_t out_type, void* hip_stream);
+
+/* From g_dev [n][width] of g_type, the gradient of out: dy[p] = w[p] g[r] (of `type`) and dw[p] =
+ * sum g[r] y[p] (fp32), both 0 for a dropped pair.  dy_dev may be y_dev (with the same distance between rows). */
+pnn_status pnn_combine_grad(const pnn_combine* args, const void* g_dev, int64_t g_ld, int32_t g_type, void* dy_dev, int64_t dy_ld,
+                            float* dw_dev, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Distillation: a network learns another's answers (a way to combine CNs beside averaging them).
  * Row r has `classes` logits z, a teacher's `top` entries (class idx, logit t) and a label y.
  *   p = softmax(t / T) over the row's entries, q = softmax(z / T), s = softmax(z):

@@ -58,6 +58,17 @@ class PnnDistill(ctypes.Structure):
                 ("y", ctypes.c_void_p), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
+class PnnRouter(ctypes.Structure):
+    _fields_ = [("s", ctypes.c_void_p), ("s_ld", ctypes.c_int64), ("type", ctypes.c_int32), ("networks", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("per_row", ctypes.c_int32), ("normalize", ctypes.c_int32)]
+
+
+class PnnCombine(ctypes.Structure):
+    _fields_ = [("y", ctypes.c_void_p), ("y_ld", ctypes.c_int64), ("type", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("n", ctypes.c_int64), ("per_row", ctypes.c_int32), ("networks", ctypes.c_int32), ("ids", ctypes.c_void_p),
+                ("w", ctypes.c_void_p)]
+
+
 class PnnError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -123,6 +134,14 @@ def lib() -> ctypes.CDLL:
         L.pnn_grouped_backward_weights.argtypes = [groups, layer, vp, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
         for name in ("pnn_group_bytes", "pnn_group_rows", "pnn_grouped_forward", "pnn_grouped_workspace",
                      "pnn_grouped_backward_input", "pnn_grouped_backward_weights"):
+            getattr(L, name).restype = i32
+        router, combine = P(PnnRouter), P(PnnCombine)
+        L.pnn_route_bytes.argtypes = [i64, i32, P(i64)]
+        L.pnn_route.argtypes = [router, vp, vp, vp, vp, vp, i64, vp]
+        L.pnn_route_grad.argtypes = [router, vp, vp, vp, vp, vp, i64, vp]
+        L.pnn_combine_rows.argtypes = [combine, vp, i64, i32, vp]
+        L.pnn_combine_grad.argtypes = [combine, vp, i64, i32, vp, i64, vp, vp]
+        for name in ("pnn_route_bytes", "pnn_route", "pnn_route_grad", "pnn_combine_rows", "pnn_combine_grad"):
             getattr(L, name).restype = i32
         distill = P(PnnDistill)
         L.pnn_distill_bytes.argtypes = [i64, i32, P(i64)]
@@ -555,6 +574,103 @@ def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: b
         return w, b
 
     return _on(stream, body, x, dy, dw, db, groups=groups)
+
+
+@functools.lru_cache(maxsize=1024)
+def _route_bytes(n: int, networks: int) -> int:
+    size = ctypes.c_int64()
+    _call("pnn_route_bytes", n, networks, ctypes.byref(size))
+    return size.value
+
+
+def _router(s, per_row: int, normalize: bool) -> PnnRouter:
+    if s.dim() != 2:
+        raise ValueError(f"s has shape {tuple(s.shape)}, expected a matrix")
+    ps, lds = _rows(s, "s", s.shape, s.dtype)
+    return PnnRouter(ps, lds, _type_of(s), s.shape[1], s.shape[0], per_row, 1 if normalize else 0)
+
+
+def route(s, per_row: int, normalize: bool = False, balance: bool = True, stream=None):
+    """(ids int32 [n, per_row], gates fp32 [n, per_row], counts int32 [networks + 1], loss fp32 [1]) of scores s
+    [n, networks]: the networks of each row's largest scores, their softmax (normalize: among them), the pairs of each
+    network with the rows that take part, the balance loss; balance=False leaves the last two out (None)."""
+    torch = _t()
+    a = _router(s, per_row, normalize)
+
+    def body(h):
+        ids, gates = _empty(s, (a.n, per_row), torch.int32), _empty(s, (a.n, per_row), torch.float32)
+        if not balance:
+            _call("pnn_route", ctypes.byref(a), ids.data_ptr(), gates.data_ptr(), None, None, None, 0, h)
+            return ids, gates, None, None
+        size = _route_bytes(a.n, a.networks)
+        ws, counts = _empty(s, size // 4, torch.float32), _empty(s, a.networks + 1, torch.int32)
+        loss = _empty(s, 1, torch.float32)
+        _call("pnn_route", ctypes.byref(a), ids.data_ptr(), gates.data_ptr(), counts.data_ptr(), loss.data_ptr(), ws.data_ptr(),
+              size, h)
+        return ids, gates, counts, loss
+
+    return _on(stream, body, s)
+
+
+def route_grad(s, ids, counts=None, dgates=None, dloss=None, normalize: bool = False, out=None, stream=None):
+    """The gradient of the scores from those of route's gates (dgates fp32 [n, per_row]) and of its balance loss (dloss
+    fp32 [1], with the counts); either may be None.  out may be s."""
+    torch = _t()
+    if ids.dim() != 2:
+        raise ValueError(f"ids has shape {tuple(ids.shape)}, expected [n, per_row]")
+    a = _router(s, ids.shape[1], normalize)
+
+    def body(h):
+        ds = out if out is not None else _empty(s, s.shape)
+        pi = _values(ids, "ids", (a.n, a.per_row), torch.int32)
+        pc = _values(counts, "counts", (a.networks + 1,), torch.int32) if counts is not None else None
+        pg = _values(dgates, "dgates", ids.shape, torch.float32) if dgates is not None else None
+        pl = _values(dloss, "dloss", (1,), torch.float32) if dloss is not None else None
+        po, ldo = _rows(ds, "out", s.shape, s.dtype)
+        _call("pnn_route_grad", ctypes.byref(a), pi, pc, pg, pl, po, ldo, h)
+        return ds
+
+    return _on(stream, body, s, ids, counts, dgates, dloss, out)
+
+
+def _combine(y, ids, gates, networks: int) -> PnnCombine:
+    torch = _t()
+    if ids.dim() != 2 or y.dim() != 2:
+        raise ValueError(f"ids and y have shapes {tuple(ids.shape)} and {tuple(y.shape)}, expected [n, per_row] and [n * per_row, width]")
+    n, per_row = ids.shape
+    py, ldy = _rows(y, "y", (n * per_row, y.shape[1]), y.dtype)
+    return PnnCombine(py, ldy, _type_of(y), y.shape[1], n, per_row, networks, _values(ids, "ids", (n, per_row), torch.int32),
+                      _values(gates, "gates", (n, per_row), torch.float32))
+
+
+def combine_rows(y, ids, gates, networks: int, out=None, out_dtype=None, stream=None):
+    """out[r] = the sum of gates[r, j] * y[r * per_row + j] over the pairs whose id lies in [0, networks)."""
+    a = _combine(y, ids, gates, networks)
+    shape = (a.n, a.width)
+
+    def body(h):
+        o = out if out is not None else _empty(y, shape, out_dtype)
+        po, ldo = _rows(o, "out", shape, out_dtype or o.dtype)
+        _call("pnn_combine_rows", ctypes.byref(a), po, ldo, _type_of(o), h)
+        return o
+
+    return _on(stream, body, y, ids, gates, out)
+
+
+def combine_grad(dout, y, ids, gates, networks: int, dy=None, stream=None):
+    """(dy of y's type, dgates fp32) from dout [n, width], the gradient of combine_rows's result.  dy may be y."""
+    torch = _t()
+    a = _combine(y, ids, gates, networks)
+
+    def body(h):
+        d = dy if dy is not None else _empty(y, y.shape)
+        dgates = _empty(y, (a.n, a.per_row), torch.float32)
+        pg, ldg = _rows(dout, "dout", (a.n, a.width), dout.dtype)
+        pd, ldd = _rows(d, "dy", y.shape, y.dtype)
+        _call("pnn_combine_grad", ctypes.byref(a), pg, ldg, _type_of(dout), pd, ldd, dgates.data_ptr(), h)
+        return d, dgates
+
+    return _on(stream, body, y, dout, ids, gates, dy)
 
 
 @functools.lru_cache(maxsize=1024)

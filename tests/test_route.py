@@ -1,0 +1,325 @@
+"""Rows that choose their networks (ids, gates, counts, balance loss) and the gradient of the scores, against the
+formulas in 64 bits, their derivative and differences."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2304_09590_amd import pnn
+
+gpu = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = 2.0 ** -24  # half a step of fp32
+FAKE = 1 << 20
+
+
+# ---- refusals, on the host -----------------------------------------------------------------------
+
+def args(**over):
+    a = dict(s=FAKE, s_ld=8, type=pnn.FP32, networks=8, n=4, per_row=2, normalize=0)
+    a.update(over)
+    return pnn.PnnRouter(*(a[f[0]] for f in pnn.PnnRouter._fields_))
+
+
+BAD = [(dict(n=-1), pnn.PNN_ESHAPE), (dict(n=1 << 31), pnn.PNN_ESHAPE), (dict(n=(1 << 29) + 1), pnn.PNN_ESHAPE)] + [
+    (d, pnn.PNN_EINVAL) for d in (
+        dict(networks=0), dict(networks=1025), dict(per_row=0), dict(per_row=9), dict(per_row=65, networks=128, s_ld=128),
+        dict(s=None), dict(s=FAKE + 2), dict(s_ld=7), dict(type=2))]
+
+
+@pytest.mark.parametrize("over,status", BAD)
+def test_arguments_are_refused(over, status):
+    L, a = pnn.lib(), args(**over)
+    assert L.pnn_route(ctypes.byref(a), FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 40, None) == status
+    assert L.pnn_route_grad(ctypes.byref(a), FAKE, FAKE, FAKE, FAKE, FAKE, 1024, None) == status
+    assert L.pnn_last_error(None)
+
+
+def test_memory_is_refused():
+    L, a, size = pnn.lib(), args(), ctypes.c_int64()
+    assert L.pnn_route_bytes(4, 8, ctypes.byref(size)) == pnn.PNN_OK and size.value >= 4 * 17
+    assert L.pnn_route_bytes(4, 8, None) == L.pnn_route_bytes(4, 0, ctypes.byref(size)) == pnn.PNN_EINVAL
+    assert L.pnn_route(None, FAKE, FAKE, None, None, None, 0, None) == pnn.PNN_EINVAL
+    for ids, gates, counts, loss, ws, have, status in (
+            (None, FAKE, FAKE, FAKE, FAKE, 1 << 20, pnn.PNN_EINVAL), (FAKE, None, FAKE, FAKE, FAKE, 1 << 20, pnn.PNN_EINVAL),
+            (FAKE, FAKE, FAKE, None, FAKE, 1 << 20, pnn.PNN_EINVAL), (FAKE, FAKE, None, FAKE, FAKE, 1 << 20, pnn.PNN_EINVAL),
+            (FAKE + 2, FAKE, FAKE, FAKE, FAKE, 1 << 20, pnn.PNN_EINVAL), (FAKE, FAKE, FAKE + 1, FAKE, FAKE, 1 << 20, pnn.PNN_EINVAL),
+            (FAKE, FAKE, FAKE, FAKE, None, 1 << 20, pnn.PNN_ESHAPE), (FAKE, FAKE, FAKE, FAKE, FAKE, 64, pnn.PNN_ESHAPE),
+            (FAKE, FAKE, FAKE, FAKE, FAKE + 4, 1 << 20, pnn.PNN_EINVAL)):
+        assert L.pnn_route(ctypes.byref(a), ids, gates, counts, loss, ws, have, None) == status
+    for ids, counts, dgates, dloss, ds, ld in (
+            (None, FAKE, FAKE, FAKE, FAKE, 8), (FAKE, None, FAKE, FAKE, FAKE, 8), (FAKE, FAKE, FAKE + 2, FAKE, FAKE, 8),
+            (FAKE, FAKE, FAKE, FAKE + 1, FAKE, 8), (FAKE, FAKE, FAKE, FAKE, None, 8), (FAKE, FAKE, FAKE, FAKE, FAKE + 2, 8),
+            (FAKE, FAKE, FAKE, FAKE, FAKE, 7)):
+        assert L.pnn_route_grad(ctypes.byref(a), ids, counts, dgates, dloss, ds, ld, None) == pnn.PNN_EINVAL
+
+
+def test_no_rows_need_no_device():
+    a = args(n=0, s=None)
+    assert pnn.lib().pnn_route(ctypes.byref(a), None, None, None, None, None, 0, None) == pnn.PNN_OK
+    assert pnn.lib().pnn_route_grad(ctypes.byref(a), None, None, None, None, None, 0, None) == pnn.PNN_OK
+
+
+def test_the_binding_refuses():
+    with pytest.raises(ValueError, match="matrix"):
+        pnn.route(torch.zeros(4), 1)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        pnn.route(torch.zeros(4, 8, dtype=torch.float64), 1)
+    with pytest.raises(ValueError, match="not contiguous"):
+        pnn.route(torch.zeros(8, 4).T, 1)
+    with pytest.raises(ValueError, match="CUDA"):
+        pnn.route(torch.zeros(4, 8), 1)
+    with pytest.raises(ValueError, match="ids has shape"):
+        pnn.route_grad(torch.zeros(4, 8), torch.zeros(4, dtype=torch.int32))
+
+
+# ---- values --------------------------------------------------------------------------------------
+
+def reference(s, k, normalize, dgates, dloss, ids=None):
+    """ids, gates, counts, loss, ds and what the gates, the loss and ds may be off by.  An exponential of d is off by
+    (3 |d| + 2) U: the difference, the factor and the product, two for the instruction; a sum by the terms' and a step
+    for each addition that a term passes through."""
+    n, K = s.shape
+    x, dg = s.double().cpu(), dgates.double().cpu()
+    nan = ~(torch.isfinite(x) | (x == -math.inf)).all(1)
+    clean = torch.where(nan[:, None], torch.zeros_like(x), x)
+    order = torch.argsort(-clean, dim=1, stable=True)[:, :k]
+    kept = (clean.gather(1, order) > -math.inf) & ~nan[:, None]
+    chosen = torch.where(kept, order, -1).to(torch.int32)
+    top = clean.amax(1, keepdim=True)
+    live = (top > -math.inf) & ~nan[:, None]
+    d = torch.where(live, clean - torch.where(live, top, 0.0), torch.full_like(x, -math.inf))
+    e = torch.exp(d)
+    p = e / torch.where(live, e.sum(1, keepdim=True), 1.0)
+    size = torch.where(p > 0, d.abs(), torch.zeros_like(d))
+    adds = 40
+    off_sum = (3 * (p * size).sum(1, keepdim=True) + adds) * U
+    off_p = p * ((3 * size + 6) * U + off_sum)
+    i = (chosen if ids is None else ids.cpu()).long()
+    kept = (i >= 0) & (i < K) & live
+    at = torch.where(kept, i, 0)
+    part, poff = torch.where(kept, p.gather(1, at), 0.0), torch.where(kept, off_p.gather(1, at), 0.0)
+    gates, goff = part, poff
+    if normalize:
+        mass = torch.where(part.sum(1, keepdim=True) > 0, part.sum(1, keepdim=True), 1.0)
+        gates = part / mass
+        # (at the chosen ones alone: the whole row's sum plays no part)
+        rel = torch.where(kept, (3 * size.gather(1, at) + 8) * U, 0.0)
+        goff = gates * (rel + (gates * rel).sum(1, keepdim=True) + 70 * U)
+    counts = torch.bincount(chosen[chosen >= 0].long(), minlength=K).double()
+    rows = int(live.sum())
+    weight = K * counts / max(1.0, float(counts.sum())) / max(1, rows)
+    P = p.sum(0)
+    loss = float((weight * P).sum())
+    passed = n / 1024 + 400  # additions that a row's share passes through
+    loss_off = float((weight * (off_p.sum(0) + P * passed * U)).sum()) + (passed + 8) * U * loss
+    a, aoff = dloss * weight, abs(dloss) * weight * 6 * U
+    dgk = torch.where(kept, dg, 0.0)
+    dot = (p * a).sum(1, keepdim=True)
+    dotoff = (off_p * a.abs() + p * (a.abs() * adds * U + aoff)).sum(1, keepdim=True)
+    mix = (gates * dgk).sum(1, keepdim=True)
+    mixoff = (goff * dgk.abs() + gates * dgk.abs() * adds * U).sum(1, keepdim=True)
+    o, ooff = (dot, dotoff) if normalize else (dot + mix, dotoff + mixoff)
+    ds = p * (a - o)
+    dsoff = off_p * (a - o).abs() + p * (aoff + ooff + 4 * U * (a.abs() + o.abs()))
+    share = gates * (dgk - mix if normalize else dgk)
+    soff = goff * (dgk.abs() + mix.abs()) + gates * (mixoff + 4 * U * (dgk.abs() + mix.abs()))
+    if not normalize:
+        soff = goff * dgk.abs() + 2 * U * share.abs()
+    share, soff = torch.where(kept, share, 0.0), torch.where(kept, soff, 0.0)
+    ds = ds.scatter_add(1, at, share)
+    dsoff = dsoff.scatter_add(1, at, soff + 4 * U * share.abs()) + (k + 2) * U * ds.abs() + 1e-37
+    counts = torch.cat([counts, torch.tensor([float(rows)])]).to(torch.int32)
+    bad = nan[:, None]
+    return (chosen, (torch.where(bad, math.nan, gates), goff + 1e-37), counts, (math.nan if nan.any() else loss, loss_off + 1e-37),
+            (torch.where(bad, math.nan, ds), dsoff))
+
+
+def near(got, want, off, dtype=F32):
+    got = got.double().cpu()
+    if dtype == BF16:
+        off = off + (want.abs() + off) * torch.finfo(BF16).eps / 2
+    ok = ((got - want).abs() <= off) | (torch.isnan(got) & torch.isnan(want))
+    assert ok.all(), f"{int((~ok).sum())} of {ok.numel()}, largest {((got - want).abs() / off)[~ok].max():.3g} of the tolerance"
+
+
+def case(n, K, k, dtype, seed=0, pad=0, scale=2.0):
+    g = torch.Generator().manual_seed(seed)
+    s = (torch.randn(n, K + pad, generator=g) * scale).to(dtype).cuda()[:, pad:]
+    return s, torch.randn(n, k, generator=g).cuda()
+
+
+def verify(s, k, normalize, dgates, dloss=0.7):
+    ids, gates, counts, loss = pnn.route(s, k, normalize=normalize)
+    ds = pnn.route_grad(s, ids, counts, dgates, torch.tensor([dloss], device="cuda"), normalize=normalize)
+    want = reference(s, k, normalize, dgates, dloss)
+    assert torch.equal(ids.cpu(), want[0]) and torch.equal(counts.cpu(), want[2])
+    near(gates, *want[1])
+    assert (math.isnan(want[3][0]) and torch.isnan(loss).all()) or abs(float(loss) - want[3][0]) <= want[3][1]
+    near(ds, *want[4], dtype=s.dtype)
+    alone = pnn.route(s, k, normalize=normalize, balance=False)
+    assert torch.equal(alone[0], ids) and torch.equal(alone[1].view(torch.int32), gates.view(torch.int32)) and alone[2:] == (None, None)
+    return ids, gates, counts, loss, ds
+
+
+SHAPES = [(1, 1, 1, 0), (3, 2, 2, 0), (60, 16, 3, 0), (17, 17, 5, 1), (33, 64, 8, 0), (20, 65, 20, 3), (64, 128, 16, 0), (9, 129, 64, 5),
+          (50, 256, 2, 0), (7, 257, 9, 0), (5, 512, 64, 1), (5, 513, 1, 0), (9, 1000, 8, 3), (3, 1024, 64, 0), (4097, 40, 2, 0),
+          (9001, 250, 4, 0)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,k,pad", SHAPES)
+def test_choice_and_gradient(n, K, k, pad, dtype):
+    s, dgates = case(n, K, k, dtype, pad=pad)
+    for normalize in (False, True):
+        verify(s, k, normalize, dgates)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,k", [(40, 12, 4), (40, 100, 20), (40, 300, 64)])
+def test_masks_ties_and_rows_without_a_network(n, K, k, dtype):
+    s, dgates = case(n, K, k, dtype, seed=3)
+    s[1] = 0.5                                # all alike: the lowest ones
+    s[2, K // 2:] = s[2, 0]                   # ties among others
+    s[3:10, 1:] = -math.inf                   # one network left
+    s[10:14] = -math.inf                      # none
+    s[14] = torch.finfo(dtype).min            # all at the lowest value
+    s[15, ::2] = torch.finfo(dtype).min
+    s[16, :k + 1] = 3e38
+    s[17] = -3e38
+    s[17, 3] = 3e38                           # (the difference leaves the range)
+    s[18, 5] = 80.0                           # the others' shares are nearly nothing
+    dgates[3:14, 1:] = math.nan               # what stands at no network is not read
+    for normalize in (False, True):
+        ids, gates, counts, loss, ds = verify(s, k, normalize, dgates)
+        assert (ids[10:14] == -1).all() and (gates[10:14] == 0).all() and (ds[10:14] == 0).all()
+        assert torch.equal(ids[1].cpu(), torch.arange(k, dtype=torch.int32))
+        assert int(counts[-1]) == n - 4 and torch.isfinite(ds).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,K,k", [(40, 12, 4), (40, 100, 20), (40, 300, 64)])
+def test_rows_that_hold_no_number(n, K, k):
+    """NaN and infinities: the row is NaN and so is the loss, the other rows keep their values."""
+    s, dgates = case(n, K, k, F32, seed=5)
+    s[1, 0], s[2, K - 1], s[3], s[4, 2], s[5] = math.nan, math.nan, math.nan, math.inf, math.inf
+    s[6, 3], s[6, 4] = math.nan, -math.inf
+    ids, gates, counts, loss, ds = verify(s, k, False, dgates)
+    assert (ids[1:7] == -1).all() and torch.isnan(gates[1:7]).all() and torch.isnan(ds[1:7]).all() and torch.isnan(loss).all()
+    assert torch.isfinite(ds[7:]).all() and int(counts[-1]) == n - 6
+    verify(s, k, True, dgates)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,k", [(30, 12, 4), (30, 300, 20)])
+def test_given_ids_and_gradients_alone(n, K, k, dtype):
+    """Ids of the caller's: other networks than the largest, one twice, outside the networks; either gradient alone."""
+    s, dgates = case(n, K, k, dtype, seed=7)
+    ids = torch.randint(0, K, (n, k), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    ids[:, 1] = ids[:, 0]
+    ids[3, 2], ids[4], ids[5, 0] = K, -1, -2 ** 31
+    ids = ids.cuda()
+    _, _, counts, _ = pnn.route(s, k)
+    one = torch.ones(1, device="cuda")
+    zero = torch.zeros_like(dgates)
+    for normalize in (False, True):
+        near(pnn.route_grad(s, ids, None, dgates, normalize=normalize), *reference(s, k, normalize, dgates, 0.0, ids)[4], dtype=dtype)
+        near(pnn.route_grad(s, ids, counts, None, one, normalize=normalize), *reference(s, k, normalize, zero, 1.0, ids)[4], dtype=dtype)
+        assert (pnn.route_grad(s, ids, normalize=normalize) == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("normalize", [False, True])
+@pytest.mark.parametrize("n,K,k", [(11, 10, 3), (5, 200, 6)])
+def test_gradient_against_differences(n, K, k, normalize):
+    """Central differences of sum gates dgates + dloss loss in 64 bits, the chosen networks kept."""
+    s, dgates = case(n, K, k, F32, seed=9, scale=1.0)
+    ids, _, counts, _ = pnn.route(s, k, normalize=normalize)
+    ds = pnn.route_grad(s, ids, counts, dgates, torch.tensor([2.0], device="cuda"), normalize=normalize).double().cpu()
+    at = ids.long().cpu()
+    share = K * counts[:K].double().cpu() / (n * k) / n
+
+    def value(x):
+        p = torch.softmax(x, 1)
+        gates = torch.softmax(x.gather(1, at), 1) if normalize else p.gather(1, at)
+        return (gates * dgates.double().cpu()).sum(1) + 2.0 * (p * share).sum(1)
+
+    h = 1e-4
+    for e in list(range(4)) + [int(at[0, 0]), K - 1]:
+        up, down = s.double().cpu(), s.double().cpu()
+        up[:, e] += h
+        down[:, e] -= h
+        # the third derivative of a softmax is at most 1 a term: h^2 / 6 of the terms' sizes, and 64-bit noise over h
+        size = dgates.double().cpu().abs().sum(1) + 2.0
+        assert ((value(up) - value(down)) / (2 * h) - ds[:, e]).abs().le(size * (h * h + 1e-10 + 2.0 ** -20)).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,k,pad", [(30, 10, 3, 0), (30, 100, 9, 3), (21, 700, 30, 6)])
+def test_gradient_in_place_and_strided(n, K, k, pad, dtype):
+    s, dgates = case(n, K, k, dtype, seed=11, pad=pad)
+    one = torch.ones(1, device="cuda")
+    ids, _, counts, _ = pnn.route(s, k)
+    want = pnn.route_grad(s, ids, counts, dgates, one)
+    whole = torch.full((n + 2, K + 7), 5.0, dtype=dtype, device="cuda")
+    plain = whole.clone()
+    pnn.route_grad(s, ids, counts, dgates, one, out=whole[1:-1, 3:-4])
+    plain[1:-1, 3:-4] = want
+    assert torch.equal(whole, plain)
+    pnn.route_grad(s, ids, counts, dgates, one, out=s)
+    assert torch.equal(s, want)
+
+
+@gpu
+def test_rows_behind_32_bits():
+    n, K = 36_000_000, 64
+    s = torch.zeros(n, K, dtype=BF16, device="cuda")
+    s[-1, 63], s[-2, 5] = 4, 4
+    ids, gates, counts, loss = pnn.route(s, 1)
+    assert ids[-3:].flatten().tolist() == [0, 5, 63] and counts[[0, 5, 63, 64]].tolist() == [n - 2, 1, 1, n]
+    top = math.exp(4) / (math.exp(4) + 63)
+    assert abs(float(gates[-1]) - top) <= 1e-6 and (gates[:-2] == 1 / 64).all()
+    assert abs(float(loss) - 1) <= 1e-3  # (every sum of p is n / 64 up to two rows, and n / 1024 + 400 additions)
+    ds = pnn.route_grad(s, ids, None, torch.ones_like(gates), out=s)
+    assert abs(float(ds[-1, 63]) - top * (1 - top)) <= 2.0 ** -8 and abs(float(ds[-1, 0]) + top * (1 - top) / 63) <= 2.0 ** -8
+    assert (ds[:-2, 0] == ds[0, 0]).all() and (ds[:-2, 1:] == ds[0, 1]).all()
+
+
+@gpu
+def test_no_rows():
+    s = torch.empty(0, 8, device="cuda")
+    ids, gates, counts, loss = pnn.route(s, 2)
+    assert ids.shape == gates.shape == (0, 2) and (counts == 0).all() and float(loss) == 0
+    assert pnn.route_grad(s, ids, counts, gates).shape == (0, 8)
+
+
+@gpu
+@pytest.mark.parametrize("n,K,k", [(40, 10, 3), (5000, 300, 8)])
+def test_another_stream_a_graph_and_the_same_bits(n, K, k):
+    s, dgates = case(n, K, k, F32)
+    one = torch.ones(1, device="cuda")
+
+    def step(stream=None):
+        ids, gates, counts, loss = pnn.route(s, k, normalize=True, stream=stream)
+        return ids, gates, counts, loss, pnn.route_grad(s, ids, counts, dgates, one, normalize=True, stream=stream)
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for _ in range(4):
+        s.mul_(-0.75)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(kept, step()):
+            assert torch.equal(a, b)
