@@ -321,6 +321,34 @@ pnn_status pnn_grouped_backward_weights(const pnn_groups* groups, const pnn_grou
                                         int64_t dw_ld, float* db_dev, int64_t db_net, void* ws_dev, int64_t ws_bytes,
                                         void* hip_stream);
 
+/* The forward product from 8-bit codes, for serving: rows and weights are integers in -127..127 with a scale
+ * for each row and for each output of a network, a quarter of fp32's bytes and twice the rate of bf16. */
+
+/* q[r][i] = the integer nearest to 127 x[r][i] / max_i |x[r][i]| (ties to even), scale[r] = max_i |x[r][i]| / 127
+ * (fp32), so that x is about scale q.  x_dev [n][width] of `type`; q_dev int8 [n][width rounded up to a multiple of
+ * 16], zeros past the width, its rows at multiples of 16 bytes.  A row of zeros has codes and a scale of 0, one
+ * with a NaN or an infinity codes of 0 and a scale of NaN, which its products show. */
+pnn_status pnn_quantize_rows(const void* x_dev, int64_t x_ld, int32_t type, int64_t n, int32_t width, int8_t* q_dev, int64_t q_ld,
+                             float* scale_dev, void* hip_stream);
+
+/* One layer of every network in codes: w_dev[e w_net + o w_ld + i] with scale_dev[e scale_net + o] (fp32), biases
+ * as above.  inputs is a multiple of 16, at most 2^17 (sums are 32-bit integers and do not overflow); w_ld and w_net are
+ * multiples of 16, w_dev is 16-byte aligned. */
+typedef struct {
+    int32_t inputs, outputs;
+    const int8_t* w_dev;
+    int64_t w_net, w_ld;
+    const float* scale_dev;
+    int64_t scale_net;
+    const float* b_dev;
+    int64_t b_net;
+} pnn_group_codes;
+
+/* y[p] = phi(x_scale[r] w_scale[e][o] sum_i x[r][i] w_e[o][i] + b_e), r = p / per_row, as pnn_grouped_forward; the sum
+ * is exact, and rounded to fp32 once.  x_dev int8 [n][inputs], rows at multiples of 16 bytes; x_scale_dev [n]. */
+pnn_status pnn_grouped_forward_int8(const pnn_groups* groups, const pnn_group_codes* layer, const int8_t* x_dev, int64_t x_ld,
+                                    const float* x_scale_dev, int32_t act, void* y_dev, int64_t y_ld, int32_t y_type, void* hip_stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Rows that choose their networks.  A router scores every network for a row; the row goes through
  * the ones that it likes best, and their results are weighed into one.  No handle and nothing kept, as

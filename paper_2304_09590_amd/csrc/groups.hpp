@@ -10,6 +10,9 @@
 //   forward          y[p]  = phi(W_e x[p / per_row] + b_e), e = id[p]
 //   input gradient   dx[r] = sum_j W_e^T dy[r per_row + j] (.) phi'(a[r])
 //   weight gradient  dW_e  = sum_p dy[p] x[p / per_row]^T,  db_e = sum_p dy[p]
+//
+// The forward product also takes rows and weights as 8-bit codes with a scale for each row and each output:
+//   y[p] = phi(sx[p / per_row] sw[e, o] sum_i qx qw + b), the sum in integers.
 #pragma once
 #include "kernels.hpp"
 
@@ -289,6 +292,8 @@ struct GroupGemm {
     Div wdiv;
     const float* b;            // bias (nullable)
     int64_t bnet;
+    const float *sx, *sw;      // (codes) scales of p's rows, and of w's
+    int64_t swnet;
     int act;                   // activation (forward), or the one whose slope at a scales the result; -1 none
     const void* a;             // stored activations of the slope, row (pair)
     int64_t lda;
@@ -321,6 +326,24 @@ typedef f4 f4_a4 __attribute__((aligned(4)));
 template <typename T> struct Raw8;
 template <> struct Raw8<bf16_t> { u4v v; };
 template <> struct Raw8<float> { f4 v[2]; };
+
+// Two neighbouring 8-bit codes.  A matrix of codes is walked in these, as a bf16 matrix of half the width: a lane's
+// 16 bytes are the operand of one instruction either way (16 x 16 x 32 bf16, 16 x 16 x 64 codes), so the tiles, the
+// copies and the places in LDS are the same.  Rows start at multiples of 16 bytes and are whole numbers of them.
+struct codes_t { uint16_t two; };
+template <> struct Raw8<codes_t> { u4v v; };
+__device__ inline void load8(Raw8<codes_t>& r, const codes_t* p, int nv) { r.v = nv >= 8 ? *(const u4v*)p : u4v{0, 0, 0, 0}; }
+
+typedef int i4 __attribute__((ext_vector_type(4)));
+template <typename T> struct Sum4 { typedef f4 type; };      // a lane's sums of a 16 x 16 block
+template <> struct Sum4<codes_t> { typedef i4 type; };
+template <typename T>
+__device__ inline typename Sum4<T>::type group_mfma(bf8v a, bf8v b, typename Sum4<T>::type c) {
+    if constexpr (std::is_same<T, codes_t>::value)
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, a), __builtin_bit_cast(i4, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
 // the first nv of eight values at p (the others 0); nv <= 0 reads nothing
 __device__ inline void load8(Raw8<bf16_t>& r, const bf16_t* p, int nv) {
@@ -535,7 +558,7 @@ __device__ inline void group_slope8(int act, float (&v)[8], const float (&a)[8])
 // a lane takes eight neighbouring results of one column: rows leave in stores of 16 or 32 bytes a lane.
 template <int MI> constexpr int group_turn() { return 16 * (16 * MI + 4); }  // floats of a wave
 template <int DIR, typename T, typename TO, int MI, int NJ>
-__device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], const f4 (&accb)[NJ], int e, int split, int p0, int m0,
+__device__ inline void group_store(const GroupGemm& g, const typename Sum4<T>::type (&acc)[MI][NJ], const f4 (&accb)[NJ], int e, int split, int p0, int m0,
                                    int n0, int nv, int wm, int wn, int lane, bool bias_rows, float* turn) {
     constexpr int LD = 16 * MI + 4, PER = 2 * MI, COLS = MI == 1 ? 16 : 64 / PER;  // lanes of a column, columns at a time
     const int l15 = lane & 15, kg = lane >> 4, part = lane % PER * 8, m = m0 + wm + part;
@@ -548,10 +571,17 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     int own[OWN];
 #pragma unroll
     for (int h = 0; h < OWN; ++h) own[h] = DIR != GR_DW && wn + 64 * h + lane < nv ? g.pairs[p0 + wn + 64 * h + lane] : 0;
-    float bias[8];
+    constexpr bool CODES = std::is_same<T, codes_t>::value;
+    float bias[8], scale_m[8], scale_n[OWN];
     if (DIR == GR_FWD) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) bias[r] = g.b && r < left && e < g.K ? g.b[e * g.bnet + m + r] : 0.0f;
+    }
+    if (CODES) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) scale_m[r] = r < left && e < g.K ? g.sw[e * g.swnet + m + r] : 0.0f;
+#pragma unroll
+        for (int h = 0; h < OWN; ++h) scale_n[h] = wn + 64 * h + lane < nv ? g.sx[g.pdiv.of(own[h])] : 0.0f;
     }
     // what a result is combined with (slopes' activations, weights to update) is loaded sixteen columns ahead:
     // behind a store it would wait for it
@@ -575,11 +605,12 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
     for (int j = 0; j < NJ; ++j) {
         if (has_with && j + 1 < NJ) fetch(j + 1);
 #pragma unroll
-        for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = acc[i][j];
+        for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = __builtin_convertvector(acc[i][j], f4);
         __builtin_amdgcn_wave_barrier();
         auto leave = [&](int c, bool smooth) {
             const int col = c * COLS + lane / PER, n = column(j, c);
             const int64_t pair = DIR != GR_DW ? pair_of(j, c) : 0;
+            const float by = CODES ? __shfl(scale_n[j / 4], 16 * (j & 3) + c * COLS + lane / PER) : 1.0f;
             if (n >= nv || left <= 0) return;
             const f4 lo = *(const f4*)(turn + col * LD + part), hi = *(const f4*)(turn + col * LD + part + 4);
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -600,7 +631,7 @@ __device__ inline void group_store(const GroupGemm& g, const f4 (&acc)[MI][NJ], 
                 for (int r = 0; r < 8; ++r) v[r] = 0.0f;
             } else if (DIR == GR_FWD) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] += bias[r];
+                for (int r = 0; r < 8; ++r) v[r] = CODES ? __builtin_fmaf(v[r] * by, scale_m[r], bias[r]) : v[r] + bias[r];
                 if (smooth) group_act8(g.act, v);
                 else group_rectify8(g.act, v);
             } else if (has_with) {
@@ -801,8 +832,9 @@ struct RTile {
 
 // AHEAD: a stage is waited for one step before it is multiplied, so that a step's first operands are read
 // during the step before it.
-template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
+template <int DIR, typename T, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
 __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g) {
+    typedef typename Sum4<T>::type Sum;
     typedef RTile<DIR == GR_FWD, BM> TA;
     typedef RTile<DIR != GR_DW, BN> TB;
     constexpr int THREADS = 64 * WM * WN;
@@ -817,12 +849,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
     const int e = place.e, m0 = place.m0, n0 = place.n0, nv = place.nv, split = place.split, p0 = place.p0, Kx = place.Kx;
     const int mv = g.M - m0 < BM ? g.M - m0 : BM;
     const bf16_t* zeros = (const bf16_t*)group_zeros;
-    f4 acc[MI][NJ], accb[NJ];
+    Sum acc[MI][NJ];
+    f4 accb[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         accb[j] = f4{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < MI; ++i) acc[i][j] = f4{0, 0, 0, 0};
+        for (int i = 0; i < MI; ++i) acc[i][j] = Sum{0, 0, 0, 0};
     }
     const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
     const bool bias_rows = DIR == GR_DW && g.db && m0 == 0 && wm == 0;
@@ -942,7 +975,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j) acc[i][j] = group_mfma<T>(f[i], fb[j], acc[i][j]);
             if (DIR == GR_DW) refill(t);  // (behind the operands' reads, which then do not wait for the
             // numbers': 131,072 pairs 2048 x 2048 1,132 -> 1,103 us)
             // reads two operands ahead of the products that take them, the next step's with the last ones
@@ -985,7 +1018,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < NJ; ++j) acc[i][j] = group_mfma<T>(fa[i], fb[j], acc[i][j]);
             // reads two operands ahead of the products that take them
             __builtin_amdgcn_sched_group_barrier(0x100, RB * NJ + 2 * RA, 0);
 #pragma unroll
@@ -999,7 +1032,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void group_ring_kernel(GroupGemm g
         }
     }
     ring_wait<0>();  // (no copy outlives its workgroup)
-    group_store<DIR, bf16_t, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
+    group_store<DIR, T, TO, MI, NJ>(g, acc, accb, e, split, p0, m0, n0, nv, wm, wn, lane, bias_rows,
                                          (float*)ring + wave * group_turn<MI>());
 }
 
@@ -1101,7 +1134,9 @@ template <typename T, typename TO>
 __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int STEP = F32 ? 32 : 64, W = STEP / 4;  // values of a lane per step
-    __shared__ float part[4][GS_OUT / 16][16][20];
+    typedef typename Sum4<T>::type Sum;
+    typedef typename std::conditional<std::is_same<T, codes_t>::value, int, float>::type S;
+    __shared__ S part[4][GS_OUT / 16][16][20];
     const int tid = threadIdx.x, lane = tid & 63, l15 = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int mt = (g.M + GS_OUT - 1) / GS_OUT;
@@ -1112,9 +1147,9 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
     const int e = t.x, m0 = (int)band * GS_OUT, p0 = t.y;
     const int end = e < g.K ? g.off[e + 1] : g.N;
     const int nv = end - p0 < 16 ? end - p0 : 16;
-    f4 acc[GS_OUT / 16];
+    Sum acc[GS_OUT / 16];
 #pragma unroll
-    for (int i = 0; i < GS_OUT / 16; ++i) acc[i] = f4{0, 0, 0, 0};
+    for (int i = 0; i < GS_OUT / 16; ++i) acc[i] = Sum{0, 0, 0, 0};
     if (e < g.K) {
         const int share = (g.Kx + 4 * STEP - 1) / (4 * STEP) * STEP;
         const int k1 = (wave + 1) * share < g.Kx ? (wave + 1) * share : g.Kx;
@@ -1141,14 +1176,13 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
                         for (int c = 0; c < 8; ++c)
                             acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(rw[i][h].v[c >> 2][c & 3], rx[h].v[c >> 2][c & 3], acc[i], 0, 0, 0);
                     } else {
-                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, rw[i][h].v),
-                                                                         __builtin_bit_cast(bf8v, rx[h].v), acc[i], 0, 0, 0);
+                        acc[i] = group_mfma<T>(__builtin_bit_cast(bf8v, rw[i][h].v), __builtin_bit_cast(bf8v, rx[h].v), acc[i]);
                     }
                 }
         }
     }
 #pragma unroll
-    for (int i = 0; i < GS_OUT / 16; ++i) *(f4*)&part[wave][i][l15][4 * kg] = acc[i];
+    for (int i = 0; i < GS_OUT / 16; ++i) *(Sum*)&part[wave][i][l15][4 * kg] = acc[i];
     __syncthreads();
     const int n = tid >> 4, i = (tid >> 3) & 1, o = (tid & 7) * 2;
     if (n >= nv) return;
@@ -1159,8 +1193,11 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
         if (m >= g.M) continue;
         float v = 0.0f;
         if (e < g.K) {
+            S sum = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v += part[q][i][n][o + r];
+            for (int q = 0; q < 4; ++q) sum += part[q][i][n][o + r];
+            v = (float)sum;
+            if (std::is_same<T, codes_t>::value) v = v * g.sx[g.pdiv.of((int)pair)] * g.sw[e * g.swnet + m];
             if (g.b) v += g.b[e * g.bnet + m];
             v = group_act(g.act, v);
         }

@@ -154,13 +154,13 @@ bool ring_ok(const void* p, int64_t ld, int64_t net, int width) {
     return aligned16(p) && ld % 8 == 0 && ld < (int64_t(1) << 31) && net % 8 == 0 && width % 8 == 0;
 }
 
-template <int DIR, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
+template <int DIR, typename T, typename TO, int BM, int BN, int WM, int WN, int NST, bool AHEAD>
 pnn_status launch_ring(const GroupGemm& a, int64_t blocks, hipStream_t s) {
     const int lds = NST * (BM + BN) * 32 * 2 + (DIR == GR_DW ? WM * WN * 2 * (NST - 1) * 256 : 0);
     TRY(grid_fits(blocks, 64 * WM * WN));
     static std::atomic<uint64_t> set{0};
-    TRY(lds_of((const void*)group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD>, lds, set));
-    group_ring_kernel<DIR, TO, BM, BN, WM, WN, NST, AHEAD><<<(unsigned)blocks, 64 * WM * WN, lds, s>>>(a);
+    TRY(lds_of((const void*)group_ring_kernel<DIR, T, TO, BM, BN, WM, WN, NST, AHEAD>, lds, set));
+    group_ring_kernel<DIR, T, TO, BM, BN, WM, WN, NST, AHEAD><<<(unsigned)blocks, 64 * WM * WN, lds, s>>>(a);
     return launched(DIR == GR_FWD ? "grouped forward" : DIR == GR_DX ? "grouped input gradient" : "grouped weight gradient");
 }
 
@@ -202,17 +202,23 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     // 75 -> 78.
     a.stream = sizeof(TO) == 2 && p.P * a.M * (int64_t)sizeof(TO) >= (int64_t(96) << 20);
     if constexpr (sizeof(T) == 2) {
-        if (kind == RING_HUGE) return launch_ring<DIR, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
-        if (kind == RING) return launch_ring<DIR, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);
-        if (kind == RING_SMALL) return launch_ring<DIR, TO, 128, 64, 2, 2, 4, false>(a, blocks(128), s);
+        if (kind == RING_HUGE) return launch_ring<DIR, T, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
+        if (kind == RING) return launch_ring<DIR, T, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);
+        if (kind == RING_SMALL) return launch_ring<DIR, T, TO, 128, 64, 2, 2, 4, false>(a, blocks(128), s);
     }
     const int64_t all = blocks(kind == TILE128 ? 128 : kind == TILE64 ? 64 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
     TRY(grid_fits(all, 256));
-    if (kind == TILE128) group_tile_kernel<DIR, T, TO, 128><<<(unsigned)all, 256, 0, s>>>(a);
-    else if (kind == TILE64) group_tile_kernel<DIR, T, TO, 64><<<(unsigned)all, 256, 0, s>>>(a);
-    else if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
+    const char* what = DIR == GR_FWD ? "grouped forward" : "grouped input gradient";
+    if constexpr (!std::is_same<T, codes_t>::value) {  // (rows of codes are always at 16 bytes)
+        if (kind != FEW) {
+            if (kind == TILE128) group_tile_kernel<DIR, T, TO, 128><<<(unsigned)all, 256, 0, s>>>(a);
+            else group_tile_kernel<DIR, T, TO, 64><<<(unsigned)all, 256, 0, s>>>(a);
+            return launched(what);
+        }
+    }
+    if constexpr (DIR == GR_FWD) group_few_fwd_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
     else group_few_dx_kernel<T, TO><<<(unsigned)all, 256, 0, s>>>(a);
-    return launched(DIR == GR_FWD ? "grouped forward" : "grouped input gradient");
+    return launched(what);
 }
 
 template <int DIR>
@@ -246,9 +252,9 @@ pnn_status run_group_weights(const pnn_groups* g, int32_t inputs, int32_t output
         return group_dw_blocks((int64_t)((inputs + bm - 1) / bm) * ((outputs + bn - 1) / bn), (int64_t)S * g->networks);
     };
     if (type != PNN_FP32 && ring_ok(x, x_ld, 0, inputs) && ring_ok(dy, dy_ld, 0, outputs)) {
-        if (kind == RING_HUGE) TRY((launch_ring<GR_DW, float, 256, 256, 2, 4, 4, true>(a, blocks(256, 256), s)));
-        else if (kind == RING) TRY((launch_ring<GR_DW, float, 256, 128, 2, 2, 3, false>(a, blocks(256, 128), s)));
-        else TRY((launch_ring<GR_DW, float, 128, 64, 2, 2, 4, false>(a, blocks(128, 64), s)));
+        if (kind == RING_HUGE) TRY((launch_ring<GR_DW, bf16_t, float, 256, 256, 2, 4, 4, true>(a, blocks(256, 256), s)));
+        else if (kind == RING) TRY((launch_ring<GR_DW, bf16_t, float, 256, 128, 2, 2, 3, false>(a, blocks(256, 128), s)));
+        else TRY((launch_ring<GR_DW, bf16_t, float, 128, 64, 2, 2, 4, false>(a, blocks(128, 64), s)));
     } else {
         const bool small = blocks(128, 128) < GROUP_FILL;
         const int64_t all = small ? blocks(64, 64) : blocks(128, 128);

@@ -37,6 +37,7 @@
 #include "kernels.hpp"
 #include "groups.hpp"
 #include "distill.hpp"
+#include "codes.hpp"
 #include "route.hpp"
 
 using namespace pnn;
@@ -1800,6 +1801,7 @@ void pnn_destroy(pnn_net* n) {
 }  // extern "C"
 
 #include "groups_host.hpp"
+#include "codes_host.hpp"
 #include "route_host.hpp"
 #include "distill_host.hpp"
 #include "routed_host.hpp"

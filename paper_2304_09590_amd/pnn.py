@@ -58,6 +58,12 @@ class PnnDistill(ctypes.Structure):
                 ("y", ctypes.c_void_p), ("temperature", ctypes.c_float), ("alpha", ctypes.c_float)]
 
 
+class PnnGroupCodes(ctypes.Structure):
+    _fields_ = [("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("w", ctypes.c_void_p), ("w_net", ctypes.c_int64),
+                ("w_ld", ctypes.c_int64), ("scale", ctypes.c_void_p), ("scale_net", ctypes.c_int64), ("b", ctypes.c_void_p),
+                ("b_net", ctypes.c_int64)]
+
+
 class PnnRouter(ctypes.Structure):
     _fields_ = [("s", ctypes.c_void_p), ("s_ld", ctypes.c_int64), ("type", ctypes.c_int32), ("networks", ctypes.c_int32),
                 ("n", ctypes.c_int64), ("per_row", ctypes.c_int32), ("normalize", ctypes.c_int32)]
@@ -135,6 +141,10 @@ def lib() -> ctypes.CDLL:
         for name in ("pnn_group_bytes", "pnn_group_rows", "pnn_grouped_forward", "pnn_grouped_workspace",
                      "pnn_grouped_backward_input", "pnn_grouped_backward_weights"):
             getattr(L, name).restype = i32
+        L.pnn_quantize_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp]
+        L.pnn_quantize_rows.restype = i32
+        L.pnn_grouped_forward_int8.argtypes = [groups, P(PnnGroupCodes), vp, i64, vp, i32, vp, i64, i32, vp]
+        L.pnn_grouped_forward_int8.restype = i32
         router, combine = P(PnnRouter), P(PnnCombine)
         L.pnn_route_bytes.argtypes = [i64, i32, P(i64)]
         L.pnn_route.argtypes = [router, vp, vp, vp, vp, vp, i64, vp]
@@ -574,6 +584,55 @@ def grouped_backward_weights(groups: RowGroups, dy, x, dw=None, db=None, bias: b
         return w, b
 
     return _on(stream, body, x, dy, dw, db, groups=groups)
+
+
+def quantize_rows(x, stream=None):
+    """(codes int8, scales fp32) of the rows of x [..., width]: the integers nearest to 127 x / max |x| of the row and
+    max |x| / 127; codes are [..., width rounded up to a multiple of 16], zeros past the width."""
+    torch = _t()
+    if x.dim() < 2 or 0 in x.shape[-1:]:
+        raise ValueError(f"x has shape {tuple(x.shape)}, expected rows")
+    if x.dim() > 2 and not x.is_contiguous():
+        raise ValueError("a stack of matrices has to be contiguous")
+    width = x.shape[-1]
+    rows = x if x.dim() == 2 else x.view(-1, width)
+    n, padded = rows.shape[0], -(-width // 16) * 16
+    px, ldx = _rows(rows, "x", rows.shape, x.dtype)
+    kind = _type_of(x)
+
+    def body(s):
+        codes, scale = _empty(x, (*x.shape[:-1], padded), torch.int8), _empty(x, x.shape[:-1], torch.float32)
+        _call("pnn_quantize_rows", px, ldx, kind, n, width, codes.data_ptr(), padded, scale.data_ptr(), s)
+        return codes, scale
+
+    return _on(stream, body, x)
+
+
+def grouped_forward_int8(groups: RowGroups, x, x_scale, w, w_scale, b=None, act: Optional[int] = None, out=None, out_dtype=None,
+                         stream=None):
+    """grouped_forward from 8-bit codes: x int8 [n, inputs] with x_scale fp32 [n], w int8 [networks, outputs, inputs]
+    with w_scale fp32 [networks, outputs] (quantize_rows gives both); y is out_dtype, float32 if None."""
+    torch = _t()
+    shape = w.shape
+    if len(shape) != 3 or shape[0] != groups.networks:
+        raise ValueError(f"w has shape {tuple(shape)}, expected ({groups.networks}, outputs, inputs)")
+    outputs, inputs = shape[1:]
+    pw, w_ld = _rows(w, "w", shape, torch.int8)
+    ps, scale_net = _rows(w_scale, "w_scale", shape[:2], torch.float32)
+    pb, b_net = _rows(b, "b", shape[:2], torch.float32) if b is not None else (None, 0)
+    layer = PnnGroupCodes(inputs, outputs, pw, w.stride(0) if groups.networks > 1 else 0, w_ld, ps, scale_net, pb, b_net)
+    size = (groups.n * groups.per_row, outputs)
+
+    def body(s):
+        y = out if out is not None else _empty(x_scale, size, out_dtype)
+        px, ldx = _rows(x, "x", (groups.n, inputs), torch.int8)
+        pxs = _values(x_scale, "x_scale", (groups.n,), torch.float32)
+        py, ldy = _rows(y, "out", size, out_dtype or y.dtype)
+        _call("pnn_grouped_forward_int8", ctypes.byref(groups.struct), ctypes.byref(layer), px, ldx, pxs,
+              -1 if act is None else act, py, ldy, _type_of(y), s)
+        return y
+
+    return _on(stream, body, x, x_scale, w, w_scale, b, out, groups=groups)
 
 
 @functools.lru_cache(maxsize=1024)
