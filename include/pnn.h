@@ -410,6 +410,48 @@ pnn_status pnn_combine_grad(const pnn_combine* args, const void* g_dev, int64_t 
                             float* dw_dev, void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A step of AdamW over many tensors, beside the SGD of the training calls: for networks that a program
+ * trains with the gradients above.  With step number t, which the call counts on the device,
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32.  Parameters are fp32, with a bf16 copy (rounded to nearest even) where the products read one.
+ * Moments are fp32 (bits = 32) or 8-bit codes (bits = 8), a byte a value and a scale for each 256 values of
+ * a tensor: the largest |m| or v among them.  m's byte is a sign (the high bit) and a code c of 127, v's a code of 255:
+ * 0 stands for 0, another for scale * 2^((c - 127) / 8) or 2^((c - 255) / 8).  A step takes the moments
+ * before they are rounded.  Rounding goes up or down at random in proportion (v's lowest code counts for
+ * all below it), by bits that are a function of seed, t, the tensor's place in the call, and the value's place: the
+ * same call gives the same bits.  A moment that is infinite or NaN makes its block's scale NaN.  States begin as zeros. */
+typedef struct {
+    float* p_dev;                     /* [n] */
+    const void* g_dev;                /* [n] of g_type */
+    void *m_dev, *v_dev;              /* [n] fp32, or bytes */
+    float *m_scale_dev, *v_scale_dev; /* [ceil(n / 256)] (bits = 8) */
+    uint16_t* copy_dev;               /* [n] bf16, nullable */
+    int64_t n;                        /* 0..2^40 */
+} pnn_adamw_tensor;
+
+typedef struct {
+    int32_t bits;         /* 32 or 8 */
+    int32_t g_type;
+    double lr;            /* 0..1e6 */
+    double beta1, beta2;  /* in [0, 1) */
+    double eps;           /* 1e-30..1 */
+    double weight_decay;  /* 0..1e6 */
+    const float* lr_dev;  /* (nullable) [1], read by the step instead of lr: a recorded step's rate may change */
+    uint32_t seed;
+    int32_t* steps_dev;   /* [2]: the steps done so far, and 0 (the library's own during a call) */
+} pnn_adamw;
+
+/* One step of `count` tensors (host array, read during the call; values are contiguous, no two tensors
+ * overlap, aligned to their types).  Any number of launches, one for each 48 tensors.  Calls that share steps_dev are
+ * ordered by the caller.  May be recorded into a graph. */
+pnn_status pnn_adamw_step(const pnn_adamw* args, const pnn_adamw_tensor* tensors, int32_t count, void* hip_stream);
+
+/* What the 8-bit states of n values stand for, in fp32. */
+pnn_status pnn_adamw_values(const uint8_t* m_dev, const uint8_t* v_dev, const float* m_scale_dev, const float* v_scale_dev, int64_t n,
+                            float* m_out_dev, float* v_out_dev, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Distillation: a network learns another's answers (a way to combine CNs beside averaging them).
  * Row r has `classes` logits z, a teacher's `top` entries (class idx, logit t) and a label y.
  *   p = softmax(t / T) over the row's entries, q = softmax(z / T), s = softmax(z):

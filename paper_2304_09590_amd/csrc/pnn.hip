@@ -36,6 +36,7 @@
 #include "../../include/pnn.h"
 #include "kernels.hpp"
 #include "groups.hpp"
+#include "adamw.hpp"
 #include "distill.hpp"
 #include "codes.hpp"
 #include "route.hpp"
@@ -1803,5 +1804,6 @@ void pnn_destroy(pnn_net* n) {
 #include "groups_host.hpp"
 #include "codes_host.hpp"
 #include "route_host.hpp"
+#include "adamw_host.hpp"
 #include "distill_host.hpp"
 #include "routed_host.hpp"

@@ -75,6 +75,17 @@ class PnnCombine(ctypes.Structure):
                 ("w", ctypes.c_void_p)]
 
 
+class PnnAdamwTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class PnnAdamw(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32), ("g_type", ctypes.c_int32), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("lr_dev", ctypes.c_void_p),
+                ("seed", ctypes.c_uint32), ("steps", ctypes.c_void_p)]
+
+
 class PnnError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -153,6 +164,10 @@ def lib() -> ctypes.CDLL:
         L.pnn_combine_grad.argtypes = [combine, vp, i64, i32, vp, i64, vp, vp]
         for name in ("pnn_route_bytes", "pnn_route", "pnn_route_grad", "pnn_combine_rows", "pnn_combine_grad"):
             getattr(L, name).restype = i32
+        L.pnn_adamw_step.argtypes = [P(PnnAdamw), P(PnnAdamwTensor), i32, vp]
+        L.pnn_adamw_step.restype = i32
+        L.pnn_adamw_values.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp]
+        L.pnn_adamw_values.restype = i32
         distill = P(PnnDistill)
         L.pnn_distill_bytes.argtypes = [i64, i32, P(i64)]
         L.pnn_distill_loss.argtypes = [distill, vp, vp, i64, vp]
@@ -730,6 +745,105 @@ def combine_grad(dout, y, ids, gates, networks: int, dy=None, stream=None):
         return d, dgates
 
     return _on(stream, body, y, dout, ids, gates, dy)
+
+
+class AdamW:
+    """AdamW over many tensors at once (pnn_adamw_step): fp32 params, their gradients (float32 or bfloat16, read by every
+    step from the tensors given here), optionally bf16 copies that each step writes (None for a tensor without
+    one), states in 32 or in 8 bits.
+
+    state: lists of the moments m and v (bits = 8: bytes, and lists of their scales, one for 256 values), zeros if None;
+    steps: int32 [2], the steps done and 0.  Both belong to the object afterwards: saved and given again, training goes
+    on with the same bits.  lr may be a float32 tensor [1] on the device, which each step reads."""
+
+    def __init__(self, params, grads, copies=None, bits: int = 32, lr=1e-3, betas: Tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay: float = 1e-2, seed: int = 0, state=None, steps=None):
+        torch = _t()
+        self.params, self.grads, self.copies, self.bits = list(params), list(grads), list(copies) if copies is not None else None, bits
+        count = len(self.params)
+        if not count:
+            raise ValueError("no parameters")
+        if bits not in (32, 8):
+            raise ValueError(f"bits = {bits}, expected 32 or 8")
+        if len(self.grads) != count or (self.copies is not None and len(self.copies) != count):
+            raise ValueError("as many gradients and copies as parameters are expected")
+        first = self.params[0]
+        held = torch.float32 if bits == 32 else torch.uint8
+        if state is None:
+            state = [[torch.zeros(p.shape, dtype=held, device=p.device) for p in self.params] for _ in "mv"]
+            if bits == 8:
+                state += [[torch.zeros(-(-p.numel() // 256), device=p.device) for p in self.params] for _ in "mv"]
+        self.state = [list(s) for s in state]
+        if len(self.state) != (2 if bits == 32 else 4) or any(len(s) != count for s in self.state):
+            raise ValueError("state: lists of m and v, with 8 bits of their scales too, one for each parameter")
+        self.steps = steps if steps is not None else torch.zeros(2, dtype=torch.int32, device=first.device)
+        g_type = self.grads[0].dtype
+        lists = [(self.params, "params", torch.float32), (self.grads, "grads", g_type), (self.state[0], "m", held), (self.state[1], "v", held)]
+        if self.copies is not None:
+            lists.append((self.copies, "copies", torch.bfloat16))
+        self._tensors = (PnnAdamwTensor * count)()
+        written = set()
+        for i, p in enumerate(self.params):
+            n, t = p.numel(), self._tensors[i]
+            given = [(x[i], name, dtype, n) for x, name, dtype in lists]
+            if bits == 8:
+                given += [(self.state[2][i], "m's scales", torch.float32, -(-n // 256)), (self.state[3][i], "v's scales", torch.float32, -(-n // 256))]
+            for x, name, dtype, size in given:
+                if x is None and name == "copies":
+                    continue
+                if x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or x.device != first.device:
+                    raise ValueError(f"{name}[{i}] is {tuple(x.shape)} of {x.dtype} on {x.device}, expected {size} contiguous values of {dtype} "
+                                     f"on {first.device}")
+                if name != "grads" and size:
+                    at = x.data_ptr()
+                    if at in written:
+                        raise ValueError(f"{name}[{i}] stands twice among what a step writes")
+                    written.add(at)
+            t.p, t.g, t.m, t.v = (x[i].data_ptr() for x, _, _ in lists[:4])
+            t.copy = self.copies[i].data_ptr() if self.copies is not None and self.copies[i] is not None else None
+            if bits == 8:
+                t.m_scale, t.v_scale = self.state[2][i].data_ptr(), self.state[3][i].data_ptr()
+            t.n = n
+        _values(self.steps, "steps", (2,), torch.int32)
+        self._lr = lr if torch.is_tensor(lr) else None
+        if self._lr is not None:
+            _values(self._lr, "lr", (1,), torch.float32)
+        self.args = PnnAdamw(bits, _type_of(self.grads[0]), 0.0 if self._lr is not None else lr, betas[0], betas[1], eps, weight_decay,
+                             None if self._lr is None else self._lr.data_ptr(), seed & 0xFFFFFFFF, self.steps.data_ptr())
+
+    @property
+    def lr(self):
+        return self._lr if self._lr is not None else self.args.lr
+
+    @lr.setter
+    def lr(self, value: float):
+        if self._lr is not None:
+            raise ValueError("the rate is a tensor: write to it")
+        self.args.lr = value
+
+    def step(self, stream=None) -> None:
+        """One step with what the gradients hold now."""
+        used = ()
+        if stream is not None:  # (what a torch.cuda.Stream is to keep)
+            used = [t for ts in (self.params[1:], self.grads, self.copies or (), *self.state) for t in ts]
+        _on(stream, lambda s: _call("pnn_adamw_step", ctypes.byref(self.args), self._tensors, len(self.params), s), self.params[0],
+            *used, self.steps, self._lr)
+
+
+def adamw_values(m, v, m_scale, v_scale, stream=None):
+    """(m, v) in fp32, of the shape of 8-bit states and their scales (one for each 256 values)."""
+    torch = _t()
+    n = m.numel()
+    scales = (-(-n // 256),)
+
+    def body(s):
+        om, ov = _empty(m, m.shape, torch.float32), _empty(m, m.shape, torch.float32)
+        _call("pnn_adamw_values", _values(m, "m", m.shape, torch.uint8), _values(v, "v", m.shape, torch.uint8),
+              _values(m_scale, "m_scale", scales, torch.float32), _values(v_scale, "v_scale", scales, torch.float32), n, om.data_ptr(),
+              ov.data_ptr(), s)
+        return om, ov
+
+    return _on(stream, body, m, v, m_scale, v_scale)
 
 
 @functools.lru_cache(maxsize=1024)
