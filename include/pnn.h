@@ -430,7 +430,16 @@ typedef struct {
     int64_t n;                        /* 0..2^40 */
 } pnn_adamw_tensor;
 
+/* A plan of the tensors (host array, read during the call; values are contiguous and aligned to their types, no two
+ * tensors that a step writes overlap): where a step finds them, as long as they stay where they are.  All have `bits`
+ * and g_type.  plan_dev is 16-byte aligned; a program lays it out once. */
+pnn_status pnn_adamw_bytes(const pnn_adamw_tensor* tensors, int32_t count, int64_t* bytes, int64_t* chunks);
+pnn_status pnn_adamw_plan(const pnn_adamw_tensor* tensors, int32_t count, int32_t bits, int32_t g_type, void* plan_dev,
+                          int64_t plan_bytes, void* hip_stream);
+
 typedef struct {
+    void* plan_dev;       /* written by pnn_adamw_plan; a step counts its workgroups there */
+    int64_t chunks;       /* as pnn_adamw_bytes gives them */
     int32_t bits;         /* 32 or 8 */
     int32_t g_type;
     double lr;            /* 0..1e6 */
@@ -442,10 +451,9 @@ typedef struct {
     int32_t* steps_dev;   /* [2]: the steps done so far, and 0 (the library's own during a call) */
 } pnn_adamw;
 
-/* One step of `count` tensors (host array, read during the call; values are contiguous, no two tensors
- * overlap, aligned to their types).  Any number of launches, one for each 48 tensors.  Calls that share steps_dev are
- * ordered by the caller.  May be recorded into a graph. */
-pnn_status pnn_adamw_step(const pnn_adamw* args, const pnn_adamw_tensor* tensors, int32_t count, void* hip_stream);
+/* One step of all tensors of a plan, in one launch.  Calls that share tensors, a plan or steps_dev are ordered by the caller.  May
+ * be recorded into a graph. */
+pnn_status pnn_adamw_step(const pnn_adamw* args, void* hip_stream);
 
 /* What the 8-bit states of n values stand for, in fp32. */
 pnn_status pnn_adamw_values(const uint8_t* m_dev, const uint8_t* v_dev, const float* m_scale_dev, const float* v_scale_dev, int64_t n,

@@ -322,6 +322,8 @@ __device__ inline float group_act(int act, float z) {
 // global loads of gfx950 take any alignment, so odd widths and strides cost lines, not instructions.
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef u4v u4v_a2 __attribute__((aligned(2)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+typedef u2v u2v_a2 __attribute__((aligned(2)));
 typedef f4 f4_a4 __attribute__((aligned(4)));
 template <typename T> struct Raw8;
 template <> struct Raw8<bf16_t> { u4v v; };

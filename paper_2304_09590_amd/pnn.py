@@ -81,7 +81,8 @@ class PnnAdamwTensor(ctypes.Structure):
 
 
 class PnnAdamw(ctypes.Structure):
-    _fields_ = [("bits", ctypes.c_int32), ("g_type", ctypes.c_int32), ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
+    _fields_ = [("plan", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("bits", ctypes.c_int32), ("g_type", ctypes.c_int32),
+                ("lr", ctypes.c_double), ("beta1", ctypes.c_double),
                 ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("lr_dev", ctypes.c_void_p),
                 ("seed", ctypes.c_uint32), ("steps", ctypes.c_void_p)]
 
@@ -164,8 +165,11 @@ def lib() -> ctypes.CDLL:
         L.pnn_combine_grad.argtypes = [combine, vp, i64, i32, vp, i64, vp, vp]
         for name in ("pnn_route_bytes", "pnn_route", "pnn_route_grad", "pnn_combine_rows", "pnn_combine_grad"):
             getattr(L, name).restype = i32
-        L.pnn_adamw_step.argtypes = [P(PnnAdamw), P(PnnAdamwTensor), i32, vp]
-        L.pnn_adamw_step.restype = i32
+        L.pnn_adamw_bytes.argtypes = [P(PnnAdamwTensor), i32, P(i64), P(i64)]
+        L.pnn_adamw_plan.argtypes = [P(PnnAdamwTensor), i32, i32, i32, vp, i64, vp]
+        L.pnn_adamw_step.argtypes = [P(PnnAdamw), vp]
+        for name in ("pnn_adamw_bytes", "pnn_adamw_plan", "pnn_adamw_step"):
+            getattr(L, name).restype = i32
         L.pnn_adamw_values.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp]
         L.pnn_adamw_values.restype = i32
         distill = P(PnnDistill)
@@ -777,39 +781,51 @@ class AdamW:
         if len(self.state) != (2 if bits == 32 else 4) or any(len(s) != count for s in self.state):
             raise ValueError("state: lists of m and v, with 8 bits of their scales too, one for each parameter")
         self.steps = steps if steps is not None else torch.zeros(2, dtype=torch.int32, device=first.device)
-        g_type = self.grads[0].dtype
-        lists = [(self.params, "params", torch.float32), (self.grads, "grads", g_type), (self.state[0], "m", held), (self.state[1], "v", held)]
+        kind = _type_of(self.grads[0])
+        sizes = [p.numel() for p in self.params]
+        scales = [-(-n // 256) for n in sizes]
+        dev = first.get_device()
+        table = np.zeros((count, len(PnnAdamwTensor._fields_)), dtype=np.int64)  # (an entry's fields are 8 bytes each)
+        table[:, 7] = sizes
+        written, lengths = [], []
+        columns = [(0, "params", self.params, torch.float32, sizes), (1, "grads", self.grads, self.grads[0].dtype, sizes),
+                   (2, "m", self.state[0], held, sizes), (3, "v", self.state[1], held, sizes)]
+        if bits == 8:
+            columns += [(4, "m's scales", self.state[2], torch.float32, scales), (5, "v's scales", self.state[3], torch.float32, scales)]
         if self.copies is not None:
-            lists.append((self.copies, "copies", torch.bfloat16))
-        self._tensors = (PnnAdamwTensor * count)()
-        written = set()
-        for i, p in enumerate(self.params):
-            n, t = p.numel(), self._tensors[i]
-            given = [(x[i], name, dtype, n) for x, name, dtype in lists]
-            if bits == 8:
-                given += [(self.state[2][i], "m's scales", torch.float32, -(-n // 256)), (self.state[3][i], "v's scales", torch.float32, -(-n // 256))]
-            for x, name, dtype, size in given:
-                if x is None and name == "copies":
+            columns.append((6, "copies", self.copies, torch.bfloat16, sizes))
+        for field, name, column, dtype, expected in columns:
+            for i, (x, n) in enumerate(zip(column, expected)):
+                if x is None and field == 6:
                     continue
-                if x.dtype is not dtype or x.numel() != size or not x.is_contiguous() or x.device != first.device:
-                    raise ValueError(f"{name}[{i}] is {tuple(x.shape)} of {x.dtype} on {x.device}, expected {size} contiguous values of {dtype} "
+                if x.dtype is not dtype or x.numel() != n or not x.is_contiguous() or x.get_device() != dev:
+                    raise ValueError(f"{name}[{i}] is {tuple(x.shape)} of {x.dtype} on {x.device}, expected {n} contiguous values of {dtype} "
                                      f"on {first.device}")
-                if name != "grads" and size:
-                    at = x.data_ptr()
-                    if at in written:
-                        raise ValueError(f"{name}[{i}] stands twice among what a step writes")
-                    written.add(at)
-            t.p, t.g, t.m, t.v = (x[i].data_ptr() for x, _, _ in lists[:4])
-            t.copy = self.copies[i].data_ptr() if self.copies is not None and self.copies[i] is not None else None
-            if bits == 8:
-                t.m_scale, t.v_scale = self.state[2][i].data_ptr(), self.state[3][i].data_ptr()
-            t.n = n
+            table[:, field] = [0 if x is None else x.data_ptr() for x in column]
+            if field != 1:
+                written.append(table[:, field])
+                lengths.append(np.where(table[:, field] != 0, np.asarray(expected) * dtype.itemsize, 0))
+        written, lengths = np.concatenate(written), np.concatenate(lengths)
+        order = np.argsort(written[lengths > 0])
+        written, lengths = written[lengths > 0][order], lengths[lengths > 0][order]
+        if (written[1:] < written[:-1] + lengths[:-1]).any():
+            raise ValueError("two of the tensors that a step writes overlap")
+        tensors = table.ctypes.data_as(ctypes.POINTER(PnnAdamwTensor))
         _values(self.steps, "steps", (2,), torch.int32)
         self._lr = lr if torch.is_tensor(lr) else None
         if self._lr is not None:
             _values(self._lr, "lr", (1,), torch.float32)
-        self.args = PnnAdamw(bits, _type_of(self.grads[0]), 0.0 if self._lr is not None else lr, betas[0], betas[1], eps, weight_decay,
-                             None if self._lr is None else self._lr.data_ptr(), seed & 0xFFFFFFFF, self.steps.data_ptr())
+
+        def body(h):
+            size, chunks = ctypes.c_int64(), ctypes.c_int64()
+            _call("pnn_adamw_bytes", tensors, count, ctypes.byref(size), ctypes.byref(chunks))
+            plan = _empty(first, size.value, torch.uint8)
+            _call("pnn_adamw_plan", tensors, count, bits, kind, plan.data_ptr(), size.value, h)
+            return plan, chunks.value
+
+        self._plan, chunks = _on(None, body, first, self.steps, self._lr)
+        self.args = PnnAdamw(self._plan.data_ptr(), chunks, bits, kind, 0.0 if self._lr is not None else lr, betas[0], betas[1], eps,
+                             weight_decay, None if self._lr is None else self._lr.data_ptr(), seed & 0xFFFFFFFF, self.steps.data_ptr())
 
     @property
     def lr(self):
@@ -825,9 +841,8 @@ class AdamW:
         """One step with what the gradients hold now."""
         used = ()
         if stream is not None:  # (what a torch.cuda.Stream is to keep)
-            used = [t for ts in (self.params[1:], self.grads, self.copies or (), *self.state) for t in ts]
-        _on(stream, lambda s: _call("pnn_adamw_step", ctypes.byref(self.args), self._tensors, len(self.params), s), self.params[0],
-            *used, self.steps, self._lr)
+            used = [t for ts in (self.params, self.grads, self.copies or (), *self.state) for t in ts]
+        _on(stream, lambda s: _call("pnn_adamw_step", ctypes.byref(self.args), s), self.steps, *used, self._plan, self._lr)
 
 
 def adamw_values(m, v, m_scale, v_scale, stream=None):

@@ -16,37 +16,49 @@ FAKE = 1 << 20
 
 # ---- refusals, on the host -----------------------------------------------------------------------
 
-ARGS = dict(bits=32, g_type=pnn.FP32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, lr_dev=None, seed=0, steps=FAKE)
+ARGS = dict(plan=FAKE, chunks=1, bits=32, g_type=pnn.FP32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, lr_dev=None,
+            seed=0, steps=FAKE)
 TENSOR = dict(p=FAKE, g=FAKE, m=FAKE, v=FAKE, m_scale=None, v_scale=None, copy=None, n=10)
-BAD = [("args", d, pnn.PNN_EINVAL) for d in (
-    dict(bits=16), dict(g_type=2), dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
-    dict(beta2=math.nan), dict(beta2=1 - 1e-12), dict(eps=0.0), dict(eps=2.0), dict(eps=math.nan), dict(weight_decay=-1.0),
-    dict(weight_decay=math.inf), dict(lr_dev=FAKE + 2), dict(steps=None), dict(steps=FAKE + 1))] + [
-    ("tensor", dict(n=-1), pnn.PNN_ESHAPE), ("tensor", dict(n=(1 << 40) + 1), pnn.PNN_ESHAPE)] + [("tensor", d, pnn.PNN_EINVAL) for d in (
-        dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(p=FAKE + 2), dict(g=FAKE + 2), dict(m=FAKE + 1), dict(v=FAKE + 2),
-        dict(copy=FAKE + 1))]
 
 
-def call(args=ARGS, tensors=(TENSOR,), count=None):
-    a = pnn.PnnAdamw(*args.values())
+def planned(tensors=(TENSOR,), count=None, bits=32, g_type=pnn.FP32, plan=FAKE, size=1 << 20):
     t = (pnn.PnnAdamwTensor * max(1, len(tensors)))(*(pnn.PnnAdamwTensor(*d.values()) for d in tensors))
-    return pnn.lib().pnn_adamw_step(ctypes.byref(a), t, len(tensors) if count is None else count, None)
+    return pnn.lib().pnn_adamw_plan(t, len(tensors) if count is None else count, bits, g_type, plan, size, None)
 
 
-@pytest.mark.parametrize("which,over,status", BAD)
-def test_arguments_are_refused(which, over, status):
-    # (the second tensor: nothing is launched for the first)
-    assert call({**ARGS, **over} if which == "args" else ARGS, (TENSOR, {**TENSOR, **(over if which == "tensor" else {})})) == status
+@pytest.mark.parametrize("over", [
+    dict(plan=None), dict(plan=FAKE + 8), dict(chunks=-1), dict(chunks=1 << 31), dict(bits=16), dict(g_type=2), dict(lr=-1.0), dict(lr=math.nan),
+    dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan), dict(beta2=1 - 1e-12), dict(eps=0.0),
+    dict(eps=2.0), dict(eps=math.nan), dict(weight_decay=-1.0), dict(weight_decay=math.inf), dict(lr_dev=FAKE + 2), dict(steps=None),
+    dict(steps=FAKE + 1)])
+def test_steps_are_refused(over):
+    a = pnn.PnnAdamw(*{**ARGS, **over}.values())
+    assert pnn.lib().pnn_adamw_step(ctypes.byref(a), None) == pnn.PNN_EINVAL
+    assert pnn.lib().pnn_last_error(None)
+
+
+@pytest.mark.parametrize("over,status", [(dict(n=-1), pnn.PNN_ESHAPE), (dict(n=(1 << 40) + 1), pnn.PNN_ESHAPE)] + [
+    (d, pnn.PNN_EINVAL) for d in (
+        dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(p=FAKE + 2), dict(g=FAKE + 2), dict(m=FAKE + 1), dict(v=FAKE + 2),
+        dict(copy=FAKE + 1))])
+def test_tensors_are_refused(over, status):
+    assert planned((TENSOR, {**TENSOR, **over})) == status
     assert pnn.lib().pnn_last_error(None)
 
 
 def test_memory_is_refused():
-    L = pnn.lib()
-    assert L.pnn_adamw_step(None, None, 0, None) == pnn.PNN_EINVAL
-    assert call(count=-1) == pnn.PNN_ESHAPE
-    assert L.pnn_adamw_step(ctypes.byref(pnn.PnnAdamw(*ARGS.values())), None, 1, None) == pnn.PNN_EINVAL
+    L, size, chunks = pnn.lib(), ctypes.c_int64(), ctypes.c_int64()
+    assert L.pnn_adamw_step(None, None) == pnn.PNN_EINVAL
+    assert planned(count=-1) == pnn.PNN_ESHAPE and planned(bits=16) == planned(g_type=2) == pnn.PNN_EINVAL
+    assert planned(plan=None) == planned(plan=FAKE + 8) == pnn.PNN_EINVAL and planned(size=16) == pnn.PNN_ESHAPE
+    assert L.pnn_adamw_plan(None, 1, 32, 0, FAKE, 1 << 20, None) == pnn.PNN_EINVAL
+    assert planned(({**TENSOR, "n": 0, "p": None},), plan=None) == planned((), plan=None) == pnn.PNN_OK
+    assert planned(({**TENSOR, "n": 1 << 40},) * 16) == pnn.PNN_ESHAPE
+    t = (pnn.PnnAdamwTensor * 2)(*(pnn.PnnAdamwTensor(*{**TENSOR, "n": n}.values()) for n in (4097, 1)))
+    assert L.pnn_adamw_bytes(t, 2, ctypes.byref(size), ctypes.byref(chunks)) == pnn.PNN_OK and chunks.value == 3 and size.value >= 3 * 56
+    assert L.pnn_adamw_bytes(t, 2, None, ctypes.byref(chunks)) == L.pnn_adamw_bytes(t, 2, ctypes.byref(size), None) == pnn.PNN_EINVAL
     for over in (dict(), dict(m_scale=FAKE), dict(m_scale=FAKE + 2, v_scale=FAKE), dict(m_scale=FAKE, v_scale=FAKE + 2)):
-        assert call({**ARGS, "bits": 8}, ({**TENSOR, **over},)) == pnn.PNN_EINVAL
+        assert planned(({**TENSOR, **over},), bits=8) == pnn.PNN_EINVAL
     good = [FAKE, FAKE, FAKE, FAKE, 10, FAKE, FAKE]
     for i, value, status in [(i, None, pnn.PNN_EINVAL) for i in (0, 1, 2, 3, 5, 6)] + [(i, FAKE + 2, pnn.PNN_EINVAL) for i in (2, 3, 5, 6)] + [
             (4, -1, pnn.PNN_ESHAPE), (4, (1 << 40) + 1, pnn.PNN_ESHAPE), (4, 0, pnn.PNN_OK)]:
@@ -68,15 +80,13 @@ def test_the_binding_refuses():
         with pytest.raises(ValueError, match=why):
             pnn.AdamW(*a, **kw)
     one = p(5)
-    with pytest.raises(ValueError, match="twice"):
-        pnn.AdamW([one, one], [p(5), p(5)])
-    with pytest.raises(ValueError, match="twice"):
-        pnn.AdamW([one], [p(5)], state=[[one], [p(5)]])
+    for a, kw in (([one, one], {}), ([one[:3], one[2:]], {}), ([one], dict(state=[[one], [p(5)]])), ([one[:2]], dict(copies=[one.view(BF16)[3:5]]))):
+        with pytest.raises(ValueError, match="overlap"):
+            pnn.AdamW(a, [torch.zeros_like(x) for x in a], **kw)
     with pytest.raises(ValueError, match="CUDA"):
-        pnn.AdamW([p(3)], [p(3)]).step()
-    fixed = pnn.AdamW([p(3)], [p(3)], lr=torch.ones(1))
-    with pytest.raises(ValueError, match="tensor"):
-        fixed.lr = 0.1
+        pnn.AdamW([one[:2], one[2:], one[5:]], [p(2), p(3), p(0)])
+    with pytest.raises(ValueError, match="CUDA"):
+        pnn.AdamW([p(3)], [p(3)])
     with pytest.raises(ValueError, match="m is"):
         pnn.adamw_values(p(3), p(3), p(1), p(1)) if torch.cuda.is_available() else pnn._values(p(3), "m", (3,), torch.uint8)
 
@@ -361,6 +371,9 @@ def test_a_graph_another_stream_and_resumed_training(bits):
             assert same(eager, again)
         for x in g:
             x.mul_(-0.75)
+    assert other.lr is rate
+    with pytest.raises(ValueError, match="tensor"):
+        other.lr = 0.1
 
 
 @gpu
