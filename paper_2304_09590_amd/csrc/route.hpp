@@ -16,8 +16,9 @@
 namespace pnn {
 
 constexpr int RT_MAX_TOP = 64;       // most networks of a row
-constexpr int RT_THREADS = 512;      // threads of a workgroup that routes
+constexpr int RT_THREADS = 1024;     // threads of a workgroup that routes
 constexpr int RT_MAX_BLOCKS = 256;   // most workgroups whose sums are joined
+constexpr int RT_JOIN = 16;          // networks that a workgroup joins
 
 struct RouteArgs {
     const void* s;
@@ -30,6 +31,8 @@ struct RouteArgs {
     float* loss;
     float* part;              // [blocks][K] sums of p
     int32_t* part_counts;     // [blocks][K + 1]
+    float* dots;              // [workgroups that join] sums of counts times sums of p, then their pairs
+    int32_t* arrived;         // workgroups that have joined
     int blocks;
     // gradient
     const float *dgates, *dloss;
@@ -51,8 +54,6 @@ struct RouteLane {
 template <typename T, int L, int V>
 __device__ inline void route_load(float (&x)[V], const T* s, int K, int l) {
     typedef RouteLane<L, V> At;
-    typedef uint32_t u2v __attribute__((ext_vector_type(2)));
-    typedef u2v u2v_a2 __attribute__((aligned(2)));
 #pragma unroll
     for (int v = 0; v < V; v += At::CH) {
         const int c = At::column(l, v);
@@ -73,29 +74,34 @@ __device__ inline void route_load(float (&x)[V], const T* s, int K, int l) {
     }
 }
 
-template <int L> __device__ inline float route_max(float v) {
-    v = row_allmax16(v);
+template <int CTRL, typename T> __device__ inline T route_dpp(T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// over the L lanes of a row: 16 by DPP, their four rows by exchanges of halves
+template <int L, typename T, typename F>
+__device__ inline T route_reduce(T v, F f) {
+    v = f(v, route_dpp<DPP_ROW_MIRROR>(v));
+    v = f(v, route_dpp<DPP_ROW_HALF_MIRROR>(v));
+    v = f(v, route_dpp<DPP_XOR2>(v));
+    v = f(v, route_dpp<DPP_XOR1>(v));
     if (L == 64) {
-        v = fmaxf(v, __shfl_xor(v, 16));
-        v = fmaxf(v, __shfl_xor(v, 32));
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        v = f(__builtin_bit_cast(T, (uint32_t)a[0]), __builtin_bit_cast(T, (uint32_t)a[1]));
+        const uint32_t w = __builtin_bit_cast(uint32_t, v);
+        const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        v = f(__builtin_bit_cast(T, (uint32_t)b[0]), __builtin_bit_cast(T, (uint32_t)b[1]));
     }
     return v;
+}
+template <int L> __device__ inline float route_max(float v) {
+    return route_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 template <int L> __device__ inline float route_sum(float v) {
-    v = row_allsum16(v);
-    if (L == 64) {
-        v += __shfl_xor(v, 16);
-        v += __shfl_xor(v, 32);
-    }
-    return v;
+    return route_reduce<L>(v, [](float a, float b) { return a + b; });
 }
 template <int L> __device__ inline int route_min(int v) {
-#pragma unroll
-    for (int d = 1; d < L; d <<= 1) {
-        const int u = __shfl_xor(v, d);
-        v = u < v ? u : v;
-    }
-    return v;
+    return route_reduce<L>(v, [](int a, int b) { return a < b ? a : b; });
 }
 
 // e = exp(x - max) of a row; 1 / sum: 0 for a row of -inf, NaN for one with a NaN or an infinity
@@ -116,13 +122,23 @@ __device__ inline void route_softmax(const float (&x)[V], float (&e)[V], float& 
     inv = s == 0.0f ? 0.0f : 1.0f / s;
 }
 
+// the counts and the loss of all networks: a workgroup's share of dot = sum counts_e sum p_e
+__device__ inline float route_loss(float dot, int pairs, int rows, int K) {
+    // (without a row to count the loss is 0, or NaN where a row held one)
+    return dot * ((float)K / ((float)(pairs > 0 ? pairs : 1) * (float)(rows > 0 ? rows : 1)));
+}
+
+// Choosing is k times the largest of the row's lanes' largest (the lowest index on ties).  The lane that held it then
+// needs its next: its V scores lie in LDS, where 16 lanes look at one each, so a choice costs the same whatever V is.
+// (Looking through all lanes' scores again, 16,384 rows of 1,000 scores in bf16, eight each, took 59 us.)
 template <typename T, int L, int V>
 __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
-    constexpr int WAVES = RT_THREADS / 64, ROWS = 64 / L, KEEP = RT_MAX_TOP / L;
+    constexpr int WAVES = RT_THREADS / 64, ROWS = 64 / L, KEEP = RT_MAX_TOP / L, LD = V == 1 ? 1 : V + 4;
     __shared__ int cnt[GR_MAX_NETS + 1];
-    __shared__ float sums[WAVES][L * V];
+    __shared__ __align__(16) float lds[RT_THREADS * LD];  // (LD of each lane; afterwards the waves' sums)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane % L, sub = lane / L;
+    float *mine = lds + tid * LD, *row0 = lds + (tid - l) * LD;  // this lane's scores, and the row's first lane's
     if (a.counts) {
         for (int e = tid; e <= a.K; e += RT_THREADS) cnt[e] = 0;
         __syncthreads();
@@ -137,6 +153,20 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
         const int64_t r = in ? r0 + sub : a.n - 1;
         float x[V], e[V], top, inv;
         route_load<T, L, V>(x, (const T*)a.s + r * a.lds, a.K, l);
+        // the lane's largest and its column
+        float best = x[0];
+        int at = At::column(l, 0);
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (x[v] > best) {
+                best = x[v];
+                at = At::column(l, v);
+            }
+        if (V > 1) {
+#pragma unroll
+            for (int v = 0; v < V; v += 4) *(f4*)(mine + v) = f4{x[v], x[(v + 1) % V], x[(v + 2) % V], x[(v + 3) % V]};
+            __builtin_amdgcn_wave_barrier();
+        }
         route_softmax<L, V>(x, e, top, inv);
         const bool bad = inv != inv, has = inv > 0.0f;
         if (a.counts && in) {
@@ -151,25 +181,31 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
             id[q] = -1;
             ge[q] = 0.0f;
             for (int j = 0; j < L && q * L + j < a.k; ++j) {
-                float best = x[0];
-                int at = At::column(l, 0);
-#pragma unroll
-                for (int v = 1; v < V; ++v)
-                    if (x[v] > best) {
-                        best = x[v];
-                        at = At::column(l, v);
-                    }
                 const float m = route_max<L>(best);
                 const int c = route_min<L>(best == m ? at : INT32_MAX);
-                if (m == -RT_INF || !has) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (At::column(l, v) == c) x[v] = -RT_INF;
-                const float g = __builtin_amdgcn_exp2f((m - top) * RT_LOG2E);
+                const bool some = has && m > -RT_INF;
+                const float g = some ? __builtin_amdgcn_exp2f((m - top) * RT_LOG2E) : 0.0f;
                 chosen += g;
                 if (l == j) {
-                    id[q] = c;
+                    id[q] = some ? c : -1;
                     ge[q] = g;
+                }
+                if (q * L + j + 1 == a.k) break;
+                if (V == 1) {
+                    if (l == c) best = -RT_INF;
+                    continue;
+                }
+                // the lane that held it looks for its next (a row that holds no number finds nothing: any lane will do)
+                const int of = some ? c : 0, o = of / At::CH % L, i = lane & 15;
+                float w = i < V ? row0[o * LD + i] : -RT_INF;
+                const int col = At::column(o, i < V ? i : 0);
+                if (col == of || w != w) w = -RT_INF;
+                if (l < 16 && i < V && col == of) row0[o * LD + i] = -RT_INF;
+                const float next = route_max<16>(w);
+                const int next_at = route_min<16>(i < V && w == next ? col : INT32_MAX);
+                if (l == o) {
+                    best = next;
+                    at = next_at;
                 }
             }
         }
@@ -179,7 +215,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
             for (int q = 0; q < KEEP; ++q)
                 if (q * L + l < a.k) {
                     a.ids[r * a.k + q * L + l] = id[q];
-                    a.gates[r * a.k + q * L + l] = id[q] < 0 && !bad ? 0.0f : bad ? by : ge[q] * by;
+                    a.gates[r * a.k + q * L + l] = bad ? by : ge[q] * by;
                     if (a.counts && id[q] >= 0) atomicAdd(&cnt[id[q]], 1);
                 }
         }
@@ -190,76 +226,151 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     for (int v = 0; v < V; ++v) {
 #pragma unroll
         for (int d = L; d < 64; d <<= 1) acc[v] += __shfl_xor(acc[v], d);
-        if (sub == 0) sums[wave][At::column(l, v)] = acc[v];
     }
     __syncthreads();
-    for (int e = tid; e < a.K; e += RT_THREADS) {
-        float s = sums[0][e];
+    float* sums = lds;  // [waves][L * V]
+    if (sub == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += sums[w][e];
-        a.part[(int64_t)blockIdx.x * a.K + e] = s;
+        for (int v = 0; v < V; ++v) sums[wave * L * V + At::column(l, v)] = acc[v];
     }
-    for (int e = tid; e <= a.K; e += RT_THREADS) a.part_counts[(int64_t)blockIdx.x * (a.K + 1) + e] = cnt[e];
-}
-
-// counts and loss from the workgroups' sums, in their order
-__global__ __launch_bounds__(1024) void route_join_kernel(RouteArgs a) {
-    __shared__ float red[16];
-    __shared__ int total[16], rows_of[1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __syncthreads();
+    const bool alone = gridDim.x == 1;
     float dot = 0.0f;
-    int all = 0;
-    for (int e = tid; e <= a.K; e += 1024) {
-        int c = 0;
-        float s = 0.0f;
-        for (int b = 0; b < a.blocks; ++b) {
-            c += a.part_counts[(int64_t)b * (a.K + 1) + e];
-            if (e < a.K) s += a.part[(int64_t)b * a.K + e];
-        }
-        a.counts[e] = c;
-        if (e == a.K) {
-            rows_of[0] = c;
-        } else {
-            all += c;
-            dot += (float)c * s;
-        }
-    }
+    int pairs = 0;
+    for (int e = tid; e <= a.K; e += RT_THREADS) {
+        float s = e < a.K ? sums[e] : 0.0f;
+        if (e < a.K) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        dot += __shfl_xor(dot, d);
-        all += __shfl_xor(all, d);
+            for (int w = 1; w < WAVES; ++w) s += sums[w * L * V + e];
+        }
+        if (alone) {
+            a.counts[e] = cnt[e];
+            if (e < a.K) {
+                dot += (float)cnt[e] * s;
+                pairs += cnt[e];
+            }
+        } else {
+            a.part_counts[(int64_t)blockIdx.x * (a.K + 1) + e] = cnt[e];
+            if (e < a.K) a.part[(int64_t)blockIdx.x * a.K + e] = s;
+        }
     }
+    if (!alone) {
+        if (blockIdx.x == 0 && tid == 0) *a.arrived = 0;
+        return;
+    }
+    __syncthreads();
+    dot = route_sum<64>(dot);
+    pairs = route_reduce<64>(pairs, [](int x, int y) { return x + y; });
     if (lane == 0) {
-        red[wave] = dot;
-        total[wave] = all;
+        lds[wave] = dot;
+        lds[WAVES + wave] = __int_as_float(pairs);
     }
     __syncthreads();
     if (tid == 0) {
-        for (int w = 1; w < 16; ++w) {
-            dot += red[w];
-            all += total[w];
+        for (int w = 1; w < WAVES; ++w) {
+            dot += lds[w];
+            pairs += __float_as_int(lds[WAVES + w]);
         }
-        const int rows = rows_of[0];
-        // (without a row to count the loss is 0, or NaN where a row held one)
-        a.loss[0] = dot * ((float)a.K / ((float)(all > 0 ? all : 1) * (float)(rows > 0 ? rows : 1)));
+        a.loss[0] = route_loss(dot, pairs, cnt[a.K], a.K);
     }
 }
 
+// Counts and loss from the workgroups' sums, in their order: 16 networks a workgroup, 16 threads each; the last
+// workgroup to come adds up what all have written.
+__global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
+    __shared__ float sums[16][RT_JOIN];
+    __shared__ int counts[16][RT_JOIN];
+    __shared__ bool last;
+    const int tid = threadIdx.x, x = tid % RT_JOIN, y = tid / RT_JOIN, e = (int)blockIdx.x * RT_JOIN + x;
+    int c[RT_MAX_BLOCKS / 16];
+    float s[RT_MAX_BLOCKS / 16];
+#pragma unroll
+    for (int i = 0; i < RT_MAX_BLOCKS / 16; ++i) {
+        const int b = y * (RT_MAX_BLOCKS / 16) + i;
+        c[i] = e <= a.K && b < a.blocks ? a.part_counts[(int64_t)b * (a.K + 1) + e] : 0;
+        s[i] = e < a.K && b < a.blocks ? a.part[(int64_t)b * a.K + e] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 1; i < RT_MAX_BLOCKS / 16; ++i) {
+        c[0] += c[i];
+        s[0] += s[i];
+    }
+    sums[y][x] = s[0];
+    counts[y][x] = c[0];
+    __syncthreads();
+    if (tid < 64) {  // (lanes from RT_JOIN on add nothing)
+        int all = 0;
+        float p = 0.0f;
+        if (tid < RT_JOIN) {
+            for (int i = 0; i < 16; ++i) {
+                all += counts[i][tid];
+                p += sums[i][tid];
+            }
+            if (e <= a.K) a.counts[e] = all;
+        }
+        const bool network = tid < RT_JOIN && e < a.K;
+        const float dot = route_sum<16>(network ? (float)all * p : 0.0f);
+        const int pairs = route_reduce<16>(network ? all : 0, [](int x, int y) { return x + y; });
+        if (tid == 0) {
+            a.dots[2 * blockIdx.x] = dot;
+            a.dots[2 * blockIdx.x + 1] = __int_as_float(pairs);
+        }
+        // (counts[K], the number of rows, is one of the networks' places of the last workgroup)
+        __threadfence();
+        if (tid == 0) last = atomicAdd(a.arrived, 1) == (int)gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last || tid >= 64) return;
+    __threadfence();
+    float dot = 0.0f;
+    int pairs = 0;
+    for (int w = tid; w < (int)gridDim.x; w += 64) {
+        dot += __hip_atomic_load(a.dots + 2 * w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        pairs += __float_as_int(__hip_atomic_load(a.dots + 2 * w + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    }
+    dot = route_sum<64>(dot);
+    pairs = route_reduce<64>(pairs, [](int x, int y) { return x + y; });
+    if (tid == 0) a.loss[0] = route_loss(dot, pairs, __hip_atomic_load(a.counts + a.K, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), a.K);
+}
+
+// four neighbouring values, the first nv of them
+__device__ inline void route_store4(float* p, const float* v, int nv) {
+    if (nv >= 4) {
+        *(f4_a4*)p = f4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < nv) p[i] = v[i];
+    }
+}
+__device__ inline void route_store4(bf16_t* p, const float* v, int nv) {
+    if (nv >= 4) {
+        *(u2v_a2*)p = u2v{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < nv) p[i] = f2bf(v[i]);
+    }
+}
+
+// What the gates add lies in LDS, a place for each score of the row: the lanes that hold the choices add theirs there.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
-    constexpr int WAVES = 4, ROWS = 64 / L, KEEP = RT_MAX_TOP / L;
+    constexpr int WAVES = 4, ROWS = 64 / L, KEEP = RT_MAX_TOP / L, LD = V == 1 ? 1 : V + 4;
+    __shared__ __align__(16) float lds[256 * LD];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane % L, sub = lane / L;
+    float *mine = lds + tid * LD, *row0 = lds + (tid - l) * LD;
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine[v] = 0.0f;
     float w[V];  // a_e
 #pragma unroll
     for (int v = 0; v < V; ++v) w[v] = 0.0f;
     if (a.dloss) {
         int all = 0;
         for (int e = lane; e < a.K; e += 64) all += a.counts[e];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor(all, d);
-        const int rows = a.counts[a.K];
-        const float by = a.dloss[0] * ((float)a.K / ((float)(all > 0 ? all : 1) * (float)(rows > 0 ? rows : 1)));
+        all = route_reduce<64>(all, [](int x, int y) { return x + y; });
+        const float by = a.dloss[0] * route_loss(1.0f, all, a.counts[a.K], a.K);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = At::column(l, v);
@@ -270,6 +381,22 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     for (int64_t r0 = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; r0 < a.n; r0 += step) {
         const bool in = r0 + sub < a.n;
         const int64_t r = in ? r0 + sub : a.n - 1;
+        int id[KEEP];
+        float gate[KEEP], dg[KEEP], chosen = 0.0f, mix = 0.0f;
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) {
+            id[q] = -1;
+            gate[q] = -RT_INF;
+            dg[q] = 0.0f;
+            if (a.dgates && q * L + l < a.k) {
+                const int i = a.ids[r * a.k + q * L + l];
+                if ((unsigned)i < (unsigned)a.K) {
+                    id[q] = i;
+                    gate[q] = to_f<T>(((const T*)a.s)[r * a.lds + i]);
+                    dg[q] = a.dgates[r * a.k + q * L + l];
+                }
+            }
+        }
         float x[V], p[V], top, inv;
         route_load<T, L, V>(x, (const T*)a.s + r * a.lds, a.K, l);
         route_softmax<L, V>(x, p, top, inv);
@@ -280,24 +407,13 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
             dot += p[v] * w[v];
         }
         dot = route_sum<L>(dot);
-        int id[KEEP];
-        float gate[KEEP], dg[KEEP], chosen = 0.0f, mix = 0.0f;
         if (a.dgates) {
 #pragma unroll
             for (int q = 0; q < KEEP; ++q) {
-                id[q] = -1;
-                gate[q] = dg[q] = 0.0f;
-                if (q * L + l < a.k) {
-                    const int i = a.ids[r * a.k + q * L + l];
-                    if ((unsigned)i < (unsigned)a.K) {
-                        id[q] = i;
-                        gate[q] = __builtin_amdgcn_exp2f((to_f<T>(((const T*)a.s)[r * a.lds + i]) - top) * RT_LOG2E);
-                        dg[q] = a.dgates[r * a.k + q * L + l];
-                        chosen += gate[q];
-                    }
-                }
+                gate[q] = __builtin_amdgcn_exp2f((gate[q] - top) * RT_LOG2E);
+                if (id[q] >= 0) chosen += gate[q];
             }
-            chosen = a.normalize ? route_sum<L>(chosen) : 0.0f;
+            if (a.normalize) chosen = route_sum<L>(chosen);
             const float by = a.normalize ? (chosen != 0.0f ? 1.0f / chosen : 0.0f) : inv;
 #pragma unroll
             for (int q = 0; q < KEEP; ++q) {
@@ -305,30 +421,35 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
                 if (id[q] >= 0) mix += gate[q] * dg[q];
             }
             mix = route_sum<L>(mix);
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q)
+                if (id[q] >= 0) {
+                    const int c = id[q];
+                    atomicAdd(row0 + c / At::CH % L * LD + c / (At::CH * L) * At::CH + c % At::CH,
+                              gate[q] * (a.normalize ? dg[q] - mix : dg[q]));
+                }
+            __builtin_amdgcn_wave_barrier();
         }
         const float off = a.normalize ? dot : dot + mix;
         float d[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) d[v] = p[v] * (w[v] - off);
+        for (int v = 0; v < V; ++v) {
+            d[v] = p[v] * (w[v] - off);
+            if (a.dgates) d[v] += mine[v];
+        }
         if (a.dgates) {
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int q = 0; q < KEEP; ++q) {
-                const float mine = gate[q] * (a.normalize ? dg[q] - mix : dg[q]);
-                for (int j = 0; j < L && q * L + j < a.k; ++j) {
-                    const int at = __shfl(id[q], sub * L + j);
-                    const float more = __shfl(mine, sub * L + j);
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        if (At::column(l, v) == at) d[v] += more;
-                }
-            }
+            for (int q = 0; q < KEEP; ++q)
+                if (id[q] >= 0) row0[id[q] / At::CH % L * LD + id[q] / (At::CH * L) * At::CH + id[q] % At::CH] = 0.0f;
         }
         if (!in) continue;
         T* out = (T*)a.ds + r * a.ldds;
+        if constexpr (V == 1) {
+            if (l < a.K) out[l] = from_f<T>(d[0]);
+        } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = At::column(l, v);
-            if (c < a.K) out[c] = from_f<T>(d[v]);
+            for (int v = 0; v < V; v += 4) route_store4(out + At::column(l, v), d + v, a.K - At::column(l, v));
         }
     }
 }

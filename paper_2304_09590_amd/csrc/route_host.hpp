@@ -81,7 +81,7 @@ extern "C" {
 pnn_status pnn_route_bytes(int64_t n, int32_t networks, int64_t* bytes) {
     TRY(check_route(n, networks));
     if (!bytes) return fail(nullptr, PNN_EINVAL, "bytes is NULL");
-    *bytes = 4 * round_up((int64_t)route_blocks(n, networks) * (2 * networks + 1), 4);
+    *bytes = 4 * (round_up((int64_t)route_blocks(n, networks) * (2 * networks + 1), 4) + 2 * (GR_MAX_NETS / RT_JOIN + 1) + 2);
     return PNN_OK;
 }
 
@@ -109,13 +109,15 @@ pnn_status pnn_route(const pnn_router* a, int32_t* ids_dev, float* gates_dev, in
     r.blocks = counts_dev ? route_blocks(a->n, a->networks) : (int)std::min<int64_t>((a->n + each - 1) / each, 4096);
     r.part = (float*)ws_dev;
     r.part_counts = (int32_t*)ws_dev + (int64_t)r.blocks * a->networks;
+    r.dots = (float*)ws_dev + round_up((int64_t)r.blocks * (2 * a->networks + 1), 4);
+    r.arrived = (int32_t*)r.dots + 2 * (GR_MAX_NETS / RT_JOIN + 1);
     route_by_width(a->networks, [&](auto L, auto V) {
         if (a->type == PNN_FP32) route_kernel<float, L(), V()><<<r.blocks, RT_THREADS, 0, s>>>(r);
         else route_kernel<bf16_t, L(), V()><<<r.blocks, RT_THREADS, 0, s>>>(r);
     });
     TRY(launched("routing"));
-    if (!counts_dev) return PNN_OK;
-    route_join_kernel<<<1, 1024, 0, s>>>(r);
+    if (!counts_dev || r.blocks == 1) return PNN_OK;  // (a workgroup that is alone has it all)
+    route_join_kernel<<<a->networks / RT_JOIN + 1, 256, 0, s>>>(r);
     return launched("the balance loss");
 }
 
@@ -135,7 +137,7 @@ pnn_status pnn_route_grad(const pnn_router* a, const int32_t* ids_dev, const int
     r.dgates = dgates_dev; r.dloss = dloss_dev;
     r.ds = ds_dev; r.ldds = ds_ld;
     const int64_t each = 4 * route_rows(a->networks);
-    const unsigned blocks = (unsigned)std::min<int64_t>((a->n + each - 1) / each, 4096);
+    const unsigned blocks = (unsigned)std::min<int64_t>((a->n + each - 1) / each, 2048);
     route_by_width(a->networks, [&](auto L, auto V) {
         if (a->type == PNN_FP32) route_grad_kernel<float, L(), V()><<<blocks, 256, 0, s>>>(r);
         else route_grad_kernel<bf16_t, L(), V()><<<blocks, 256, 0, s>>>(r);
