@@ -50,29 +50,46 @@ struct RouteLane {
     static __device__ inline int column(int l, int v) { return (v / CH * L + l) * CH + v % CH; }
 };
 
-// the scores of a row (-inf outside it)
+// the scores of a row as loaded (-inf outside it), and as fp32
 template <typename T, int L, int V>
-__device__ inline void route_load(float (&x)[V], const T* s, int K, int l) {
+struct RouteRaw {
     typedef RouteLane<L, V> At;
-#pragma unroll
-    for (int v = 0; v < V; v += At::CH) {
-        const int c = At::column(l, v);
-        if (At::CH == 4 && c + 4 <= K) {
-            if constexpr (sizeof(T) == 4) {
-                const f4 q = *(const f4_a4*)(s + c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[(v + i) % V] = q[i];
-            } else {
-                const u2v q = *(const u2v_a2*)(s + c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[(v + i) % V] = i & 1 ? bf_hi(q[i >> 1]) : bf_lo(q[i >> 1]);
-            }
+    typedef typename std::conditional<sizeof(T) == 4, f4, u2v>::type Four;
+    typedef typename std::conditional<sizeof(T) == 4, f4_a4, u2v_a2>::type Loose;
+    Four four[V == 1 ? 1 : V / 4];
+    T one;
+    __device__ inline void load(const T* s, int K, int l) {
+        const T none = from_f<T>(-RT_INF);
+        if constexpr (V == 1) {
+            one = l < K ? s[l] : none;
         } else {
 #pragma unroll
-            for (int i = 0; i < At::CH; ++i) x[v + i] = c + i < K ? to_f<T>(s[c + i]) : -RT_INF;
+            for (int h = 0; h < V / 4; ++h) {
+                const int c = At::column(l, 4 * h);
+                if (c + 4 <= K) {
+                    four[h] = *(const Loose*)(s + c);
+                } else {
+                    T t[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[i] = c + i < K ? s[c + i] : none;
+                    if constexpr (sizeof(T) == 4) four[h] = f4{t[0], t[1], t[2], t[3]};
+                    else four[h] = u2v{(uint32_t)t[0] | (uint32_t)t[1] << 16, (uint32_t)t[2] | (uint32_t)t[3] << 16};
+                }
+            }
         }
     }
-}
+    __device__ inline void get(float (&x)[V]) const {
+        if constexpr (V == 1) {
+            x[0] = to_f<T>(one);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (sizeof(T) == 4) x[v] = four[v / 4][v % 4];
+                else x[v] = v & 1 ? bf_hi(four[v / 4][v % 4 >> 1]) : bf_lo(four[v / 4][v % 4 >> 1]);
+            }
+        }
+    }
+};
 
 template <int CTRL, typename T> __device__ inline T route_dpp(T v) {
     return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
@@ -128,17 +145,39 @@ __device__ inline float route_loss(float dot, int pairs, int rows, int K) {
     return dot * ((float)K / ((float)(pairs > 0 ? pairs : 1) * (float)(rows > 0 ? rows : 1)));
 }
 
+// Scores as integers that are ordered alike (-0 as 0): of bf16 ones the low half is free, and holds the column so that
+// of equal scores the lowest index is the largest key.
+constexpr int RT_GONE = INT32_MIN;               // a score that was chosen
+constexpr int RT_NONE = (int)0x807fffffu;        // -inf, or anything below the smallest number
+template <typename T>
+__device__ inline int route_key(float x, int column) {
+    constexpr int MASK = sizeof(T) == 4 ? 0x7fffffff : 0x7fff0000;
+    const int b = __float_as_int(x + 0.0f), k = b ^ (b >> 31 & MASK);
+    return sizeof(T) == 4 ? k : k | (0xffff - column);
+}
+template <typename T>
+__device__ inline float route_value(int key) {
+    constexpr int MASK = sizeof(T) == 4 ? 0x7fffffff : 0x7fff0000;
+    const int k = sizeof(T) == 4 ? key : key & (int)0xffff0000;
+    return __int_as_float(k ^ (k >> 31 & MASK));
+}
+template <int L> __device__ inline int route_top(int v) {
+    return route_reduce<L>(v, [](int a, int b) { return a > b ? a : b; });
+}
+
 // Choosing is k times the largest of the row's lanes' largest (the lowest index on ties).  The lane that held it then
-// needs its next: its V scores lie in LDS, where 16 lanes look at one each, so a choice costs the same whatever V is.
-// (Looking through all lanes' scores again, 16,384 rows of 1,000 scores in bf16, eight each, took 59 us.)
+// needs its next: its V keys lie in LDS, where 16 lanes look at one each, so a choice costs the same whatever V is.
+// 16,384 rows of 1,000 scores in bf16, eight each: 59 us with all lanes' scores looked through again for each choice, 35
+// this way with scores and columns apart.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
+    constexpr bool APART = sizeof(T) == 4;  // columns apart from the keys
     constexpr int WAVES = RT_THREADS / 64, ROWS = 64 / L, KEEP = RT_MAX_TOP / L, LD = V == 1 ? 1 : V + 4;
     __shared__ int cnt[GR_MAX_NETS + 1];
-    __shared__ __align__(16) float lds[RT_THREADS * LD];  // (LD of each lane; afterwards the waves' sums)
+    __shared__ __align__(16) int lds[RT_THREADS * LD];  // (LD of each lane; afterwards the waves' sums)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane % L, sub = lane / L;
-    float *mine = lds + tid * LD, *row0 = lds + (tid - l) * LD;  // this lane's scores, and the row's first lane's
+    int *mine = lds + tid * LD, *row0 = lds + (tid - l) * LD;  // this lane's keys, and the row's first lane's
     if (a.counts) {
         for (int e = tid; e <= a.K; e += RT_THREADS) cnt[e] = 0;
         __syncthreads();
@@ -147,68 +186,81 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = 0.0f;
     const int64_t step = (int64_t)gridDim.x * WAVES * ROWS;
+    int64_t r0 = ((int64_t)blockIdx.x * WAVES + wave) * ROWS;
+    RouteRaw<T, L, V> raw;
+    auto load = [&](int64_t at) { raw.load((const T*)a.s + (at + sub < a.n ? at + sub : a.n - 1) * a.lds, a.K, l); };
+    if (r0 < a.n) load(r0);
     // (all lanes of a wave run every step: what they exchange needs all of them)
-    for (int64_t r0 = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; r0 < a.n; r0 += step) {
+    for (; r0 < a.n; r0 += step) {
         const bool in = r0 + sub < a.n;
         const int64_t r = in ? r0 + sub : a.n - 1;
         float x[V], e[V], top, inv;
-        route_load<T, L, V>(x, (const T*)a.s + r * a.lds, a.K, l);
-        // the lane's largest and its column
-        float best = x[0];
-        int at = At::column(l, 0);
+        raw.get(x);
+        int best = RT_GONE, at = 0;  // the lane's largest key, and its column
+        if (APART || V == 1) {
 #pragma unroll
-        for (int v = 1; v < V; ++v)
-            if (x[v] > best) {
-                best = x[v];
-                at = At::column(l, v);
+            for (int v = 0; v < V; ++v) {
+                const int k = route_key<T>(x[v], At::column(l, v));
+                if (V > 1) mine[v] = k;
+                if (APART && k > best) at = At::column(l, v);
+                best = k > best ? k : best;
             }
-        if (V > 1) {
+        } else {
 #pragma unroll
-            for (int v = 0; v < V; v += 4) *(f4*)(mine + v) = f4{x[v], x[(v + 1) % V], x[(v + 2) % V], x[(v + 3) % V]};
-            __builtin_amdgcn_wave_barrier();
+            for (int v = 0; v < V; ++v) {
+                const int k = route_key<T>(x[v], At::column(l, v));
+                mine[v] = k;
+                best = k > best ? k : best;
+            }
         }
+        __builtin_amdgcn_wave_barrier();
         route_softmax<L, V>(x, e, top, inv);
+        if (r0 + step < a.n) load(r0 + step);
         const bool bad = inv != inv, has = inv > 0.0f;
         if (a.counts && in) {
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] += e[v] * inv;
             if (l == 0 && has) atomicAdd(&cnt[a.K], 1);
         }
-        int id[KEEP];
-        float ge[KEEP], chosen = 0.0f;
+        int id[KEEP], key[KEEP];
 #pragma unroll
         for (int q = 0; q < KEEP; ++q) {
             id[q] = -1;
-            ge[q] = 0.0f;
+            key[q] = RT_NONE;
             for (int j = 0; j < L && q * L + j < a.k; ++j) {
-                const float m = route_max<L>(best);
-                const int c = route_min<L>(best == m ? at : INT32_MAX);
-                const bool some = has && m > -RT_INF;
-                const float g = some ? __builtin_amdgcn_exp2f((m - top) * RT_LOG2E) : 0.0f;
-                chosen += g;
+                const int m = route_top<L>(best);
+                const int c = APART ? route_min<L>(best == m ? at : INT32_MAX) : 0xffff - (m & 0xffff);
                 if (l == j) {
-                    id[q] = some ? c : -1;
-                    ge[q] = g;
+                    id[q] = has && m > RT_NONE ? c : -1;
+                    key[q] = m;
                 }
                 if (q * L + j + 1 == a.k) break;
                 if (V == 1) {
-                    if (l == c) best = -RT_INF;
+                    if (l == c) best = RT_GONE;
                     continue;
                 }
-                // the lane that held it looks for its next (a row that holds no number finds nothing: any lane will do)
-                const int of = some ? c : 0, o = of / At::CH % L, i = lane & 15;
-                float w = i < V ? row0[o * LD + i] : -RT_INF;
-                const int col = At::column(o, i < V ? i : 0);
-                if (col == of || w != w) w = -RT_INF;
-                if (l < 16 && i < V && col == of) row0[o * LD + i] = -RT_INF;
-                const float next = route_max<16>(w);
-                const int next_at = route_min<16>(i < V && w == next ? col : INT32_MAX);
-                if (l == o) {
-                    best = next;
-                    at = next_at;
+                // the lane that held it looks for its next (where nothing is left, any lane will do)
+                const int o = c / At::CH % L, i = lane & 15, col = At::column(o, i < V ? i : 0);
+                int w = i < V ? row0[o * LD + i] : RT_GONE;
+                if (APART ? col == c : w == m) {
+                    w = RT_GONE;
+                    if (l < 16 && i < V) row0[o * LD + i] = RT_GONE;
                 }
+                const int next = route_top<16>(w);
+                if (APART) {
+                    const int next_at = route_min<16>(i < V && w == next ? col : INT32_MAX);
+                    if (l == o) at = next_at;
+                }
+                if (l == o) best = next;
             }
         }
+        float ge[KEEP], chosen = 0.0f;
+#pragma unroll
+        for (int q = 0; q < KEEP; ++q) {
+            ge[q] = id[q] >= 0 ? __builtin_amdgcn_exp2f((route_value<T>(key[q]) - top) * RT_LOG2E) : 0.0f;
+            chosen += ge[q];
+        }
+        if (a.normalize) chosen = route_sum<L>(chosen);
         if (in) {
             const float by = bad ? inv : a.normalize ? (chosen > 0.0f ? 1.0f / chosen : 0.0f) : inv;
 #pragma unroll
@@ -228,7 +280,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
         for (int d = L; d < 64; d <<= 1) acc[v] += __shfl_xor(acc[v], d);
     }
     __syncthreads();
-    float* sums = lds;  // [waves][L * V]
+    float* sums = (float*)lds;  // [waves][L * V]
     if (sub == 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) sums[wave * L * V + At::column(l, v)] = acc[v];
@@ -262,14 +314,14 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     dot = route_sum<64>(dot);
     pairs = route_reduce<64>(pairs, [](int x, int y) { return x + y; });
     if (lane == 0) {
-        lds[wave] = dot;
-        lds[WAVES + wave] = __int_as_float(pairs);
+        sums[wave] = dot;
+        lds[WAVES + wave] = pairs;
     }
     __syncthreads();
     if (tid == 0) {
         for (int w = 1; w < WAVES; ++w) {
-            dot += lds[w];
-            pairs += __float_as_int(lds[WAVES + w]);
+            dot += sums[w];
+            pairs += lds[WAVES + w];
         }
         a.loss[0] = route_loss(dot, pairs, cnt[a.K], a.K);
     }
@@ -366,19 +418,24 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     float w[V];  // a_e
 #pragma unroll
     for (int v = 0; v < V; ++v) w[v] = 0.0f;
-    if (a.dloss) {
-        int all = 0;
-        for (int e = lane; e < a.K; e += 64) all += a.counts[e];
-        all = route_reduce<64>(all, [](int x, int y) { return x + y; });
-        const float by = a.dloss[0] * route_loss(1.0f, all, a.counts[a.K], a.K);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = At::column(l, v);
-            w[v] = c < a.K ? by * (float)a.counts[c] : 0.0f;
-        }
-    }
     const int64_t step = (int64_t)gridDim.x * WAVES * ROWS;
-    for (int64_t r0 = ((int64_t)blockIdx.x * WAVES + wave) * ROWS; r0 < a.n; r0 += step) {
+    int64_t r0 = ((int64_t)blockIdx.x * WAVES + wave) * ROWS;
+    RouteRaw<T, L, V> raw;
+    auto load = [&](int64_t at) { raw.load((const T*)a.s + (at + sub < a.n ? at + sub : a.n - 1) * a.lds, a.K, l); };
+    if (r0 < a.n) load(r0);
+    if (a.dloss) {
+        int c[V], all = 0;
+        const int rows = a.counts[a.K];
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = At::column(l, v) < a.K ? a.counts[At::column(l, v)] : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) all += c[v];
+        all = route_reduce<L>(all, [](int x, int y) { return x + y; });
+        const float by = a.dloss[0] * route_loss(1.0f, all, rows, a.K);
+#pragma unroll
+        for (int v = 0; v < V; ++v) w[v] = by * (float)c[v];
+    }
+    for (; r0 < a.n; r0 += step) {
         const bool in = r0 + sub < a.n;
         const int64_t r = in ? r0 + sub : a.n - 1;
         int id[KEEP];
@@ -398,8 +455,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
             }
         }
         float x[V], p[V], top, inv;
-        route_load<T, L, V>(x, (const T*)a.s + r * a.lds, a.K, l);
+        raw.get(x);
         route_softmax<L, V>(x, p, top, inv);
+        if (r0 + step < a.n) load(r0 + step);
         float dot = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
