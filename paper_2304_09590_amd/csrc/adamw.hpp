@@ -284,23 +284,12 @@ __device__ inline float ad_scalar(float v) { return __uint_as_float(__builtin_am
 
 // the largest of a wave's sizes; NaN if one is infinite or none (sizes are compared as integers, which order them
 // with infinities and NaN last)
-template <int CTRL> __device__ inline uint32_t ad_dpp_max(uint32_t v) {
-    const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
-    return u > v ? u : v;
-}
 __device__ inline uint32_t ad_size(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 __device__ inline float ad_scale(const float (&x)[4]) {
     uint32_t v = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v = ad_size(x[k]) > v ? ad_size(x[k]) : v;
-    v = ad_dpp_max<DPP_ROW_MIRROR>(v);
-    v = ad_dpp_max<DPP_ROW_HALF_MIRROR>(v);
-    v = ad_dpp_max<DPP_XOR2>(v);
-    v = ad_dpp_max<DPP_XOR1>(v);
-    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = a[0] > a[1] ? a[0] : a[1];
-    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    v = b[0] > b[1] ? b[0] : b[1];
+    v = lanes_reduce<64>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
     return v < 0x7f800000u ? __uint_as_float(v) : __builtin_nanf("");
 }
 

@@ -22,10 +22,11 @@ pnn_status check_scale(const char* name, const float* p) {
 // threads of a row, 16 values each
 template <typename T>
 void launch_codes(const CodesArgs& c, hipStream_t s) {
-    const int threads = c.width <= 256 ? 16 : c.width <= 1024 ? 64 : 256, each = 256 / threads;
-    const unsigned blocks = (unsigned)std::min<int64_t>((c.n + each - 1) / each, 8192);
+    const int threads = c.width <= 256 ? 16 : c.width <= 1024 ? 64 : c.width <= 2048 ? 128 : 256, each = 256 / threads;
+    const unsigned blocks = (unsigned)std::min<int64_t>((c.n + each - 1) / each, 2048);
     if (threads == 16) codes_kernel<T, 16><<<blocks, 256, 0, s>>>(c);
     else if (threads == 64) codes_kernel<T, 64><<<blocks, 256, 0, s>>>(c);
+    else if (threads == 128) codes_kernel<T, 128><<<blocks, 256, 0, s>>>(c);
     else codes_kernel<T, 256><<<blocks, 256, 0, s>>>(c);
 }
 

@@ -258,6 +258,26 @@ __host__ inline size_t group_lds(int K) {
     return (size_t)GR_WAVES * (K + 2) * 8 + sizeof(int) * ((size_t)GR_WAVES * (K + 1) + (2 + GR_HEIGHTS) * (K + 2));
 }
 
+template <int CTRL, typename T> __device__ inline T lanes_dpp(T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// f over each 16 lanes (by DPP) or all 64 (and exchanges of halves), for every one of them; 32-bit values
+template <int L, typename T, typename F>
+__device__ inline T lanes_reduce(T v, F f) {
+    v = f(v, lanes_dpp<DPP_ROW_MIRROR>(v));
+    v = f(v, lanes_dpp<DPP_ROW_HALF_MIRROR>(v));
+    v = f(v, lanes_dpp<DPP_XOR2>(v));
+    v = f(v, lanes_dpp<DPP_XOR1>(v));
+    if (L == 64) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, v);
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        v = f(__builtin_bit_cast(T, (uint32_t)a[0]), __builtin_bit_cast(T, (uint32_t)a[1]));
+        const uint32_t w = __builtin_bit_cast(uint32_t, v);
+        const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+        v = f(__builtin_bit_cast(T, (uint32_t)b[0]), __builtin_bit_cast(T, (uint32_t)b[1]));
+    }
+    return v;
+}
 // ------------------------------------------------------------------------------------
 // products
 

@@ -91,34 +91,14 @@ struct RouteRaw {
     }
 };
 
-template <int CTRL, typename T> __device__ inline T route_dpp(T v) {
-    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-// over the L lanes of a row: 16 by DPP, their four rows by exchanges of halves
-template <int L, typename T, typename F>
-__device__ inline T route_reduce(T v, F f) {
-    v = f(v, route_dpp<DPP_ROW_MIRROR>(v));
-    v = f(v, route_dpp<DPP_ROW_HALF_MIRROR>(v));
-    v = f(v, route_dpp<DPP_XOR2>(v));
-    v = f(v, route_dpp<DPP_XOR1>(v));
-    if (L == 64) {
-        const uint32_t u = __builtin_bit_cast(uint32_t, v);
-        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-        v = f(__builtin_bit_cast(T, (uint32_t)a[0]), __builtin_bit_cast(T, (uint32_t)a[1]));
-        const uint32_t w = __builtin_bit_cast(uint32_t, v);
-        const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-        v = f(__builtin_bit_cast(T, (uint32_t)b[0]), __builtin_bit_cast(T, (uint32_t)b[1]));
-    }
-    return v;
-}
 template <int L> __device__ inline float route_max(float v) {
-    return route_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+    return lanes_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 template <int L> __device__ inline float route_sum(float v) {
-    return route_reduce<L>(v, [](float a, float b) { return a + b; });
+    return lanes_reduce<L>(v, [](float a, float b) { return a + b; });
 }
 template <int L> __device__ inline int route_min(int v) {
-    return route_reduce<L>(v, [](int a, int b) { return a < b ? a : b; });
+    return lanes_reduce<L>(v, [](int a, int b) { return a < b ? a : b; });
 }
 
 // e = exp(x - max) of a row; 1 / sum: 0 for a row of -inf, NaN for one with a NaN or an infinity
@@ -162,7 +142,7 @@ __device__ inline float route_value(int key) {
     return __int_as_float(k ^ (k >> 31 & MASK));
 }
 template <int L> __device__ inline int route_top(int v) {
-    return route_reduce<L>(v, [](int a, int b) { return a > b ? a : b; });
+    return lanes_reduce<L>(v, [](int a, int b) { return a > b ? a : b; });
 }
 
 // Choosing is k times the largest of the row's lanes' largest (the lowest index on ties).  The lane that held it then
@@ -312,7 +292,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     }
     __syncthreads();
     dot = route_sum<64>(dot);
-    pairs = route_reduce<64>(pairs, [](int x, int y) { return x + y; });
+    pairs = lanes_reduce<64>(pairs, [](int x, int y) { return x + y; });
     if (lane == 0) {
         sums[wave] = dot;
         lds[WAVES + wave] = pairs;
@@ -362,7 +342,7 @@ __global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
         }
         const bool network = tid < RT_JOIN && e < a.K;
         const float dot = route_sum<16>(network ? (float)all * p : 0.0f);
-        const int pairs = route_reduce<16>(network ? all : 0, [](int x, int y) { return x + y; });
+        const int pairs = lanes_reduce<16>(network ? all : 0, [](int x, int y) { return x + y; });
         if (tid == 0) {
             a.dots[2 * blockIdx.x] = dot;
             a.dots[2 * blockIdx.x + 1] = __int_as_float(pairs);
@@ -381,7 +361,7 @@ __global__ __launch_bounds__(256) void route_join_kernel(RouteArgs a) {
         pairs += __float_as_int(__hip_atomic_load(a.dots + 2 * w + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     }
     dot = route_sum<64>(dot);
-    pairs = route_reduce<64>(pairs, [](int x, int y) { return x + y; });
+    pairs = lanes_reduce<64>(pairs, [](int x, int y) { return x + y; });
     if (tid == 0) a.loss[0] = route_loss(dot, pairs, __hip_atomic_load(a.counts + a.K, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), a.K);
 }
 
@@ -430,7 +410,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
         for (int v = 0; v < V; ++v) c[v] = At::column(l, v) < a.K ? a.counts[At::column(l, v)] : 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) all += c[v];
-        all = route_reduce<L>(all, [](int x, int y) { return x + y; });
+        all = lanes_reduce<L>(all, [](int x, int y) { return x + y; });
         const float by = a.dloss[0] * route_loss(1.0f, all, rows, a.K);
 #pragma unroll
         for (int v = 0; v < V; ++v) w[v] = by * (float)c[v];

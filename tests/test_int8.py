@@ -95,7 +95,7 @@ def test_codes(shape, pad, dtype):
 
 
 @gpu
-@pytest.mark.parametrize("width", [5, 300, 2000, 5000])
+@pytest.mark.parametrize("width", [5, 300, 1030, 2000, 4000, 5000])
 def test_codes_of_extremes(width):
     x = torch.randn(20, width, generator=torch.Generator().manual_seed(2))
     x[0] = 0
