@@ -194,8 +194,9 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     const GroupPlan p = group_plan(g->n, g->per_row, g->networks);
     // Codes take half the steps of bf16 for the same results, whose stores weigh more: with two workgroups a CU one
     // stores while the other multiplies.  Us for tiles of 256 x 128 against 256 x 256: 32 networks 1024 -> 4096, 65,536
-    // pairs (537 MB in bf16) 392, 412; 2048 -> 4096 689, 682; 16 networks 2048 -> 2048, 32,768 pairs (134 MB) 174,
-    // 180; 4096 -> 4096 637, 622; 64 networks 784 -> 512, 60,000 pairs (61 MB) 62, 57; fp32 1024 -> 4096 (1.1 GB) 530, 547.
+    // pairs (537 MB in bf16) 392, 412 (on another card 390, 390); 2048 -> 4096 689, 682; 16 networks 2048 -> 2048, 32,768
+    // pairs (134 MB) 174, 180; 4096 -> 4096 637, 622; 64 networks 784 -> 512, 60,000 pairs (61 MB) 62, 57; fp32
+    // 1024 -> 4096 (1.1 GB) 530, 547.
     if (std::is_same<T, codes_t>::value && kind == RING_HUGE && a.Kx <= 1024 && p.P * a.M * (int64_t)sizeof(TO) >= (int64_t(96) << 20))
         kind = RING;
     const int height = kind == FEW ? 0 : kind == TILE64 || kind == RING_SMALL ? 1 : kind == RING_HUGE ? 3 : 2;

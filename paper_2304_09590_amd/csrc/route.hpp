@@ -40,6 +40,12 @@ struct RouteArgs {
     int64_t ldds;
 };
 
+// what lanes of a wave have written to LDS before is what others of it read after (its accesses keep their order)
+__device__ inline void route_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 constexpr float RT_INF = __builtin_huge_valf();
 constexpr float RT_LOG2E = 1.44269504f;
 
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
                 best = k > best ? k : best;
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        route_order();
         route_softmax<L, V>(x, e, top, inv);
         if (r0 + step < a.n) load(r0 + step);
         const bool bad = inv != inv, has = inv > 0.0f;
@@ -385,7 +391,8 @@ __device__ inline void route_store4(bf16_t* p, const float* v, int nv) {
     }
 }
 
-// What the gates add lies in LDS, a place for each score of the row: the lanes that hold the choices add theirs there.
+// What the gates add lies in LDS, a place for each score of the row, where the lanes that hold the choices write theirs (a
+// network that stands twice gets a sum in the order of the choices).
 template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
@@ -393,6 +400,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     __shared__ __align__(16) float lds[256 * LD];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane % L, sub = lane / L;
     float *mine = lds + tid * LD, *row0 = lds + (tid - l) * LD;
+    auto place = [&](int c) { return row0 + c / At::CH % L * LD + c / (At::CH * L) * At::CH + c % At::CH; };
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v] = 0.0f;
     float w[V];  // a_e
@@ -459,14 +467,31 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
                 if (id[q] >= 0) mix += gate[q] * dg[q];
             }
             mix = route_sum<L>(mix);
+            // each choice writes its number, and finds another's where the same network stands twice
+            bool twice = false;
 #pragma unroll
             for (int q = 0; q < KEEP; ++q)
-                if (id[q] >= 0) {
-                    const int c = id[q];
-                    atomicAdd(row0 + c / At::CH % L * LD + c / (At::CH * L) * At::CH + c % At::CH,
-                              gate[q] * (a.normalize ? dg[q] - mix : dg[q]));
-                }
-            __builtin_amdgcn_wave_barrier();
+                if (id[q] >= 0) *(int*)place(id[q]) = q * L + l;
+            route_order();
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q)
+                if (id[q] >= 0) twice |= *(const int*)place(id[q]) != q * L + l;
+            route_order();
+            const bool any = __ballot(twice) != 0;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) {
+                gate[q] *= a.normalize ? dg[q] - mix : dg[q];
+                if (id[q] >= 0) *place(id[q]) = any ? 0.0f : gate[q];
+            }
+            route_order();
+            if (any) {  // one after another
+#pragma unroll
+                for (int q = 0; q < KEEP; ++q)
+                    for (int j = 0; j < L && q * L + j < a.k; ++j) {
+                        if (l == j && id[q] >= 0) *place(id[q]) += gate[q];
+                        route_order();
+                    }
+            }
         }
         const float off = a.normalize ? dot : dot + mix;
         float d[V];
@@ -476,10 +501,10 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
             if (a.dgates) d[v] += mine[v];
         }
         if (a.dgates) {
-            __builtin_amdgcn_wave_barrier();
+            route_order();
 #pragma unroll
             for (int q = 0; q < KEEP; ++q)
-                if (id[q] >= 0) row0[id[q] / At::CH % L * LD + id[q] / (At::CH * L) * At::CH + id[q] % At::CH] = 0.0f;
+                if (id[q] >= 0) *place(id[q]) = 0.0f;
         }
         if (!in) continue;
         T* out = (T*)a.ds + r * a.ldds;

@@ -222,6 +222,7 @@ def test_given_ids_and_gradients_alone(n, K, k, dtype):
     ids = torch.randint(0, K, (n, k), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
     ids[:, 1] = ids[:, 0]
     ids[3, 2], ids[4], ids[5, 0] = K, -1, -2 ** 31
+    ids[6:10] = ids[6:10, :1]  # one network in all places
     ids = ids.cuda()
     _, _, counts, _ = pnn.route(s, k)
     one = torch.ones(1, device="cuda")
@@ -230,6 +231,7 @@ def test_given_ids_and_gradients_alone(n, K, k, dtype):
         near(pnn.route_grad(s, ids, None, dgates, normalize=normalize), *reference(s, k, normalize, dgates, 0.0, ids)[4], dtype=dtype)
         near(pnn.route_grad(s, ids, counts, None, one, normalize=normalize), *reference(s, k, normalize, zero, 1.0, ids)[4], dtype=dtype)
         assert (pnn.route_grad(s, ids, normalize=normalize) == 0).all()
+        assert torch.equal(pnn.route_grad(s, ids, counts, dgates, one, normalize=normalize), pnn.route_grad(s, ids, counts, dgates, one, normalize=normalize))
 
 
 @gpu
