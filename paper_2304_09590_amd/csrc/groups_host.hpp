@@ -207,7 +207,10 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     // Forward in us, cached -> streamed, and with the next layer, which reads the result: 2048 x 2048, 134 MB 314 ->
     // 263, 641 -> 603; 67 MB 157 -> 154, 357 -> 370; 1024 x 1024, 134 MB 171 -> 148, 356 -> 328; 17 MB 38 -> 38,
     // 75 -> 78.
-    a.stream = sizeof(TO) == 2 && p.P * a.M * (int64_t)sizeof(TO) >= (int64_t(96) << 20);
+    // fp32 results of codes from 256 MiB on: 65,536 pairs 1024 -> 4096 (1 GiB) 539 -> 485, with a reader 816 -> 776; 29,601
+    // pairs 48 -> 3352 (378 MiB) 152 -> 150, 265 -> 253; 128 MiB 74 -> 77, 102 -> 115.
+    constexpr int64_t LARGE = sizeof(TO) == 2 ? 96 : std::is_same<T, codes_t>::value ? 256 : INT64_MAX >> 20;  // MiB
+    a.stream = p.P * a.M * (int64_t)sizeof(TO) >= LARGE << 20;
     if constexpr (sizeof(T) == 2) {
         if (kind == RING_HUGE) return launch_ring<DIR, T, TO, 256, 256, 2, 4, 4, true>(a, blocks(256), s);
         if (kind == RING) return launch_ring<DIR, T, TO, 256, 128, 2, 2, 3, false>(a, blocks(256), s);

@@ -241,6 +241,18 @@ def test_results_behind_32_bits():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,n", [(BF16, 25000), (F32, 35000)])
+def test_results_larger_than_the_caches(dtype, n):
+    """An odd number of outputs and a distance between rows that is no multiple of 16 bytes; what lies beside stays."""
+    K, I, O = 5, 64, 2047
+    ids, x, xs, w, ws, b = case(n, 1, K, I, O, seed=10)
+    whole = torch.full((n, O + 2), 5.0, dtype=dtype, device="cuda")
+    assert n * O * whole.element_size() > (96 if dtype == BF16 else 256) << 20
+    verify(ids, x, xs, w, ws, b, "relu", dtype, K, out=whole[:, 1:-1])
+    assert (whole[:, 0] == 5).all() and (whole[:, -1] == 5).all()
+
+
+@gpu
 def test_rows_to_answers_on_another_stream_and_in_a_graph():
     """Two layers as a program serves them: codes of the rows, the product, codes of its results, the next product."""
     g = torch.Generator(device="cuda").manual_seed(3)
