@@ -22,11 +22,18 @@ pnn_status check_route(const pnn_router* a) {
 
 bool misaligned4(const void* p) { return ((uintptr_t)p & 3) != 0; }
 
-// rows that a wave takes at a time: those of up to 256 scores lie on 16 lanes
-int route_rows(int32_t networks) { return networks <= 256 ? 4 : 1; }
+// Lanes of a row.  Few lanes share the exchanges of a choice among several rows, many have fewer scores each to look at.
+// Us with counts, two and eight choices: 60,000 rows of 250 on 16 lanes 18, 26, on 64 32, 73; of 40 10, 19 against
+// 22, 45; of 500 on 32 lanes 29, 48, on 64 38, 79; 8,000 rows of 500 7.2, 9.6 against 7.6, 13.0; 1,000 rows of 500 6.7, 9.1
+// against 5.1, 7.8; of 250 on 16 lanes 6.8, 9.0, on 64 7.6, 7.7.  (1,000 scores on 32 lanes do not fit the registers.)
+int route_lanes(int64_t n, int32_t K) { return K <= 256 ? 16 : K <= 512 && n > 4096 ? 32 : 64; }
+// The gradient has no choices, and a wave its networks' weights to begin with.  Us on 16 lanes against 64: 60,000 rows of 250 26,
+// 28, of 40 12, 19; 16,000 rows 12.0, 11.4 and 6.1, 6.8; 8,000 rows 8.7, 7.3 and 4.9, 4.7; 1,000 rows 6.7, 3.8 and 4.5, 3.1.
+int route_grad_lanes(int64_t n, int32_t K) { return K <= 256 && n > 8192 ? 16 : 64; }
 
-int route_blocks(int64_t n, int32_t networks) {
-    const int64_t each = RT_THREADS / 64 * route_rows(networks);
+int64_t route_rows(int lanes) { return RT_THREADS / 64 * (64 / lanes); }  // of a workgroup, at a time
+int route_blocks(int64_t n, int32_t K) {
+    const int64_t each = route_rows(route_lanes(n, K));
     return (int)std::max<int64_t>(1, std::min<int64_t>((n + each - 1) / each, RT_MAX_BLOCKS));
 }
 
@@ -38,16 +45,39 @@ RouteArgs route_args(const pnn_router* a) {
     return r;
 }
 
-// f(scores of a lane, lanes of a row) by the number of networks
-template <typename F>
-void route_by_width(int32_t K, F f) {
-    using std::integral_constant;
-    if (K <= 16) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (K <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-    else if (K <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-    else if (K <= 256) f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-    else if (K <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-    else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+template <typename T>
+void launch_route(const RouteArgs& r, hipStream_t s) {
+    const int lanes = route_lanes(r.n, r.K);
+#define PNN_ROUTE(L, V) route_kernel<T, L, V><<<r.blocks, RT_THREADS, 0, s>>>(r)
+    if (r.K <= 16) PNN_ROUTE(16, 1);
+    else if (r.K <= 64) PNN_ROUTE(16, 4);
+    else if (r.K <= 128) PNN_ROUTE(16, 8);
+    else if (r.K <= 256) PNN_ROUTE(16, 16);
+    else if (lanes == 32) PNN_ROUTE(32, 16);
+    else if (r.K <= 512) PNN_ROUTE(64, 8);
+    else PNN_ROUTE(64, 16);
+#undef PNN_ROUTE
+}
+
+template <typename T>
+void launch_route_grad(const RouteArgs& r, hipStream_t s) {
+    const int lanes = route_grad_lanes(r.n, r.K);
+    const int64_t each = 4 * (64 / lanes);
+    // (us with 1,024 workgroups against 2,048: 60,000 rows of 250 26, 29, of 1,000 93, 101; of 500 45, 42)
+    const unsigned blocks = (unsigned)std::min<int64_t>((r.n + each - 1) / each, r.K > 256 && r.K <= 512 ? 2048 : 1024);
+#define PNN_ROUTE(L, V) route_grad_kernel<T, L, V><<<blocks, 256, 0, s>>>(r)
+    if (lanes == 16) {
+        if (r.K <= 16) PNN_ROUTE(16, 1);
+        else if (r.K <= 64) PNN_ROUTE(16, 4);
+        else if (r.K <= 128) PNN_ROUTE(16, 8);
+        else PNN_ROUTE(16, 16);
+    } else {
+        if (r.K <= 64) PNN_ROUTE(64, 1);
+        else if (r.K <= 256) PNN_ROUTE(64, 4);
+        else if (r.K <= 512) PNN_ROUTE(64, 8);
+        else PNN_ROUTE(64, 16);
+    }
+#undef PNN_ROUTE
 }
 
 pnn_status check_combine(const pnn_combine* a) {
@@ -104,17 +134,17 @@ pnn_status pnn_route(const pnn_router* a, int32_t* ids_dev, float* gates_dev, in
     RouteArgs r = route_args(a);
     r.ids = ids_dev; r.gates = gates_dev;
     r.counts = counts_dev; r.loss = loss_dev;
-    const int64_t each = RT_THREADS / 64 * route_rows(a->networks);
-    // (without sums to join, as many workgroups as rows keep busy)
-    r.blocks = counts_dev ? route_blocks(a->n, a->networks) : (int)std::min<int64_t>((a->n + each - 1) / each, 4096);
+    r.blocks = route_blocks(a->n, a->networks);
+    if (!counts_dev && a->networks <= 128) {  // (without sums to join: small rows keep more than one workgroup a CU busy)
+        const int64_t each = route_rows(route_lanes(a->n, a->networks));
+        r.blocks = (int)std::min<int64_t>((a->n + each - 1) / each, 4096);
+    }
     r.part = (float*)ws_dev;
     r.part_counts = (int32_t*)ws_dev + (int64_t)r.blocks * a->networks;
     r.dots = (float*)ws_dev + round_up((int64_t)r.blocks * (2 * a->networks + 1), 4);
     r.arrived = (int32_t*)r.dots + 2 * (GR_MAX_NETS / RT_JOIN + 1);
-    route_by_width(a->networks, [&](auto L, auto V) {
-        if (a->type == PNN_FP32) route_kernel<float, L(), V()><<<r.blocks, RT_THREADS, 0, s>>>(r);
-        else route_kernel<bf16_t, L(), V()><<<r.blocks, RT_THREADS, 0, s>>>(r);
-    });
+    if (a->type == PNN_FP32) launch_route<float>(r, s);
+    else launch_route<bf16_t>(r, s);
     TRY(launched("routing"));
     if (!counts_dev || r.blocks == 1) return PNN_OK;  // (a workgroup that is alone has it all)
     route_join_kernel<<<a->networks / RT_JOIN + 1, 256, 0, s>>>(r);
@@ -136,12 +166,8 @@ pnn_status pnn_route_grad(const pnn_router* a, const int32_t* ids_dev, const int
     r.ids = const_cast<int32_t*>(ids_dev); r.counts = const_cast<int32_t*>(counts_dev);
     r.dgates = dgates_dev; r.dloss = dloss_dev;
     r.ds = ds_dev; r.ldds = ds_ld;
-    const int64_t each = 4 * route_rows(a->networks);
-    const unsigned blocks = (unsigned)std::min<int64_t>((a->n + each - 1) / each, 2048);
-    route_by_width(a->networks, [&](auto L, auto V) {
-        if (a->type == PNN_FP32) route_grad_kernel<float, L(), V()><<<blocks, 256, 0, s>>>(r);
-        else route_grad_kernel<bf16_t, L(), V()><<<blocks, 256, 0, s>>>(r);
-    });
+    if (a->type == PNN_FP32) launch_route_grad<float>(r, s);
+    else launch_route_grad<bf16_t>(r, s);
     return launched("the router's gradient");
 }
 

@@ -165,7 +165,7 @@ def verify(s, k, normalize, dgates, dloss=0.7):
 
 SHAPES = [(1, 1, 1, 0), (3, 2, 2, 0), (60, 16, 3, 0), (17, 17, 5, 1), (33, 64, 8, 0), (20, 65, 20, 3), (64, 128, 16, 0), (9, 129, 64, 5),
           (50, 256, 2, 0), (7, 257, 9, 0), (5, 512, 64, 1), (5, 513, 1, 0), (9, 1000, 8, 3), (3, 1024, 64, 0), (4097, 40, 2, 0),
-          (9001, 250, 4, 0)]
+          (9001, 250, 4, 0), (8200, 10, 2, 0), (8200, 60, 5, 1), (8193, 100, 17, 0), (5000, 500, 33, 0), (4100, 300, 3, 1), (17000, 257, 2, 0)]
 
 
 @gpu
