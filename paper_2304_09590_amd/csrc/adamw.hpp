@@ -13,9 +13,10 @@
 // function of the seed, the step, the tensor, the block and the place, so the same call gives the same bits.
 //
 // Bound by bytes: with fp32 gradients 28 a value, or 16 and the scales in 8 bits, 2 more for a copy.  34.3 million values
-// with copies: 193 us in 32 bits (5.3 TB/s), 118 us in 8 (5.2 TB/s).  What brought the latter there from 251 us: levels
-// from LDS instead of their formula and codes without branches (187 -> 160), global addresses with scalar bases
-// instead of flat ones (160 -> 118), and the places below (58 ns for each of 1,024 workgroups).
+// with copies: 193 us in 32 bits (5.3 TB/s), 120 to 133 us in 8 (5.2 to 4.7 TB/s), where instructions take 0.8 of the
+// cycles.  What brought the latter there from 251 us: levels from LDS instead of their formula and codes without branches
+// (187 -> 160), global addresses with scalar bases instead of flat ones (160 -> 118, at gradients alike; 138 at unlike
+// ones), whole chunks without looking for ends (138 -> 125), and the places below (58 ns for each of 1,024 workgroups).
 #pragma once
 #include <stddef.h>
 
@@ -151,15 +152,16 @@ __device__ inline AdamLog ad_log(float scale, int top) {
 template <int TOP, int LOWEST>
 __device__ inline int ad_code(const AdamLevels<TOP>& levels, float x, float scale, float log, float u) {
 #pragma clang fp contract(off)
+    // (no number, or no scale: some code, which the caller leaves out)
     const int k = (int)__builtin_rintf(__builtin_amdgcn_fmed3f(log, 0.0f, (float)TOP));
-    const float* l = levels.at + (x > 0.0f && scale > 0.0f ? k : 0);  // (no number, or no scale: any place)
+    const float* l = levels.at + k;
     const float lower = l[0] * scale, near = l[1] * scale, upper = l[2] * scale;
     const bool over = x >= near;
     const float below = over ? near : lower, above = over ? upper : near;
     int c = over ? k : k - 1;
     c += u * (above - below) < x - below ? 1 : 0;
-    c = LOWEST > 0 && c < LOWEST ? LOWEST : c;
-    return x > 0.0f && scale > 0.0f ? c : 0;
+    if (LOWEST > 0) c = c < LOWEST && x > 0.0f ? LOWEST : c;
+    return c;
 }
 
 // the root, by the instruction (one unit in the last place; it takes no subnormals)
@@ -312,73 +314,80 @@ __global__ __launch_bounds__(64 * WAVES) void adamw_kernel(AdamArgs a) {
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const AdamPlace<TG, TS> x(a.plan, c, lane);
         const int b0 = wave * NB, first = b0 * AD_BLOCK + lane * 4;
-        float p[NB][4], g[NB][4], m[NB][4], v[NB][4], sm[NB], sv[NB];
-        uint32_t qm[NB], qv[NB];
+        auto work = [&](auto full) {  // (a whole chunk: no ends to look for)
+            constexpr bool FULL = decltype(full)::value;
+            float p[NB][4], g[NB][4], m[NB][4], v[NB][4], sm[NB], sv[NB];
+            uint32_t qm[NB], qv[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int at = first + b * AD_BLOCK, nv = x.n - at;
-            ad_load4(p[b], x.p + at, nv);
-            ad_load4(g[b], x.g + at, nv);
-            if constexpr (BITS == 32) {
-                ad_load4(m[b], x.m + at, nv);
-                ad_load4(v[b], x.v + at, nv);
-            } else {
-                qm[b] = ad_load4(x.m + at, nv);
-                qv[b] = ad_load4(x.v + at, nv);
-                const bool in = at - lane * 4 < x.n;
-                sm[b] = in ? x.sm[b0 + b] : 0.0f;
-                sv[b] = in ? x.sv[b0 + b] : 0.0f;
-            }
-        }
-        if (t == 0) {  // (behind the first loads)
-            t = __builtin_amdgcn_readfirstlane(done) + 1;
-            r = ad_rates(a, t);
-        }
-        const uint32_t key = BITS == 8 ? ad_mix(ad_mix(a.seed + 0x6A09E667u * (uint32_t)t) + x.tensor) : 0;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int at = first + b * AD_BLOCK, nv = x.n - at;
-            if (at - lane * 4 >= x.n) break;  // (the same for a wave)
-            if (BITS == 8) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int cm = qm[b] >> (8 * k) & 255, cv = qv[b] >> (8 * k) & 255;
-                    m[b][k] = m_levels.of(cm & 127) * (cm & 128 ? -sm[b] : sm[b]);
-                    v[b][k] = v_levels.of(cv) * sv[b];
+            for (int b = 0; b < NB; ++b) {
+                const int at = first + b * AD_BLOCK, nv = FULL ? 4 : x.n - at;
+                ad_load4(p[b], x.p + at, nv);
+                ad_load4(g[b], x.g + at, nv);
+                if constexpr (BITS == 32) {
+                    ad_load4(m[b], x.m + at, nv);
+                    ad_load4(v[b], x.v + at, nv);
+                } else {
+                    qm[b] = ad_load4(x.m + at, nv);
+                    qv[b] = ad_load4(x.v + at, nv);
+                    const bool in = FULL || at - lane * 4 < x.n;
+                    sm[b] = in ? x.sm[b0 + b] : 0.0f;
+                    sv[b] = in ? x.sv[b0 + b] : 0.0f;
                 }
             }
+            if (t == 0) {  // (behind the first loads)
+                t = __builtin_amdgcn_readfirstlane(done) + 1;
+                r = ad_rates(a, t);
+            }
+            const uint32_t key = BITS == 8 ? ad_mix(ad_mix(a.seed + 0x6A09E667u * (uint32_t)t) + x.tensor) : 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) ad_value(r, g[b][k], p[b][k], m[b][k], v[b][k]);
-            ad_store4(x.p + at, p[b], nv);
-            if (x.copy) ad_store4(x.copy + at, p[b], nv);
-            if constexpr (BITS == 32) {
-                ad_store4(x.m + at, m[b], nv);
-                ad_store4(x.v + at, v[b], nv);
-            } else {
-                // (a value that is no number makes its block's scale one that is none; lanes past the end hold zeros)
-                const float nm = ad_scale(m[b]), nw = ad_scale(v[b]);
-                const uint32_t place = ad_mix(key + x.block + (uint32_t)(b0 + b)) + (uint32_t)(lane * 4);
-                const AdamLog lm = ad_log(nm, 127), lv = ad_log(nw, 255);
-                uint32_t om = 0, ov = 0;
+            for (int b = 0; b < NB; ++b) {
+                const int at = first + b * AD_BLOCK, nv = FULL ? 4 : x.n - at;
+                if (!FULL && at - lane * 4 >= x.n) break;  // (the same for a wave)
+                if (BITS == 8) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t bits = ad_mix(place + (uint32_t)k);
-                    const float um = __builtin_fmaf((float)(bits >> 16), 0x1p-16f, 0x1p-17f);
-                    const float uv = __builtin_fmaf((float)(bits & 0xffff), 0x1p-16f, 0x1p-17f);
-                    const float size = __builtin_fabsf(m[b][k]);
-                    const int cm = ad_code<127, 0>(m_levels, size, nm, lm.of(size), um);
-                    const int cv = ad_code<255, 1>(v_levels, v[b][k], nw, lv.of(v[b][k]), uv);
-                    om |= (uint32_t)(m[b][k] < 0.0f ? cm | 128 : cm) << (8 * k);
-                    ov |= (uint32_t)cv << (8 * k);
+                    for (int k = 0; k < 4; ++k) {
+                        const int cm = qm[b] >> (8 * k) & 255, cv = qv[b] >> (8 * k) & 255;
+                        m[b][k] = m_levels.of(cm & 127) * (cm & 128 ? -sm[b] : sm[b]);
+                        v[b][k] = v_levels.of(cv) * sv[b];
+                    }
                 }
-                ad_store4(x.m + at, om, nv);
-                ad_store4(x.v + at, ov, nv);
-                if (lane == 0) {
-                    x.sm[b0 + b] = nm;
-                    x.sv[b0 + b] = nw;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) ad_value(r, g[b][k], p[b][k], m[b][k], v[b][k]);
+                ad_store4(x.p + at, p[b], nv);
+                if (x.copy) ad_store4(x.copy + at, p[b], nv);
+                if constexpr (BITS == 32) {
+                    ad_store4(x.m + at, m[b], nv);
+                    ad_store4(x.v + at, v[b], nv);
+                } else {
+                    // (a value that is no number makes its block's scale one that is none; lanes past the end hold zeros)
+                    const float nm = ad_scale(m[b]), nw = ad_scale(v[b]);
+                    const uint32_t place = ad_mix(key + x.block + (uint32_t)(b0 + b)) + (uint32_t)(lane * 4);
+                    const AdamLog lm = ad_log(nm, 127), lv = ad_log(nw, 255);
+                    uint32_t om = 0, ov = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t bits = ad_mix(place + (uint32_t)k);
+                        const float um = __builtin_fmaf((float)(bits >> 16), 0x1p-16f, 0x1p-17f);
+                        const float uv = __builtin_fmaf((float)(bits & 0xffff), 0x1p-16f, 0x1p-17f);
+                        const float size = __builtin_fabsf(m[b][k]);
+                        const int cm = ad_code<127, 0>(m_levels, size, nm, lm.of(size), um);
+                        const int cv = ad_code<255, 1>(v_levels, v[b][k], nw, lv.of(v[b][k]), uv);
+                        om |= ((uint32_t)cm | (__float_as_uint(m[b][k]) >> 24 & 128)) << (8 * k);
+                        ov |= (uint32_t)cv << (8 * k);
+                    }
+                    om = nm > 0.0f ? om : 0;
+                    ov = nw > 0.0f ? ov : 0;
+                    ad_store4(x.m + at, om, nv);
+                    ad_store4(x.v + at, ov, nv);
+                    if (lane == 0) {
+                        x.sm[b0 + b] = nm;
+                        x.sv[b0 + b] = nw;
+                    }
                 }
             }
-        }
+        };
+        if (x.n == AD_CHUNK) work(std::true_type{});
+        else work(std::false_type{});
     }
     // the last workgroup to come here counts the step: all others have read the count
     __syncthreads();

@@ -562,43 +562,73 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     }
 }
 
-// A row's pairs one after another, so that the row of g comes from the caches again.  The same rows as above: 1,342 MB in 250 us
-// (5.4 TB/s).
+// A row's pairs four at a time, which share what is loaded of g's row.  The same rows as above: 1,342 MB in 238 us (5.6
+// TB/s; a pair after the other reads a part of g twice, 1,549 MB in 247 us).
+constexpr int CB_PAIRS = 4;
 template <typename T, typename TG>
 __global__ __launch_bounds__(256) void combine_grad_kernel(CombineArgs a) {
-    __shared__ float red[4];
+    __shared__ float red[CB_PAIRS][4];
     const int rows = 256 / a.threads, tx = threadIdx.x % a.threads, ty = threadIdx.x / a.threads;
     for (int64_t r0 = (int64_t)blockIdx.x * rows; r0 < a.n; r0 += (int64_t)gridDim.x * rows) {
         const bool in = r0 + ty < a.n;
         const int64_t r = in ? r0 + ty : a.n - 1;
-        for (int j = 0; j < a.per_row; ++j) {
-            const int64_t p = r * a.per_row + j;
-            const bool kept = (unsigned)a.ids[p] < (unsigned)a.K;
-            const float w = kept ? a.w[p] : 0.0f;
-            float dot = 0.0f;
+        for (int j0 = 0; j0 < a.per_row; j0 += CB_PAIRS) {
+            const int64_t p0 = r * a.per_row + j0;
+            const int pairs = a.per_row - j0 < CB_PAIRS ? a.per_row - j0 : CB_PAIRS;
+            bool kept[CB_PAIRS];
+            float w[CB_PAIRS], dot[CB_PAIRS];
+#pragma unroll
+            for (int j = 0; j < CB_PAIRS; ++j) {
+                kept[j] = j < pairs && (unsigned)a.ids[p0 + (j < pairs ? j : 0)] < (unsigned)a.K;
+                w[j] = kept[j] ? a.w[p0 + j] : 0.0f;
+                dot[j] = 0.0f;
+            }
             for (int m = tx * 8; m < a.M && in; m += a.threads * 8) {
                 const int left = a.M - m;
-                float g[8], v[8];
-                if (kept) {
-                    load8_f<TG>(g, (const TG*)a.g + r * a.ldg + m, left);
-                    load8_f<T>(v, (const T*)a.y + p * a.ldy + m, left);
-                }
+                Raw8<TG> gr;
+                Raw8<T> yr[CB_PAIRS];
+                load8(gr, (const TG*)a.g + r * a.ldg + m, left);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (kept) dot = __builtin_fmaf(g[q], v[q], dot);
-                    v[q] = kept ? w * g[q] : 0.0f;
+                for (int j = 0; j < CB_PAIRS; ++j)
+                    if (kept[j]) load8(yr[j], (const T*)a.y + (p0 + j) * a.ldy + m, left);
+                float g[8];
+                raw8_f(g, gr);
+#pragma unroll
+                for (int j = 0; j < CB_PAIRS; ++j) {
+                    if (j >= pairs) break;
+                    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (kept[j]) {
+                        raw8_f(v, yr[j]);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            dot[j] = __builtin_fmaf(g[q], v[q], dot[j]);
+                            v[q] = w[j] * g[q];
+                        }
+                    }
+                    store8((T*)a.dy + (p0 + j) * a.lddy + m, v, left);
                 }
-                store8((T*)a.dy + p * a.lddy + m, v, left);
             }
-            for (int d = 1; d < a.threads && d < 64; d <<= 1) dot += __shfl_xor(dot, d);
+#pragma unroll
+            for (int j = 0; j < CB_PAIRS; ++j)
+                for (int d = 1; d < a.threads && d < 64; d <<= 1) dot[j] += __shfl_xor(dot[j], d);
             if (a.threads > 64) {
                 __syncthreads();
-                if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = dot;
+                if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                    for (int j = 0; j < CB_PAIRS; ++j) red[j][threadIdx.x >> 6] = dot[j];
+                }
                 __syncthreads();
-                dot = red[ty * (a.threads / 64)];
-                for (int q = 1; q < a.threads / 64; ++q) dot += red[ty * (a.threads / 64) + q];
+#pragma unroll
+                for (int j = 0; j < CB_PAIRS; ++j) {
+                    dot[j] = red[j][ty * (a.threads / 64)];
+                    for (int q = 1; q < a.threads / 64; ++q) dot[j] += red[j][ty * (a.threads / 64) + q];
+                }
             }
-            if (in && tx == 0) a.dw[p] = dot;
+            if (in && tx == 0) {
+#pragma unroll
+                for (int j = 0; j < CB_PAIRS; ++j)
+                    if (j < pairs) a.dw[p0 + j] = dot[j];
+            }
         }
     }
 }
