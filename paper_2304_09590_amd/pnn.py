@@ -699,7 +699,7 @@ def route_grad(s, ids, counts=None, dgates=None, dloss=None, normalize: bool = F
     a = _router(s, ids.shape[1], normalize)
 
     def body(h):
-        ds = out if out is not None else _empty(s, s.shape)
+        ds = out if out is not None else torch.empty_like(s)
         pi = _values(ids, "ids", (a.n, a.per_row), torch.int32)
         pc = _values(counts, "counts", (a.networks + 1,), torch.int32) if counts is not None else None
         pg = _values(dgates, "dgates", ids.shape, torch.float32) if dgates is not None else None
@@ -741,7 +741,7 @@ def combine_grad(dout, y, ids, gates, networks: int, dy=None, stream=None):
     a = _combine(y, ids, gates, networks)
 
     def body(h):
-        d = dy if dy is not None else _empty(y, y.shape)
+        d = dy if dy is not None else torch.empty_like(y)
         dgates = _empty(y, (a.n, a.per_row), torch.float32)
         pg, ldg = _rows(dout, "dout", (a.n, a.width), dout.dtype)
         pd, ldd = _rows(d, "dy", y.shape, y.dtype)
