@@ -821,9 +821,10 @@ class AdamW:
             _call("pnn_adamw_bytes", tensors, count, ctypes.byref(size), ctypes.byref(chunks))
             plan = _empty(first, size.value, torch.uint8)
             _call("pnn_adamw_plan", tensors, count, bits, kind, plan.data_ptr(), size.value, h)
-            return plan, chunks.value
+            return plan, chunks.value, h
 
-        self._plan, chunks = _on(None, body, first, self.steps, self._lr)
+        self._plan, chunks, self._made = _on(None, body, first, self.steps, self._lr)
+        self._recorded = set()  # handles of other streams that steps have been taken on
         self.args = PnnAdamw(self._plan.data_ptr(), chunks, bits, kind, 0.0 if self._lr is not None else lr, betas[0], betas[1], eps,
                              weight_decay, None if self._lr is None else self._lr.data_ptr(), seed & 0xFFFFFFFF, self.steps.data_ptr())
 
@@ -839,10 +840,20 @@ class AdamW:
 
     def step(self, stream=None) -> None:
         """One step with what the gradients hold now."""
-        used = ()
-        if stream is not None:  # (what a torch.cuda.Stream is to keep)
-            used = [t for ts in (self.params, self.grads, self.copies or (), *self.state) for t in ts]
-        _on(stream, lambda s: _call("pnn_adamw_step", ctypes.byref(self.args), s), self.steps, *used, self._plan, self._lr)
+        torch = _t()
+        # on another stream than the object's, its tensors are recorded, once (they stay so until their memory is given back):
+        # the object may go away while the step waits
+        dev = self.steps.get_device()
+        if stream is None:
+            handle = torch._C._cuda_getCurrentRawStream(dev)
+            on = torch.cuda.current_stream(dev) if handle not in self._recorded and handle != self._made else None
+        else:
+            on = stream if isinstance(stream, torch.cuda.Stream) and stream.cuda_stream not in self._recorded else None
+        _on(stream, lambda s: _call("pnn_adamw_step", ctypes.byref(self.args), s), self.steps, self._plan, self._lr)
+        if on is not None:
+            for ts in (self.params, self.grads, self.copies or (), *self.state, (self.steps, self._plan, self._lr)):
+                _record(on, ts)
+            self._recorded.add(on.cuda_stream)
 
 
 def adamw_values(m, v, m_scale, v_scale, stream=None):
