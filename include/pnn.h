@@ -440,8 +440,8 @@ pnn_status pnn_adamw_plan(const pnn_adamw_tensor* tensors, int32_t count, int32_
 typedef struct {
     void* plan_dev;       /* written by pnn_adamw_plan; a step counts its workgroups there */
     int64_t chunks;       /* as pnn_adamw_bytes gives them */
-    int32_t bits;         /* 32 or 8 */
-    int32_t g_type;
+    int32_t bits;         /* 32 or 8, and the gradients' type, as the plan was laid out: with others a step does */
+    int32_t g_type;       /* nothing, and is not counted */
     double lr;            /* 0..1e6 */
     double beta1, beta2;  /* in [0, 1) */
     double eps;           /* 1e-30..1 */

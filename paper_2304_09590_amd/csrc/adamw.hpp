@@ -45,7 +45,9 @@ struct AdamChunk {
     int n;                           // values
     uint32_t block;                  // number of its first block in the tensor
     uint32_t tensor;                 // place of the tensor in the call
+    uint32_t kind;                   // of the states and gradients that the plan was laid out for
 };
+constexpr uint32_t ad_kind(size_t state_size, size_t g_size) { return (uint32_t)(state_size << 8 | g_size); }
 
 struct AdamTensor {
     float* p;
@@ -88,6 +90,7 @@ __global__ __launch_bounds__(256) void adamw_plan_kernel(AdamPlanArgs a) {
         x.n = t.n - at < AD_CHUNK ? (int)(t.n - at) : AD_CHUNK;
         x.block = (uint32_t)block;
         x.tensor = (uint32_t)(a.number + i);
+        x.kind = ad_kind(a.state_size, a.g_size);
         a.plan[c] = x;
     }
 }
@@ -264,7 +267,7 @@ struct AdamPlace {
     PNN_GLOBAL float *sm, *sv;
     PNN_GLOBAL bf16_t* copy;
     int n;
-    uint32_t block, tensor;
+    uint32_t block, tensor, kind;
     __device__ inline AdamPlace(const AdamChunk* plan, uint32_t c, int lane) {
         constexpr int WORDS = sizeof(AdamChunk) / 4;
         const uint32_t w = ((const uint32_t*)(plan + c))[lane < WORDS ? lane : 0];
@@ -280,6 +283,7 @@ struct AdamPlace {
         n = (int)word(offsetof(AdamChunk, n) / 4);
         block = word(offsetof(AdamChunk, block) / 4);
         tensor = word(offsetof(AdamChunk, tensor) / 4);
+        kind = word(offsetof(AdamChunk, kind) / 4);
     }
 };
 __device__ inline float ad_scalar(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
@@ -313,6 +317,8 @@ __global__ __launch_bounds__(64 * WAVES) void adamw_kernel(AdamArgs a) {
     int t = 0;
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const AdamPlace<TG, TS> x(a.plan, c, lane);
+        // (a plan for other states or gradients, which all of its chunks are: nothing is touched, no workgroup counts the step)
+        if (x.kind != ad_kind(sizeof(TS), sizeof(TG))) return;
         const int b0 = wave * NB, first = b0 * AD_BLOCK + lane * 4;
         auto work = [&](auto full) {  // (a whole chunk: no ends to look for)
             constexpr bool FULL = decltype(full)::value;
