@@ -233,6 +233,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
                     w = RT_GONE;
                     if (l < 16 && i < V) row0[o * LD + i] = RT_GONE;
                 }
+                route_order();  // (all lanes of the row read it in the next round)
                 const int next = route_top<16>(w);
                 if (APART) {
                     const int next_at = route_min<16>(i < V && w == next ? col : INT32_MAX);
@@ -258,6 +259,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
                     if (a.counts && id[q] >= 0) atomicAdd(&cnt[id[q]], 1);
                 }
         }
+        route_order();  // (the next row's keys go where this one's were looked through)
     }
     if (!a.counts) return;
     // the workgroup's sums: of the rows within a wave, then of the waves, in their order
@@ -405,6 +407,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     auto place = [&](int c) { return row0 + c / At::CH % L * LD + c / (At::CH * L) * At::CH + c % At::CH; };
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v] = 0.0f;
+    route_order();
     float w[V];  // a_e
 #pragma unroll
     for (int v = 0; v < V; ++v) w[v] = 0.0f;
@@ -473,11 +476,11 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
             bool twice = false;
 #pragma unroll
             for (int q = 0; q < KEEP; ++q)
-                if (id[q] >= 0) *(int*)place(id[q]) = q * L + l;
+                if (id[q] >= 0) *place(id[q]) = __int_as_float(q * L + l);
             route_order();
 #pragma unroll
             for (int q = 0; q < KEEP; ++q)
-                if (id[q] >= 0) twice |= *(const int*)place(id[q]) != q * L + l;
+                if (id[q] >= 0) twice |= __float_as_int(*place(id[q])) != q * L + l;
             route_order();
             const bool any = __ballot(twice) != 0;
 #pragma unroll
@@ -507,6 +510,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
 #pragma unroll
             for (int q = 0; q < KEEP; ++q)
                 if (id[q] >= 0) *place(id[q]) = 0.0f;
+            route_order();  // (other lanes' choices of the next row go there)
         }
         if (!in) continue;
         T* out = (T*)a.ds + r * a.ldds;
