@@ -382,7 +382,7 @@ pnn_status pnn_route(const pnn_router* args, int32_t* ids_dev, float* gates_dev,
                      void* ws_dev, int64_t ws_bytes, void* hip_stream);
 
 /* ds_dev [n][networks] of `type`: the gradient of the scores from dgates_dev fp32 [n][per_row] (nullable)
- * at the chosen ids (what stands at an id outside the networks is not read) and from dloss_dev fp32 [1]
+ * at the chosen ids, pnn_route's or others (what stands at an id outside the networks is not read), and from dloss_dev fp32 [1]
  * (nullable), the balance loss's (counts_dev; the counts themselves have no gradient).  ds_dev may be
  * s_dev (with the same distance between rows). */
 pnn_status pnn_route_grad(const pnn_router* args, const int32_t* ids_dev, const int32_t* counts_dev, const float* dgates_dev,

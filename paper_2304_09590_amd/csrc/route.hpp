@@ -459,9 +459,18 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
         }
         dot = route_sum<L>(dot);
         if (a.dgates) {
+            // (gates among the chosen ones count from their own largest score: ids may be any, and all far below the row's)
+            float peak = top;
+            if (a.normalize) {
+                peak = gate[0];
+#pragma unroll
+                for (int q = 1; q < KEEP; ++q) peak = fmaxf(peak, gate[q]);
+                peak = route_max<L>(peak);
+                if (peak == -RT_INF) peak = 0.0f;
+            }
 #pragma unroll
             for (int q = 0; q < KEEP; ++q) {
-                gate[q] = __builtin_amdgcn_exp2f((gate[q] - top) * RT_LOG2E);
+                gate[q] = __builtin_amdgcn_exp2f((gate[q] - peak) * RT_LOG2E);
                 if (id[q] >= 0) chosen += gate[q];
             }
             if (a.normalize) chosen = route_sum<L>(chosen);

@@ -22,3 +22,55 @@ def test_rows_after_each_other_on_the_same_lanes(n, K, k, dtype):
     ids = ids.cuda()
     for normalize in (False, True):
         near(pnn.route_grad(s, ids, None, dgates, normalize=normalize), *reference(s, k, normalize, dgates, 0.0, ids)[4], dtype=dtype)
+
+
+U = 2.0 ** -24
+
+
+def among_the_chosen(s, ids, dgates):
+    """The gradient through gates that are softmax among a row's ids, in 64 bits, and what it may be off by: an exponential of d by
+    (3 |d| + 2) U, the sum by its terms' and a step for each addition, then a quotient and products."""
+    K = s.shape[1]
+    i = ids.cpu().long()
+    kept = (i >= 0) & (i < K)
+    at = torch.where(kept, i, 0)
+    x = torch.where(kept, s.double().cpu().gather(1, at), -float("inf"))
+    top = x.amax(1, keepdim=True)
+    d = x - torch.where(torch.isfinite(top), top, 0.0)
+    e = torch.exp(d)
+    gates = e / torch.where(torch.isfinite(top), e.sum(1, keepdim=True), 1.0)
+    dg = torch.where(kept, dgates.double().cpu(), 0.0)
+    mix = (gates * dg).sum(1, keepdim=True)
+    rel = torch.where(gates > 0, (3 * d.abs() + 8) * U, 0.0)
+    rel = rel + (gates * rel).sum(1, keepdim=True) + 70 * U
+    mixoff = (gates * dg.abs() * (rel + 40 * U)).sum(1, keepdim=True)
+    off = gates * (rel * (dg - mix).abs() + mixoff + 8 * U * (dg.abs() + mix.abs()))
+    want, size = torch.zeros(s.shape, dtype=torch.float64), torch.zeros(s.shape, dtype=torch.float64)
+    return want.scatter_add(1, at, gates * (dg - mix)), size.scatter_add(1, at, off) + 1e-37
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,K,k", [(50, 3, 2), (9000, 16, 3), (9000, 200, 5), (200, 60, 9), (100, 500, 20), (60, 1000, 64)])
+def test_gates_among_networks_far_below_the_largest(n, K, k, dtype):
+    """A row's gates are among its chosen networks, however far others are above them."""
+    s, dgates = case(n, K, k, dtype, seed=K, scale=1.0)
+    s[:, 0] += torch.tensor([0.0, 80.0, 100.0, 150.0, 1e4, 1e30], device="cuda")[torch.arange(n, device="cuda") % 6].to(dtype)
+    ids = torch.stack([torch.randperm(K - 1, generator=torch.Generator().manual_seed(r))[:k] + 1 for r in range(n)]).to(torch.int32)
+    ids[1::8, 1:] = -1                        # one network: its gate is 1, whatever its score
+    ids[3::8] = K                             # none
+    s[5::8, 1] = -float("inf")
+    s[6::8, 1:] = -float("inf")               # all chosen ones are masked
+    s[7::8, 1:] -= 3e38                       # (the lowest ones)
+    ids = ids.cuda()
+    got = pnn.route_grad(s, ids, None, dgates, normalize=True)
+    want, off = among_the_chosen(s, ids, dgates)
+    assert (got[1::8] == 0).all() and (got[3::8] == 0).all() and (got[6::8] == 0).all()
+    assert (want[4::12].abs().sum(1) > 1e-3).any()
+    near(got, want, off, dtype=dtype)
+    # the balance loss's share does not change with it
+    counts, one = torch.ones(K + 1, dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda")
+    alone = pnn.route_grad(s.float(), ids, counts, None, one, normalize=True).double().cpu()
+    both = pnn.route_grad(s.float(), ids, counts, dgates, one, normalize=True)
+    want, off = among_the_chosen(s.float(), ids, dgates)
+    near(both, want + alone, off + U * (want + alone).abs() + 4 * U * want.abs())
