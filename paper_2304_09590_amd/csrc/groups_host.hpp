@@ -199,6 +199,8 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     // 1024 -> 4096 (1.1 GB) 530, 547.
     if (std::is_same<T, codes_t>::value && kind == RING_HUGE && a.Kx <= 1024 && p.P * a.M * (int64_t)sizeof(TO) >= (int64_t(96) << 20))
         kind = RING;
+    if (std::is_same<T, codes_t>::value && (kind == TILE64 || kind == TILE128))  // (the callers' checks leave none of these)
+        return fail(nullptr, PNN_EINVAL, "codes that do not start at multiples of 16 bytes");
     const int height = kind == FEW ? 0 : kind == TILE64 || kind == RING_SMALL ? 1 : kind == RING_HUGE ? 3 : 2;
     a.tiles = (const int2*)((const int32_t*)g->plan_dev + p.o_tiles[height]);
     a.n_tiles = (const int32_t*)g->plan_dev + p.o_count + height;
@@ -219,7 +221,7 @@ pnn_status run_group_pairs(GroupGemm& a, const pnn_groups* g, hipStream_t s) {
     const int64_t all = blocks(kind == TILE128 ? 128 : kind == TILE64 ? 64 : DIR == GR_FWD ? GS_OUT : sizeof(T) == 4 ? 64 : 128);
     TRY(grid_fits(all, 256));
     const char* what = DIR == GR_FWD ? "grouped forward" : "grouped input gradient";
-    if constexpr (!std::is_same<T, codes_t>::value) {  // (rows of codes are always at 16 bytes)
+    if constexpr (!std::is_same<T, codes_t>::value) {
         if (kind != FEW) {
             if (kind == TILE128) group_tile_kernel<DIR, T, TO, 128><<<(unsigned)all, 256, 0, s>>>(a);
             else group_tile_kernel<DIR, T, TO, 64><<<(unsigned)all, 256, 0, s>>>(a);
