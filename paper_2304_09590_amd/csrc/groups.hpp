@@ -371,6 +371,18 @@ __device__ inline typename Sum4<T>::type group_mfma(bf8v a, bf8v b, typename Sum
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// sum * sx * sw of codes, the row's scale first: within the range as long as that lies in 2^-90..2^90 (a sum is below 2^31, the rest one
+// rounding).  A row's scale outside is taken as one inside times 2^power, which the product gets back; a wave whose rows
+// have none takes the plain product (32,768 rows 1024 -> 4096 426 us a pass either way, 1,501 rows 501 -> 203 22.4 -> 23.0).
+__device__ inline int codes_power(float sx) {
+    const float size = __builtin_fabsf(sx);
+    return size > 0x1p90f ? 64 : size < 0x1p-90f && size > 0.0f ? -48 : 0;
+}
+__device__ inline float codes_value(float sum, float sx, int power, float sw, float bias) {
+    const float v = sum * sx;
+    return power == 0 ? __builtin_fmaf(v, sw, bias) : __builtin_amdgcn_ldexpf(v * sw, power) + bias;
+}
+
 // the first nv of eight values at p (the others 0); nv <= 0 reads nothing
 __device__ inline void load8(Raw8<bf16_t>& r, const bf16_t* p, int nv) {
     if (nv >= 8) {
@@ -599,6 +611,7 @@ __device__ inline void group_store(const GroupGemm& g, const typename Sum4<T>::t
     for (int h = 0; h < OWN; ++h) own[h] = DIR != GR_DW && wn + 64 * h + lane < nv ? g.pairs[p0 + wn + 64 * h + lane] : 0;
     constexpr bool CODES = std::is_same<T, codes_t>::value;
     float bias[8], scale_m[8], scale_n[OWN];
+    bool far = false;  // (a row of the wave's has such a scale)
     if (DIR == GR_FWD) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) bias[r] = g.b && r < left && e < g.K ? g.b[e * g.bnet + m + r] : 0.0f;
@@ -633,6 +646,10 @@ __device__ inline void group_store(const GroupGemm& g, const typename Sum4<T>::t
 #pragma unroll
         for (int i = 0; i < MI; ++i) *(f4*)(turn + l15 * LD + 16 * i + 4 * kg) = __builtin_convertvector(acc[i][j], f4);
         __builtin_amdgcn_wave_barrier();
+        if (CODES && j == 0) {  // (behind the first results' way to LDS)
+#pragma unroll
+            for (int h = 0; h < OWN; ++h) far |= __ballot(codes_power(scale_n[h]) != 0) != 0;
+        }
         auto leave = [&](int c, bool smooth) {
             const int col = c * COLS + lane / PER, n = column(j, c);
             const int64_t pair = DIR != GR_DW ? pair_of(j, c) : 0;
@@ -656,8 +673,15 @@ __device__ inline void group_store(const GroupGemm& g, const typename Sum4<T>::t
 #pragma unroll
                 for (int r = 0; r < 8; ++r) v[r] = 0.0f;
             } else if (DIR == GR_FWD) {
+                if (CODES && __builtin_expect(far, false)) {
+                    const int power = codes_power(by);
+                    const float inside = __builtin_amdgcn_ldexpf(by, -power);
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = CODES ? __builtin_fmaf(v[r] * by, scale_m[r], bias[r]) : v[r] + bias[r];
+                    for (int r = 0; r < 8; ++r) v[r] = codes_value(v[r], inside, power, scale_m[r], bias[r]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) v[r] = CODES ? __builtin_fmaf(v[r] * by, scale_m[r], bias[r]) : v[r] + bias[r];
+                }
                 if (smooth) group_act8(g.act, v);
                 else group_rectify8(g.act, v);
             } else if (has_with) {
@@ -1223,8 +1247,13 @@ __global__ __launch_bounds__(256) void group_few_fwd_kernel(GroupGemm g) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) sum += part[q][i][n][o + r];
             v = (float)sum;
-            if (std::is_same<T, codes_t>::value) v = v * g.sx[g.pdiv.of((int)pair)] * g.sw[e * g.swnet + m];
-            if (g.b) v += g.b[e * g.bnet + m];
+            if (std::is_same<T, codes_t>::value) {
+                const float sx = g.sx[g.pdiv.of((int)pair)];
+                const int power = codes_power(sx);
+                v = codes_value(v, __builtin_amdgcn_ldexpf(sx, -power), power, g.sw[e * g.swnet + m], g.b ? g.b[e * g.bnet + m] : 0.0f);
+            } else if (g.b) {
+                v += g.b[e * g.bnet + m];
+            }
             v = group_act(g.act, v);
         }
         ((TO*)g.y)[pair * g.ldy + m] = from_f<TO>(v);
