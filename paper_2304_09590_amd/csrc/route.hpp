@@ -49,6 +49,15 @@ __device__ inline void route_order() {
 constexpr float RT_INF = __builtin_huge_valf();
 constexpr float RT_LOG2E = 1.44269504f;
 
+// exp(d) for d <= 0, -inf among them: 2^t for the rounded t = d log2 e, times what the rounding leaves, 1 + (d - t ln 2).  The
+// remainder is below 2^-15 where 2^t is not 0, and no number for -inf, where the median is its bound and 2^t is 0.
+// Without it (in a row's sums, where the shares that are far off are small) the error grows by 2 |d| half steps; with it there too
+// 60,000 rows of 256 networks take 50.0 us for 48.3, 16,384 of 1,000 in bf16 54.4 for 52.2.
+__device__ inline float route_exp(float d) {
+    const float t = d * RT_LOG2E, e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, __builtin_amdgcn_fmed3f(__builtin_fmaf(-t, 0.693147181f, d), -0x1p-12f, 0x1p-12f), e);
+}
+
 // A row lies on L lanes, V scores each: chunks of CH neighbouring ones, the lanes' chunks side by side.
 template <int L, int V>
 struct RouteLane {
@@ -245,7 +254,7 @@ __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
         float ge[KEEP], chosen = 0.0f;
 #pragma unroll
         for (int q = 0; q < KEEP; ++q) {
-            ge[q] = id[q] >= 0 ? __builtin_amdgcn_exp2f((route_value<T>(key[q]) - top) * RT_LOG2E) : 0.0f;
+            ge[q] = id[q] >= 0 ? route_exp(route_value<T>(key[q]) - top) : 0.0f;
             chosen += ge[q];
         }
         if (a.normalize) chosen = route_sum<L>(chosen);
@@ -470,7 +479,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
             }
 #pragma unroll
             for (int q = 0; q < KEEP; ++q) {
-                gate[q] = __builtin_amdgcn_exp2f((gate[q] - peak) * RT_LOG2E);
+                gate[q] = route_exp(gate[q] - peak);
                 if (id[q] >= 0) chosen += gate[q];
             }
             if (a.normalize) chosen = route_sum<L>(chosen);

@@ -74,3 +74,21 @@ def test_gates_among_networks_far_below_the_largest(n, K, k, dtype):
     both = pnn.route_grad(s.float(), ids, counts, dgates, one, normalize=True)
     want, off = among_the_chosen(s.float(), ids, dgates)
     near(both, want + alone, off + U * (want + alone).abs() + 4 * U * want.abs())
+
+
+@gpu
+@pytest.mark.parametrize("n,K,k", [(9, 16, 16), (9000, 40, 33), (100, 200, 64), (5000, 500, 40), (64, 1000, 64)])
+def test_gates_of_rows_with_a_wide_spread(n, K, k):
+    """Scores whose differences are exact, down to 80 below the largest: a gate is off by its exponential's four half steps, the sum's and a
+    quotient's, whatever its size."""
+    g = torch.Generator().manual_seed(K)
+    s = (torch.rand(n, K, generator=g) * 80 * 16).floor() / 16  # (11 bits)
+    s[:, 0] = 80.0
+    for normalize in (False, True):
+        ids, gates, _, _ = pnn.route(s.cuda(), k, normalize=normalize)
+        x = s.double().gather(1, ids.cpu().long())
+        e = torch.exp(s.double() - 80)
+        # (terms of the sum: 3 |d| + 2 each, far ones weigh little)
+        rel = ((e * (3 * (80 - s.double()) + 2)).sum(1, keepdim=True) / e.sum(1, keepdim=True) + 40) * U
+        want = torch.softmax(x, 1) if normalize else torch.exp(x - 80) / e.sum(1, keepdim=True)
+        assert ((gates.double().cpu() - want).abs() <= want * (8 * U + rel) + 1e-37).all()
