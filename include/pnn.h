@@ -430,9 +430,10 @@ typedef struct {
     int64_t n;                        /* 0..2^40 */
 } pnn_adamw_tensor;
 
-/* A plan of the tensors (host array, read during the call; values are contiguous and aligned to their types, no two
- * tensors that a step writes overlap): where a step finds them, as long as they stay where they are.  All have `bits`
- * and g_type.  plan_dev is 16-byte aligned; a program lays it out once. */
+/* A plan of the tensors (host array, read during the call; values are contiguous and aligned to their types): where a step
+ * finds them, as long as they stay where they are.  Nothing that a step writes overlaps; a gradient may be its own tensor's p, m, v
+ * or copy, value by value, and overlaps nothing else of these.  All have `bits` and g_type.  plan_dev is 16-byte aligned;
+ * a program lays it out once. */
 pnn_status pnn_adamw_bytes(const pnn_adamw_tensor* tensors, int32_t count, int64_t* bytes, int64_t* chunks);
 pnn_status pnn_adamw_plan(const pnn_adamw_tensor* tensors, int32_t count, int32_t bits, int32_t g_type, void* plan_dev,
                           int64_t plan_bytes, void* hip_stream);

@@ -751,6 +751,30 @@ def combine_grad(dout, y, ids, gates, networks: int, dy=None, stream=None):
     return _on(stream, body, y, dout, ids, gates, dy)
 
 
+def _check_apart(spans, steps, lr) -> None:
+    """No two of the tensors that a step of AdamW writes overlap, and what it reads does not overlap them either, but for a gradient
+    that is one of its own tensor's, value by value (a step reads a value's gradient before it writes anything of it)."""
+    count = len(spans[0][0])
+
+    def of(fields, more=()):
+        at = np.concatenate([spans[f][0] for f in fields] + [[x[0]] for x in more])
+        size = np.concatenate([spans[f][1] for f in fields] + [[x[1]] for x in more])
+        tensor = np.concatenate([np.arange(count)] * len(fields) + [[-1]] * len(more))
+        return at[size > 0], (at + size)[size > 0], tensor[size > 0]
+
+    first, end, tensor = of([f for f in spans if f != 1], [steps])
+    order = np.argsort(first)
+    first, end, tensor = first[order], end[order], tensor[order]
+    if (first[1:] < end[:-1]).any():
+        raise ValueError("two of the tensors that a step writes overlap")
+    read, until, mine = of([1], [lr] if lr is not None else [])
+    at = np.minimum(np.searchsorted(end, read, side="right"), len(end) - 1)  # the first that ends behind it, if any does
+    meets = (first[at] < until) & (end[at] > read)
+    same = (first[at] == read) & (end[at] == until) & (tensor[at] == mine) & (mine >= 0)
+    if (meets & ~same).any():
+        raise ValueError("a gradient or the rate overlaps what a step writes")
+
+
 class AdamW:
     """AdamW over many tensors at once (pnn_adamw_step): fp32 params, their gradients (float32 or bfloat16, read by every
     step from the tensors given here), optionally bf16 copies that each step writes (None for a tensor without
@@ -787,7 +811,7 @@ class AdamW:
         dev = first.get_device()
         table = np.zeros((count, len(PnnAdamwTensor._fields_)), dtype=np.int64)  # (an entry's fields are 8 bytes each)
         table[:, 7] = sizes
-        written, lengths = [], []
+        spans = {}  # field: (addresses, bytes) of the tensors
         columns = [(0, "params", self.params, torch.float32, sizes), (1, "grads", self.grads, self.grads[0].dtype, sizes),
                    (2, "m", self.state[0], held, sizes), (3, "v", self.state[1], held, sizes)]
         if bits == 8:
@@ -802,19 +826,11 @@ class AdamW:
                     raise ValueError(f"{name}[{i}] is {tuple(x.shape)} of {x.dtype} on {x.device}, expected {n} contiguous values of {dtype} "
                                      f"on {first.device}")
             table[:, field] = [0 if x is None else x.data_ptr() for x in column]
-            if field != 1:
-                written.append(table[:, field])
-                lengths.append(np.where(table[:, field] != 0, np.asarray(expected) * dtype.itemsize, 0))
-        written, lengths = np.concatenate(written), np.concatenate(lengths)
-        order = np.argsort(written[lengths > 0])
-        written, lengths = written[lengths > 0][order], lengths[lengths > 0][order]
-        if (written[1:] < written[:-1] + lengths[:-1]).any():
-            raise ValueError("two of the tensors that a step writes overlap")
+            spans[field] = table[:, field], np.where(table[:, field] != 0, np.asarray(expected) * dtype.itemsize, 0)
         tensors = table.ctypes.data_as(ctypes.POINTER(PnnAdamwTensor))
-        _values(self.steps, "steps", (2,), torch.int32)
         self._lr = lr if torch.is_tensor(lr) else None
-        if self._lr is not None:
-            _values(self._lr, "lr", (1,), torch.float32)
+        _check_apart(spans, (_values(self.steps, "steps", (2,), torch.int32), 8),
+                     None if self._lr is None else (_values(self._lr, "lr", (1,), torch.float32), 4))
 
         def body(h):
             size, chunks = ctypes.c_int64(), ctypes.c_int64()
