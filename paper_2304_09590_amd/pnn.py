@@ -840,6 +840,8 @@ class AdamW:
             return plan, chunks.value, h
 
         self._plan, chunks, self._made = _on(None, body, first, self.steps, self._lr)
+        # (kept by itself: a tensor may get other memory, and a step would write to what was given back)
+        self._memory = [x.untyped_storage() for column in columns for x in column[2] if x is not None]
         self._recorded = set()  # handles of other streams that steps have been taken on
         self.args = PnnAdamw(self._plan.data_ptr(), chunks, bits, kind, 0.0 if self._lr is not None else lr, betas[0], betas[1], eps,
                              weight_decay, None if self._lr is None else self._lr.data_ptr(), seed & 0xFFFFFFFF, self.steps.data_ptr())
@@ -855,7 +857,7 @@ class AdamW:
         self.args.lr = value
 
     def step(self, stream=None) -> None:
-        """One step with what the gradients hold now."""
+        """One step with what the gradients hold now.  A graph that it is recorded into needs the object as long as it is replayed."""
         torch = _t()
         # on another stream than the object's, its tensors are recorded, once (they stay so until their memory is given back):
         # the object may go away while the step waits

@@ -45,3 +45,28 @@ def test_a_step_of_another_kind_than_the_plans_does_nothing(held, asked, n):
     opt.args.bits, opt.args.g_type = held
     opt.step()
     assert opt.steps.tolist() == [1, 0] and not torch.equal(memory[0], before[0])
+
+
+def test_memory_is_the_objects(monkeypatch):
+    """A parameter whose data is replaced: the memory that steps write stays the object's."""
+    monkeypatch.setattr(pnn, "_on", lambda stream, body, *a, **kw: (torch.zeros(1), 0, 0))
+    p, g = torch.zeros(1000), torch.zeros(1000, dtype=torch.bfloat16)
+    at = [p.data_ptr(), g.data_ptr()]
+    opt = pnn.AdamW([p], [g], copies=[None])
+    p.data, g.data = torch.ones(1000), torch.ones(1000, dtype=torch.bfloat16)
+    assert set(at) <= {m.data_ptr() for m in opt._memory}
+    assert all(t.data_ptr() in {m.data_ptr() for m in opt._memory} for s in opt.state for t in s)
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_after_a_parameters_data_was_replaced(bits):
+    n = 3_000_000
+    p, g = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    opt = pnn.AdamW([p], [g], bits=bits)
+    at = p.data_ptr(), g.data_ptr()
+    p.data, g.data = torch.full((n,), 5.0, device="cuda"), torch.full((n,), 6.0, device="cuda")
+    others = [torch.full((n,), 7.0, device="cuda") for _ in range(4)]
+    assert not {t.data_ptr() for t in others} & set(at)
+    opt.step()
+    assert all((t == 7).all() for t in others) and (p == 5).all() and (g == 6).all() and opt.steps.tolist() == [1, 0]

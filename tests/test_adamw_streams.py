@@ -31,6 +31,9 @@ class Tensor(StandIn):
     def data_ptr(self):
         return self.at
 
+    def untyped_storage(self):
+        return self
+
     def new_empty(self, shape, dtype=None):
         return Tensor((shape,) if isinstance(shape, int) else shape, dtype or self.dtype)
 
