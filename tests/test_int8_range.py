@@ -68,3 +68,21 @@ def test_large_rows_and_small_weights(n, K):
     want = (w[ids.long()].double() @ x.double()[:, :, None])[:, :, 0]
     # (codes of 127 alone: the scales' roundings, the sum's and two products', of the terms' sizes at most)
     assert ((got.double() - want).abs() <= 6 * U * want.abs()).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,k,K,I,O", SHAPES)
+def test_powers_of_two_change_nothing_else(n, k, K, I, O):
+    """A row's scale times 2^100 or 2^-100 is its results times that, to the bit, and its neighbours' results stay."""
+    g = np.random.default_rng(n)
+    x, w = (torch.from_numpy(g.integers(-127, 128, s).astype(np.int8)).cuda() for s in ((n, I), (K, O, I)))
+    xs, ws = torch.from_numpy(scales((n,), [0, 1], 1)).cuda(), torch.from_numpy(scales((K, O), [-20, -19], 2)).cuda()
+    b = torch.from_numpy(g.standard_normal((K, O)).astype(np.float32)).cuda()
+    groups = pnn.group_rows(torch.from_numpy(g.integers(0, K, (n, k)).astype(np.int32)).cuda(), K)
+    power = torch.from_numpy(g.choice([0, 0, 0, 100, -100], n)).cuda()
+    plain = pnn.grouped_forward_int8(groups, x, xs, w, ws)
+    got = pnn.grouped_forward_int8(groups, x, torch.ldexp(xs.double(), power).float(), w, ws)
+    assert torch.equal(got, torch.ldexp(plain.double(), power.repeat_interleave(k)[:, None]).float())
+    same = (power == 0).repeat_interleave(k)
+    got = pnn.grouped_forward_int8(groups, x, torch.ldexp(xs.double(), power).float(), w, ws, b)
+    assert torch.equal(got[same], pnn.grouped_forward_int8(groups, x, xs, w, ws, b)[same])
