@@ -13,8 +13,8 @@
 // function of the seed, the step, the tensor, the block and the place, so the same call gives the same bits.
 //
 // Bound by bytes: with fp32 gradients 28 a value, or 16 and the scales in 8 bits, 2 more for a copy.  34.3 million values
-// with copies: 193 us in 32 bits (5.3 TB/s), 120 to 133 us in 8 (5.2 to 4.7 TB/s), where instructions take 0.8 of the
-// cycles.  What brought the latter there from 251 us: levels from LDS instead of their formula and codes without branches
+// with copies: 193 us in 32 bits (5.3 TB/s), 120 to 141 us in 8 (5.2 to 4.4 TB/s: cards differ, and a pass among others takes
+// less than one under the profiler), where instructions take 0.83 of the cycles.  What brought the latter there from 251 us: levels from LDS instead of their formula and codes without branches
 // (187 -> 160), global addresses with scalar bases instead of flat ones (160 -> 118, at gradients alike; 138 at unlike
 // ones), whole chunks without looking for ends (138 -> 125), and the places below (58 ns for each of 1,024 workgroups).
 #pragma once
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(64 * WAVES) void adamw_kernel(AdamArgs a) {
     }
 }
 
-// What 8-bit states stand for: 34.3 million values in 69 us, 5.0 TB/s.
+// What 8-bit states stand for: 34.3 million values in 66 to 69 us, 5.3 to 5.0 TB/s.
 __global__ __launch_bounds__(256) void adamw_values_kernel(const uint8_t* qm, const uint8_t* qv, const float* sm, const float* sv, int64_t n,
                                                            float* m, float* v) {
     __shared__ AdamLevels<127> m_levels;

@@ -66,7 +66,7 @@ struct Codes16 {
 
 // G threads a row, 16 values of it each at a time; a row that one step holds is read once, and the next one's values are
 // loaded while this one's are turned.  32,768 rows of 1,024 in fp32: 28 us (6.1 TB/s; x fits the memory-side cache), in bf16
-// 27 (38 with the middles decided in fp64, in every wave).
+// 24 to 27 (38 with the middles decided in fp64, in every wave).
 template <typename T, int G>
 __global__ __launch_bounds__(256) void codes_kernel(CodesArgs a) {
     __shared__ uint32_t red[4];

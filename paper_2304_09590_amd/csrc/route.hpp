@@ -166,8 +166,8 @@ template <int L> __device__ inline int route_top(int v) {
 // Choosing is k times the largest of the row's lanes' largest (the lowest index on ties).  The lane that held it then
 // needs its next: its V keys lie in LDS, where 16 lanes look at one each, so a choice costs the same whatever V is.
 // 16,384 rows of 1,000 scores in bf16, eight each: 59 us with all lanes' scores looked through again for each choice, 35
-// this way, 21 with keys that hold their columns and the next row's scores on their way (33 MB: 7 us; the rest is the
-// choices' instructions, a third of them exchanges between lanes).  60,000 rows of 256 in fp32, two each: 16 us, 61 MB.
+// this way, 21 to 24 with keys that hold their columns and the next row's scores on their way (33 MB: 7 us; the rest is the
+// choices' instructions, a third of them exchanges between lanes).  60,000 rows of 256 in fp32, two each: 17 us, 61 MB.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(RT_THREADS) void route_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
@@ -408,7 +408,7 @@ __device__ inline void route_store4(bf16_t* p, const float* v, int nv) {
 
 // What the gates add lies in LDS, a place for each score of the row, where the lanes that hold the choices write theirs (a
 // network that stands twice gets a sum in the order of the choices).  Bound by bytes where rows are many: 60,000 rows of 256
-// scores in fp32 26 us, 4.7 TB/s; 16,384 of 1,000 in bf16 20 to 24 us, 2.7 to 3.3 TB/s, instructions and the counts at its beginning.
+// scores in fp32 26 to 27 us, 4.7 to 4.6 TB/s; 16,384 of 1,000 in bf16 20 to 24 us, 2.7 to 3.3 TB/s, instructions and the counts at its beginning.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void route_grad_kernel(RouteArgs a) {
     typedef RouteLane<L, V> At;
@@ -565,7 +565,7 @@ struct CombineArgs {
 };
 
 // Eight neighbouring values a thread; a dropped pair's rows are not read.  Bound by bytes: 32,768 rows of two pairs of 4,096
-// values in bf16, 805 MB in 145 us (5.5 TB/s).
+// values in bf16, 805 MB in 143 us (5.6 TB/s).
 template <typename T, typename TO>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     const int rows = 256 / a.threads, tx = threadIdx.x % a.threads, ty = threadIdx.x / a.threads;
